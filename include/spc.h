@@ -365,6 +365,90 @@ int spc_permute_rows(const void* src, int64_t src_pitch, const int32_t* perm, in
                      void* dst, int64_t dst_pitch, void* stream);
 
 /*
+ * Layer norm of feature rows: z = x (+ residual), y = (z - mean(z)) / sqrt(var(z) + eps) * gamma + beta over the c channels
+ * of every row.  Sums and statistics are held in 32 bits.
+ *   x, residual   [device] n rows of c elements, row pitches ld_x, ld_r in elements; residual may be NULL.
+ *   gamma, beta   [device] c floats, whatever the rows' type; NULL stands for ones and zeros.
+ *   y, sum        [device] rows of the same type.  sum receives z, rounded to the rows' type (the norm itself is of the
+ *                 unrounded z); required with a residual, NULL without.
+ *   mean, rstd    [device] n floats each, for the backward pass; both or neither.
+ * 1 <= c <= 8192 (SPC_ERR_UNSUPPORTED above).  y and sum may be x or residual themselves (same pitch); otherwise
+ * outputs do not overlap inputs.  An infinity or NaN reaches its own row only.  Enqueues one kernel and waits for nothing.
+ */
+int spc_layer_norm_forward(const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const float* gamma,
+                           const float* beta, float eps, void* y, int64_t ld_y, void* sum, int64_t ld_s, float* mean,
+                           float* rstd, int64_t n, int32_t c, int32_t dtype, void* stream);
+/*
+ * Its gradients.  x: the rows that were normalised (spc_layer_norm_forward's x, or its sum where there was a residual); mean, rstd as
+ * the forward pass stored them; dsum: a gradient that reaches the sum past the norm, added to dx, may be NULL.
+ *   dx             [device] gradient of x, and of the residual; may be dy, x or dsum itself (same pitch).
+ *   dgamma, dbeta  [device] c floats, either may be NULL; overwritten.  Rows are added up in a fixed order (no atomics).
+ * Scratch comes from the library's block cache (as for spc_conv_forward: a warmed-up call can be captured).
+ */
+int spc_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const float* mean,
+                            const float* rstd, const float* gamma, const void* dsum, int64_t ld_ds, void* dx,
+                            int64_t ld_dx, float* dgamma, float* dbeta, int64_t n, int32_t c, int32_t dtype,
+                            void* stream);
+
+/*
+ * Linear attention with a decay for each head, along the rows of every scene in their (sorted) order:
+ *   S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T,   out_t = scale S_t^T q_t,   S of dk x dv, in 32 bits.
+ * heads query heads, of which heads / kv_heads consecutive ones share a head of keys and values.
+ * Heads have 1 to 128 channels (SPC_ERR_UNSUPPORTED above).
+ */
+typedef struct spc_attn_desc {
+  int32_t dtype;
+  int32_t n_scenes;
+  int64_t n_rows; /* below 2^31 */
+  int32_t heads, kv_heads;
+  int32_t dk, dv; /* channels of a head of queries and keys, of values and outputs */
+  float scale;
+} spc_attn_desc;
+/* Channel c of head h of row r is element r * row_pitch + h * head_pitch + c.  Pitches of inputs may be zero (broadcast). */
+typedef struct spc_attn_rows {
+  void* data; /* [device] */
+  int64_t row_pitch, head_pitch;
+} spc_attn_rows;
+/*
+ *   q, out      rows of `heads` heads; k, v: of kv_heads.  out overlaps no input.
+ *   log_decay   [device] `heads` floats, ln of the decay: <= 0, -infinity forgets at once.
+ *   offsets     [device] n_scenes + 1 ascending row numbers: scene b holds rows offsets[b] .. offsets[b+1]-1 (it may be empty).  Rows
+ *               in no scene are neither read nor written, so padded buffers need no host count.  NULL: one scene of all rows.
+ *   state_in    [device] [n_scenes][heads][dk][dv] floats, S before each scene's first row; NULL: zeros.
+ *   state_out   [device] the same shape, S behind each scene's last row (state_in for an empty scene); may be NULL; not state_in itself.
+ * An infinity or NaN in row t reaches rows from t on of its scene (and heads that read it) only.
+ * Products and sums are accumulated in 32 bits; results are bit-reproducible.  Scratch comes from the library's block cache (as
+ * for spc_conv_forward: a warmed-up call can be captured); nothing is waited for.
+ */
+int spc_linear_attention_forward(const spc_attn_desc* d, const spc_attn_rows* q, const spc_attn_rows* k,
+                                 const spc_attn_rows* v, const float* log_decay, const int32_t* offsets,
+                                 const float* state_in, const spc_attn_rows* out, float* state_out, void* stream);
+/*
+ * Its gradients (the decays are constants of the layer).  dout: gradient of out; state_in as in the forward pass; dstate_out: gradient of
+ * state_out, may be NULL (zeros).  dq, dk, dv overlap no input; dk and dv are sums over the heads that share them.  dstate_in [device]:
+ * gradient of state_in, may be NULL; not dstate_out itself.
+ */
+int spc_linear_attention_backward(const spc_attn_desc* d, const spc_attn_rows* dout, const spc_attn_rows* q,
+                                  const spc_attn_rows* k, const spc_attn_rows* v, const float* log_decay,
+                                  const int32_t* offsets, const float* state_in, const float* dstate_out,
+                                  const spc_attn_rows* dq, const spc_attn_rows* dk, const spc_attn_rows* dv,
+                                  float* dstate_in, void* stream);
+/*
+ * One more row of n_rows independent streams (n_scenes is not read): row r of q, k, v, out belongs to stream r, whose state
+ * [n_rows][heads][dk][dv] floats [device] is updated in place.  out overlaps no input.
+ */
+int spc_linear_attention_step(const spc_attn_desc* d, const spc_attn_rows* q, const spc_attn_rows* k,
+                              const spc_attn_rows* v, const float* log_decay, float* state, const spc_attn_rows* out,
+                              void* stream);
+/*
+ * offsets[b] = first of the n sorted keys whose batch index is b or more, b = 0 .. n_batch (offsets [device] n_batch + 1 int32): the
+ * scenes of the rows that spc_pack_coords has sorted.  Rejected rows (all-ones keys) lie behind the last scene if the descriptor's batch field has
+ * room for an index beyond n_batch - 1.
+ */
+int spc_batch_offsets(const void* keys, int64_t n, const spc_pack_desc* d, int32_t n_batch, int32_t* offsets,
+                      void* stream);
+
+/*
  * Measurement aids (Section 6 reports rates; these give the machine's own denominators next to the data-sheet
  * ones).  spc_probe_copy: a plain copy kernel, dst[0..bytes) = src[0..bytes) ([device], bytes a multiple of 16):
  * its rate is what a streaming kernel can reach on this GPU, and its known size calibrates the profiler's byte

@@ -44,6 +44,8 @@ EXPORTS = [
     "spc_kmap_ws_lists", "spc_kmap_nnz", "spc_kmap_search_info", "spc_search_count", "spc_resident_count", "spc_kmap_export_triples", "spc_kmap_set_size_hint", "spc_kmap_destroy",
     "spc_conv_forward", "spc_conv_forward_hybrid", "spc_conv_tune_threshold",
     "spc_conv_prepare_weights", "spc_permute_rows",
+    "spc_layer_norm_forward", "spc_layer_norm_backward",
+    "spc_linear_attention_forward", "spc_linear_attention_backward", "spc_linear_attention_step", "spc_batch_offsets",
     "spc_probe_copy", "spc_probe_mfma",
     "spc_release_cache", "spc_last_error", "spc_version",
 ]
@@ -68,6 +70,15 @@ class PackDesc(ctypes.Structure):
 class LayerDesc(ctypes.Structure):
     _fields_ = [("K", ctypes.c_int32), ("in_stride", ctypes.c_int32), ("layer_stride", ctypes.c_int32),
                 ("transposed", ctypes.c_int32), ("layout", ctypes.c_int32)]
+
+
+class AttnDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_scenes", ctypes.c_int32), ("n_rows", ctypes.c_int64), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("dk", ctypes.c_int32), ("dv", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class AttnRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_pitch", ctypes.c_int64), ("head_pitch", ctypes.c_int64)]
 
 
 _lib = None
@@ -112,6 +123,13 @@ def lib():
         L.spc_conv_tune_threshold.argtypes = [vp, vp, i64, vp, vp, vp, i64, i32, i32, i32, i32, i32, ctypes.c_float,
                                               ctypes.POINTER(ctypes.c_float), i32, ctypes.POINTER(i32), ctypes.POINTER(i32), vp]
         L.spc_permute_rows.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp]
+        f32, ad, ar = ctypes.c_float, ctypes.POINTER(AttnDesc), ctypes.POINTER(AttnRows)
+        L.spc_layer_norm_forward.argtypes = [vp, i64, vp, i64, vp, vp, f32, vp, i64, vp, i64, vp, vp, i64, i32, i32, vp]
+        L.spc_layer_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, i64, i32, i32, vp]
+        L.spc_linear_attention_forward.argtypes = [ad, ar, ar, ar, vp, vp, vp, ar, vp, vp]
+        L.spc_linear_attention_backward.argtypes = [ad, ar, ar, ar, ar, vp, vp, vp, vp, ar, ar, ar, vp, vp]
+        L.spc_linear_attention_step.argtypes = [ad, ar, ar, ar, vp, vp, ar, vp]
+        L.spc_batch_offsets.argtypes = [vp, i64, ctypes.POINTER(PackDesc), i32, vp, vp]
         L.spc_probe_copy.argtypes = [vp, vp, i64, vp]
         L.spc_probe_mfma.argtypes = [i32, vp, ctypes.POINTER(ctypes.c_double), vp]
         L.spc_last_error.restype = ctypes.c_char_p
@@ -406,6 +424,153 @@ def spc_permute_rows(src: torch.Tensor, perm: torch.Tensor, out: torch.Tensor | 
     es = src.element_size()
     _check(lib().spc_permute_rows(src.data_ptr(), src.stride(0) * es, perm.data_ptr(), perm.shape[0], src.shape[1] * es,
                                   out.data_ptr(), out.stride(0) * es, _stream(stream)))
+    return out
+
+
+def _norm_rows(t: torch.Tensor, like: torch.Tensor) -> int:
+    """Row pitch of a matrix of like's shape and type on its device."""
+    st = t.stride()
+    assert t.is_cuda and t.device == like.device and t.dtype == like.dtype and t.shape == like.shape
+    assert len(st) == 2 and (st[1] == 1 or t.shape[1] <= 1)
+    # (the pitch of a matrix of one row may be anything)
+    return st[0] if t.shape[0] > 1 else max(st[0], t.shape[1])
+
+
+def _f32(t: torch.Tensor | None, shape, device) -> int | None:
+    """Pointer of an optional contiguous fp32 tensor of this shape."""
+    if t is None:
+        return None
+    assert t.dtype == torch.float32 and t.shape == shape and t.is_contiguous() and t.device == device
+    return t.data_ptr()
+
+
+def spc_layer_norm_forward(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None, eps: float = 1e-5,
+                           residual: torch.Tensor | None = None, out: torch.Tensor | None = None, sum_out: torch.Tensor | None = None,
+                           want_stats: bool = False, stream=None):
+    """Layer norm of the rows of x [n, c] (+ residual); gamma, beta [c] fp32.  Row pitches = stride(0).  Returns (y, sum, mean, rstd): sum is
+    None without a residual, mean and rstd [n] fp32 are None without want_stats."""
+    assert x.is_cuda and x.dim() == 2 and x.dtype in _TORCH_DTYPE
+    (n, c), dev = x.shape, x.device
+    y = torch.empty((n, c), dtype=x.dtype, device=dev) if out is None else out
+    total = None
+    if residual is not None:
+        total = torch.empty((n, c), dtype=x.dtype, device=dev) if sum_out is None else sum_out
+    else:
+        assert sum_out is None
+    mean = rstd = None
+    if want_stats:
+        mean, rstd = torch.empty((2, n), dtype=torch.float32, device=dev)
+    rc = lib().spc_layer_norm_forward(x.data_ptr(), _norm_rows(x, x), residual.data_ptr() if residual is not None else None,
+                                      _norm_rows(residual, x) if residual is not None else 0, _f32(gamma, (c,), dev), _f32(beta, (c,), dev),
+                                      eps, y.data_ptr(), _norm_rows(y, x), total.data_ptr() if total is not None else None,
+                                      _norm_rows(total, x) if total is not None else 0, mean.data_ptr() if want_stats else None,
+                                      rstd.data_ptr() if want_stats else None, n, c, _TORCH_DTYPE[x.dtype],
+                                      current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return y, total, mean, rstd
+
+
+def spc_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: torch.Tensor | None = None,
+                            dsum: torch.Tensor | None = None, out: torch.Tensor | None = None, want_params: bool = True, stream=None):
+    """Gradients of spc_layer_norm_forward; x is its x, or its sum where there was a residual, dsum [n, c] a gradient that reaches that sum past
+    the norm.  Returns (dx, dgamma, dbeta), the last two [c] fp32, or None without want_params."""
+    assert x.is_cuda and x.dim() == 2 and x.dtype in _TORCH_DTYPE
+    (n, c), dev = x.shape, x.device
+    dx = torch.empty((n, c), dtype=x.dtype, device=dev) if out is None else out
+    dgamma = dbeta = None
+    if want_params:
+        dgamma, dbeta = torch.empty((2, c), dtype=torch.float32, device=dev)
+    rc = lib().spc_layer_norm_backward(dy.data_ptr(), _norm_rows(dy, x), x.data_ptr(), _norm_rows(x, x), _f32(mean, (n,), dev),
+                                       _f32(rstd, (n,), dev), _f32(gamma, (c,), dev), dsum.data_ptr() if dsum is not None else None,
+                                       _norm_rows(dsum, x) if dsum is not None else 0, dx.data_ptr(), _norm_rows(dx, x),
+                                       dgamma.data_ptr() if want_params else None, dbeta.data_ptr() if want_params else None, n, c,
+                                       _TORCH_DTYPE[x.dtype], current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return dx, dgamma, dbeta
+
+
+def _heads(t: torch.Tensor, n: int, heads: int, width: int, like: torch.Tensor) -> AttnRows:
+    st = t.stride()
+    assert t.is_cuda and t.device == like.device and t.dtype == like.dtype and t.shape == (n, heads, width) and (st[2] == 1 or width == 1)
+    return AttnRows(t.data_ptr(), st[0], st[1])
+
+
+def _attention(q, k, v, log_decay, offsets, scale):
+    """What the calls share: (descriptor, q, k, v in C form, log_decay's and offsets' addresses)."""
+    assert q.is_cuda and q.dim() == 3 and k.dim() == 3 and v.dim() == 3 and q.dtype in _TORCH_DTYPE
+    (n, heads, dk), (kv, dv), dev = q.shape, v.shape[1:], q.device
+    n_scenes = 1
+    if offsets is not None:
+        n_scenes = offsets.shape[0] - 1
+        assert offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.is_contiguous() and offsets.device == dev
+    d = AttnDesc(_TORCH_DTYPE[q.dtype], n_scenes, n, heads, kv, dk, dv, dk ** -0.5 if scale is None else scale)
+    return d, _heads(q, n, heads, dk, q), _heads(k, n, kv, dk, q), _heads(v, n, kv, dv, q), _f32(log_decay, (heads,), dev), \
+        None if offsets is None else offsets.data_ptr()
+
+
+def spc_linear_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, offsets: torch.Tensor | None = None,
+                                 scale: float | None = None, initial_state: torch.Tensor | None = None, want_state: bool = False,
+                                 out: torch.Tensor | None = None, state_out: torch.Tensor | None = None, stream=None):
+    """q [n, heads, dk], k [n, kv_heads, dk], v [n, kv_heads, dv] (any row and head pitch, e.g. column ranges of one projection's output);
+    log_decay [heads] fp32, <= 0; offsets [scenes + 1] int32 (spc_batch_offsets), None: one scene; scale None: dk ** -0.5; states
+    [scenes, heads, dk, dv] fp32.  Returns (out [n, heads, dv], state behind every scene's last row, or None)."""
+    d, rq, rk, rv, g, at = _attention(q, k, v, log_decay, offsets, scale)
+    n, heads, dev = d.n_rows, d.heads, q.device
+    shape = (d.n_scenes, heads, d.dk, d.dv)
+    if out is None:
+        out = torch.empty((n, heads, d.dv), dtype=q.dtype, device=dev)
+    if state_out is None and want_state:
+        state_out = torch.empty(shape, dtype=torch.float32, device=dev)
+    ro = _heads(out, n, heads, d.dv, q)
+    rc = lib().spc_linear_attention_forward(d, rq, rk, rv, g, at, _f32(initial_state, shape, dev), ro, _f32(state_out, shape, dev),
+                                            current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return out, state_out
+
+
+def spc_linear_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
+                                  offsets: torch.Tensor | None = None, scale: float | None = None, initial_state: torch.Tensor | None = None,
+                                  dstate: torch.Tensor | None = None, want_dinitial: bool = False, out=None, stream=None):
+    """Gradients of spc_linear_attention_forward; dstate: gradient of the state it returned.  out: (dq, dk, dv) to write to.  Returns
+    (dq, dk, dv, gradient of initial_state or None)."""
+    d, rq, rk, rv, g, at = _attention(q, k, v, log_decay, offsets, scale)
+    n, heads, kv, dev = d.n_rows, d.heads, d.kv_heads, q.device
+    shape = (d.n_scenes, heads, d.dk, d.dv)
+    if out is None:
+        out = tuple(torch.empty(s, dtype=q.dtype, device=dev) for s in ((n, heads, d.dk), (n, kv, d.dk), (n, kv, d.dv)))
+    dinitial = torch.empty(shape, dtype=torch.float32, device=dev) if want_dinitial else None
+    rc = lib().spc_linear_attention_backward(d, _heads(dout, n, heads, d.dv, q), rq, rk, rv, g, at, _f32(initial_state, shape, dev),
+                                             _f32(dstate, shape, dev), _heads(out[0], n, heads, d.dk, q), _heads(out[1], n, kv, d.dk, q),
+                                             _heads(out[2], n, kv, d.dv, q), _f32(dinitial, shape, dev),
+                                             current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return (*out, dinitial)
+
+
+def spc_linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, state: torch.Tensor,
+                              scale: float | None = None, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """One more row for every stream: q [streams, heads, dk] and so on; state [streams, heads, dk, dv] fp32 is updated in place."""
+    d, rq, rk, rv, g, _ = _attention(q, k, v, log_decay, None, scale)
+    if out is None:
+        out = torch.empty((d.n_rows, d.heads, d.dv), dtype=q.dtype, device=q.device)
+    rc = lib().spc_linear_attention_step(d, rq, rk, rv, g, _f32(state, (d.n_rows, d.heads, d.dk, d.dv), q.device),
+                                         _heads(out, d.n_rows, d.heads, d.dv, q), current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return out
+
+
+def spc_batch_offsets(keys: torch.Tensor, desc: PackDesc, n_batch: int, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """First row of every scene in sorted keys, and their end: int32 [n_batch + 1]."""
+    assert keys.dim() == 1 and keys.dtype == (torch.int32 if desc.key_bits == 32 else torch.int64)
+    if out is None:
+        out = torch.empty(n_batch + 1, dtype=torch.int32, device=keys.device)
+    assert out.dtype == torch.int32 and out.shape == (n_batch + 1,)
+    _check(lib().spc_batch_offsets(_dev_ptr(keys), keys.shape[0], ctypes.byref(desc), n_batch, _dev_ptr(out), _stream(stream)))
     return out
 
 

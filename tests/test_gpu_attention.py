@@ -1,0 +1,413 @@
+"""Linear attention with decays, forward, backward and a row at a time, against its recurrence in 64 bits.
+
+Tolerances.  An output is rounded once to its type (u: half a unit in the last place), and is a sum of products whose magnitudes add up to what the same
+recurrence gives for absolute values, B.  fp32 chains here have some 64 + 128 + 128 links and factors of decays are good to a few 2^-24: 2^-16 of
+B.  16-bit types take sums that pass through the matrix units as two pieces of at least 8 bits each, 2^-16 of B once more on either side."""
+import itertools
+
+import pytest
+import torch
+
+from paper_2511_20834_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+U = {F16: 2.0 ** -11, BF16: 2.0 ** -8, F32: 2.0 ** -24}
+TINY = {F16: 2.0 ** -24, BF16: 2.0 ** -126, F32: 2.0 ** -126}  # spacing of fp16 near zero, smallest normal numbers
+PART = {F16: 2.0 ** -14, BF16: 2.0 ** -14, F32: 2.0 ** -16}
+
+
+def recur(q, k, v, g, at, scale, S0=None):
+    """(out, last states) in 64 bits, a row at a time (differentiable)."""
+    H, G = q.shape[1], q.shape[1] // k.shape[1]
+    k, v = k.repeat_interleave(G, 1), v.repeat_interleave(G, 1)
+    l = torch.exp(g)[:, None, None]
+    out, last = [torch.zeros(0, H, v.shape[2], dtype=torch.float64)], []
+    for b in range(len(at) - 1):
+        S = torch.zeros(H, q.shape[2], v.shape[2], dtype=torch.float64) if S0 is None else S0[b]
+        for t in range(at[b], at[b + 1]):
+            S = torch.where(l > 0, l * S, 0.0) + k[t][:, :, None] * v[t][:, None, :]
+            out.append(scale * (q[t][:, :, None] * S).sum(1)[None])
+        last.append(S)
+    return torch.cat(out), torch.stack(last)
+
+
+def make(lengths, heads, kv, dk, dv, dtype, seed, states, decay=None, layout="columns"):
+    gen = torch.Generator().manual_seed(seed)
+    n = sum(lengths)
+    qkv = torch.randn(n, heads * dk + kv * (dk + dv), generator=gen).to(dtype).cuda()
+    q, k, v = qkv.split([heads * dk, kv * dk, kv * dv], 1)
+    q, k, v = q.unflatten(1, (heads, dk)), k.unflatten(1, (kv, dk)), v.unflatten(1, (kv, dv))
+    if layout == "heads":  # [heads, rows, channels] in memory
+        q, k, v = (t.transpose(0, 1).contiguous().transpose(0, 1) for t in (q, k, v))
+    elif layout == "rows":
+        q, k, v = (t.contiguous() for t in (q, k, v))
+    g = -torch.exp2(-1 - 8 * torch.rand(heads, generator=gen)) if decay is None else torch.full((heads,), decay)
+    at = [0] + list(itertools.accumulate(lengths))
+    S0 = torch.randn(len(lengths), heads, dk, dv, generator=gen).cuda() if states else None
+    return q, k, v, g.cuda(), torch.tensor(at, dtype=torch.int32).cuda(), at, S0
+
+
+def cpu(t):
+    return None if t is None else t.detach().double().cpu()
+
+
+def within(got, ref, mag, dtype, what):
+    got = cpu(got)
+    u, tiny = (U[dtype], TINY[dtype])
+    over = (got - ref).abs() - (u * ref.abs() + tiny + PART[dtype] * mag)
+    assert got.shape == ref.shape and torch.isfinite(got).all(), what
+    assert not over.numel() or over.max() <= 0, (what, float(over.max()), int(over.argmax()))
+
+
+def within32(got, ref, mag, dtype, what):
+    """States: fp32 whatever the rows' type, products exact, pieces of 16 bits and more below 2^-20 of the largest."""
+    got = cpu(got)
+    assert got.shape == ref.shape and torch.isfinite(got).all(), what
+    over = (got - ref).abs() - 2.0 ** -16 * mag - 2.0 ** -126
+    assert over.max() <= 0, (what, float(over.max()))
+
+
+def check_forward(q, k, v, g, offsets, at, S0, dtype, scale=0.3):
+    o, last = B.spc_linear_attention_forward(q, k, v, g, offsets, scale=scale, initial_state=S0, want_state=True)
+    ref, rlast = recur(cpu(q), cpu(k), cpu(v), cpu(g), at, scale, cpu(S0))
+    mag, mlast = recur(cpu(q).abs(), cpu(k).abs(), cpu(v).abs(), cpu(g), at, scale, None if S0 is None else cpu(S0).abs())
+    within(o, ref, mag, dtype, "out")
+    within32(last, rlast, mlast, dtype, "state")
+    return o, last
+
+
+def reference_gradients(do, q, k, v, g, at, scale, S0, dS):
+    """Gradients by differentiating the recurrence."""
+    leaves = [t.detach().clone().requires_grad_() for t in (q, k, v, S0)]
+    o, last = recur(leaves[0], leaves[1], leaves[2], g, at, scale, leaves[3])
+    loss = (o * do).sum() + (last * dS).sum()
+    return torch.autograd.grad(loss, leaves)
+
+
+def check_backward(q, k, v, g, offsets, at, S0, dtype, scale=0.3, seed=9):
+    gen = torch.Generator().manual_seed(seed)
+    n, H, dv = q.shape[0], q.shape[1], v.shape[2]
+    shape = (len(at) - 1, H, q.shape[2], dv)
+    do = torch.randn(n, H, dv, generator=gen).to(dtype).cuda()
+    dS = torch.randn(shape, generator=gen).cuda() if S0 is not None else None
+    got = B.spc_linear_attention_backward(do, q, k, v, g, offsets, scale=scale, initial_state=S0, dstate=dS, want_dinitial=True)
+    zero = torch.zeros(shape, dtype=torch.float64)
+    c0, cS = (zero, zero) if S0 is None else (cpu(S0), cpu(dS))
+    ref = reference_gradients(cpu(do), cpu(q), cpu(k), cpu(v), cpu(g), at, scale, c0, cS)
+    mag = reference_gradients(cpu(do).abs(), cpu(q).abs(), cpu(k).abs(), cpu(v).abs(), cpu(g), at, scale, c0.abs(), cS.abs())
+    for a, b, m, what in zip(got[:3], ref, mag, ("dq", "dk", "dv")):
+        within(a, b, m, dtype, what)
+    within32(got[3], ref[3], mag[3], dtype, "dinitial")
+    return got
+
+
+LENGTHS = [[1], [0, 1, 0], [2, 63, 64, 65], [31], [129, 0, 1, 300], [700]]
+HEADS = [(1, 1, 64, 64), (4, 4, 16, 16), (2, 2, 32, 32), (4, 2, 24, 40), (6, 1, 64, 32), (2, 1, 5, 7), (1, 1, 128, 128), (2, 2, 1, 1), (3, 3, 33, 128), (2, 2, 128, 17)]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+@pytest.mark.parametrize("heads,kv,dk,dv", HEADS)
+def test_forward(lengths, heads, kv, dk, dv, dtype):
+    states = len(lengths) != 1 or lengths[0] == 31
+    check_forward(*make(lengths, heads, kv, dk, dv, dtype, 7 * dk + dv, states), dtype)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+@pytest.mark.parametrize("heads,kv,dk,dv", HEADS)
+def test_backward(lengths, heads, kv, dk, dv, dtype):
+    states = len(lengths) != 1 or lengths[0] == 31
+    check_backward(*make(lengths, heads, kv, dk, dv, dtype, 7 * dk + dv + 1, states), dtype)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("layout", ["heads", "rows"])
+def test_layouts(layout, dtype):
+    """Heads outermost, and rows whose pitch is their width: the results are those of the column ranges, bit for bit."""
+    a = make([200, 77], 4, 2, 32, 48, dtype, 3, True)
+    b = make([200, 77], 4, 2, 32, 48, dtype, 3, True, layout=layout)
+    fa, fb = (B.spc_linear_attention_forward(*t[:5], initial_state=t[6], want_state=True) for t in (a, b))
+    assert all(torch.equal(p, q) for p, q in zip(fa, fb))
+    do = torch.randn(277, 4, 48, device="cuda").to(dtype)
+    far = torch.zeros(277, 4, 99, device="cuda", dtype=dtype)
+    far[:, :, 3:51] = do
+    ba = B.spc_linear_attention_backward(do, *a[:5], initial_state=a[6])
+    out = tuple(torch.full((277, h, w + 1), 3.0, dtype=dtype, device="cuda")[:, :, 1:] for h, w in ((4, 32), (2, 32), (2, 48)))
+    bb = B.spc_linear_attention_backward(far[:, :, 3:51], *b[:5], initial_state=b[6], out=out)
+    assert all(torch.equal(p, q) for p, q in zip(ba[:3], bb[:3]))
+    assert all((t._base[:, :, 0] == 3).all() for t in out)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("decay", [0.0, -1e-4, -3.0, -200.0, float("-inf")])
+def test_decays(decay, dtype):
+    a = make([150, 3], 2, 2, 32, 32, dtype, 5, True, decay=decay)
+    check_forward(*a, dtype)
+    q, k, v, g, offsets, at, S0 = a
+    if decay > -1e9:
+        check_backward(*a, dtype)
+    else:  # every row by itself
+        do = torch.randn(153, 2, 32, device="cuda").to(dtype)
+        dS = torch.randn(S0.shape, device="cuda")
+        dq, dk, dv, d0 = B.spc_linear_attention_backward(do, q, k, v, g, offsets, scale=0.3, initial_state=S0, dstate=dS, want_dinitial=True)
+        within(dq, 0.3 * (cpu(do) * cpu(v)).sum(2, keepdim=True) * cpu(k), (cpu(do) * cpu(v)).abs().sum(2, keepdim=True) * cpu(k).abs(), dtype, "dq")
+        assert (d0 == 0).all()
+
+
+def test_several_chunks_a_segment():
+    """Enough rows and heads for segments of more than 64 rows."""
+    for heads, dtype in ((16, BF16), (12, F16)):
+        a = make([9000, 1, 2501], heads, heads, 16, 16, dtype, 11, True)
+        check_forward(*a, dtype)
+    check_backward(*make([5000, 900], 16, 4, 16, 16, BF16, 12, True), BF16)
+
+
+def test_scales_of_features():
+    """Rows of tiny and of large features, and one channel far above the others: fp16's range is not that of sums and states."""
+    for dtype in (F16, BF16):
+        for kq, kv in ((1e-3, 1e-3), (30.0, 1e-2), (1e-2, 100.0)):
+            q, k, v, g, offsets, at, _ = make([260], 2, 2, 32, 32, dtype, 21, False, decay=-0.01)
+            q, k, v = (q.float() * kq).to(dtype), (k.float() * kq).to(dtype), (v.float() * kv).to(dtype)
+            check_forward(q, k, v, g, offsets, at, None, dtype, scale=1.0)
+        # values of one sign without a decay: states beyond fp16's largest number, outputs brought back by the scale
+        q, k, v, g, offsets, at, _ = make([500], 1, 1, 16, 16, dtype, 22, False, decay=0.0)
+        q, k, v = q.abs(), (q.abs() * 16).to(dtype), (v.abs() * 16).to(dtype)
+        check_forward(q, k, v, g, offsets, at, None, dtype, scale=2.0 ** -12)
+
+
+def test_gradients_against_differences():
+    q, k, v, g, offsets, at, S0 = make([70, 20], 4, 2, 8, 12, F32, 31, True)
+    gen = torch.Generator().manual_seed(1)
+    do, dS = torch.randn(90, 4, 12, generator=gen).cuda(), torch.randn(2, 4, 8, 12, generator=gen).cuda()
+    grads = B.spc_linear_attention_backward(do, q, k, v, g, offsets, scale=0.5, initial_state=S0, dstate=dS, want_dinitial=True)
+    at64 = [cpu(t) for t in (q, k, v, S0)]
+
+    def loss(x):
+        o, last = recur(x[0], x[1], x[2], cpu(g), at, 0.5, x[3])
+        return float((o * cpu(do)).sum() + (last * cpu(dS)).sum())
+
+    for i, grad in enumerate(grads):
+        d = torch.randn(at64[i].shape, generator=gen, dtype=torch.float64)
+        hi, lo = list(at64), list(at64)
+        hi[i], lo[i] = at64[i] + 1e-3 * d, at64[i] - 1e-3 * d
+        num, ana = (loss(hi) - loss(lo)) / 2e-3, float((cpu(grad) * d).sum())  # (the loss is linear in each of the four)
+        assert abs(num - ana) <= 2.0 ** -16 * float((cpu(grad) * d).abs().sum()) + 1e-9 * abs(loss(at64)), i
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("value", [float("inf"), float("nan"), float("-inf")])
+def test_rows_that_are_not_finite_do_not_reach_earlier_ones(dtype, value):
+    lengths, where = [200, 150], 137  # (in the middle of a chunk of the first scene)
+    q, k, v, g, offsets, at, _ = make(lengths, 4, 2, 32, 32, dtype, 41, False, layout="rows")
+    do = torch.randn(350, 4, 32, device="cuda").to(dtype)
+    o, last = B.spc_linear_attention_forward(q, k, v, g, offsets, want_state=True)
+    grads = B.spc_linear_attention_backward(do, q, k, v, g, offsets)
+    others = torch.cat([torch.arange(where), torch.arange(200, 350)]).cuda()
+    for t in (q, k, v):
+        keep = t.clone()
+        t[where, 0, 5] = value
+        o2, last2 = B.spc_linear_attention_forward(q, k, v, g, offsets, want_state=True)
+        assert torch.isfinite(o2[others]).all()
+        assert (o2[others].double() - o[others].double()).abs().max() <= 2 * U[dtype] * o[others].abs().max(), "earlier rows, other scenes"
+        assert torch.equal(o2[:, 2:], o[:, 2:]) and torch.equal(last2[:, 2:], last[:, 2:]), "other heads"
+        assert not torch.isfinite(o2[where, 0]).any() if t is not v else not torch.isfinite(o2[where, 0, 5])
+        assert torch.equal(last2[1], last[1])
+        t.copy_(keep)
+    # backward: a gradient that is not finite reaches keys and values of rows up to its own only
+    do[where, 0, 3] = value
+    dq, dk, dv, _ = B.spc_linear_attention_backward(do, q, k, v, g, offsets)
+    later = torch.arange(where + 1, 350).cuda()
+    for a, b in zip((dk, dv), grads[1:3]):
+        assert torch.isfinite(a[later]).all() and (a[later].double() - b[later].double()).abs().max() <= 2 * U[dtype] * b[later].abs().max()
+    assert torch.isfinite(dq[others]).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("streams,heads,kv,dk,dv", [(1, 8, 8, 64, 64), (3, 4, 2, 24, 40), (17, 6, 1, 5, 7), (2, 2, 2, 128, 128), (5, 1, 1, 1, 1), (70, 2, 2, 33, 128), (9, 4, 4, 16, 16),
+                                                    (4, 2, 2, 96, 32), (2, 3, 3, 128, 17)])
+def test_step(streams, heads, kv, dk, dv, dtype):
+    q, k, v, g, _, _, _ = make([streams], heads, kv, dk, dv, dtype, 51, False)
+    S = torch.randn(streams, heads, dk, dv, device="cuda")
+    before = cpu(S)
+    at = list(range(streams + 1))
+    o = B.spc_linear_attention_step(q, k, v, g, S, scale=0.3)
+    ref, last = recur(cpu(q), cpu(k), cpu(v), cpu(g), at, 0.3, before)
+    mag, mlast = recur(cpu(q).abs(), cpu(k).abs(), cpu(v).abs(), cpu(g), at, 0.3, before.abs())
+    within(o, ref, mag, dtype, "out")
+    within32(S, last, mlast, dtype, "state")
+
+
+def test_steps_carry_a_scene_on():
+    q, k, v, g, _, _, _ = make([300], 2, 2, 32, 32, F32, 61, False)
+    whole, last = B.spc_linear_attention_forward(q, k, v, g, want_state=True)
+    head, S = B.spc_linear_attention_forward(q[:290], k[:290], v[:290], g, want_state=True)
+    rest = torch.cat([B.spc_linear_attention_step(q[t:t + 1], k[t:t + 1], v[t:t + 1], g, S) for t in range(290, 300)])
+    assert torch.allclose(torch.cat([head, rest]), whole, rtol=1e-4, atol=1e-4) and torch.allclose(S, last, rtol=1e-4, atol=1e-4)
+
+
+def test_rows_in_no_scene_are_left_alone():
+    q, k, v, g, _, _, _ = make([300], 2, 1, 16, 32, F16, 71, False)
+    offsets = torch.tensor([20, 120, 250], dtype=torch.int32, device="cuda")
+    clean = B.spc_linear_attention_forward(q[20:250], k[20:250], v[20:250], g, offsets - 20)[0]
+    do = torch.randn(300, 2, 32, device="cuda").half()
+    cg = B.spc_linear_attention_backward(do[20:250], q[20:250], k[20:250], v[20:250], g, offsets - 20)
+    for t in (q, k, v, do):
+        t[:20], t[250:] = float("nan"), float("nan")
+    out = torch.full((300, 2, 32), 5.0, dtype=F16, device="cuda")
+    B.spc_linear_attention_forward(q, k, v, g, offsets, out=out)
+    assert (out[:20] == 5).all() and (out[250:] == 5).all()
+    tol = 4 * U[F16] * clean.abs().max()  # (segments lie elsewhere, sums are associated otherwise)
+    assert (out[20:250] - clean).abs().max() <= tol
+    outs = tuple(torch.full(s, 5.0, dtype=F16, device="cuda") for s in ((300, 2, 16), (300, 1, 16), (300, 1, 32)))
+    B.spc_linear_attention_backward(do, q, k, v, g, offsets, out=outs)
+    assert (outs[0][:20] == 5).all() and (outs[0][250:] == 5).all()
+    for a, b in zip(outs, cg):
+        assert torch.isfinite(a[20:250]).all() and (a[20:250] - b).abs().max() <= 4 * U[F16] * b.abs().max()
+
+
+@pytest.mark.parametrize("offsets", [[0, 1000, 300], [-5, 100, 300], [0, 200, 100, 300], [2 ** 31 - 1, -2 ** 31, 7], [300, 300, 300], [400, 500, 600]])
+def test_offsets_that_are_none_stay_inside_the_rows(offsets):
+    """Whatever offsets hold, nothing outside the tensors is touched: rows around them keep what they held, the states are written or left."""
+    guard = torch.full((900, 2, 32), 5.0, dtype=F16, device="cuda")
+    q, k, v, g, _, _, _ = make([300], 2, 2, 32, 32, F16, 81, False)
+    at = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    B.spc_linear_attention_forward(q, k, v, g, at, out=guard[300:600], want_state=True)
+    outs = tuple(torch.full((900, 2, 32), 5.0, dtype=F16, device="cuda") for _ in range(3))
+    B.spc_linear_attention_backward(v, q, k, v, g, at, out=tuple(t[300:600] for t in outs), want_dinitial=True)
+    for t in (guard, *outs):
+        assert (t[:300] == 5).all() and (t[600:] == 5).all()
+
+
+def test_no_rows_and_empty_scenes():
+    q, k, v, g, _, _, _ = make([0], 2, 2, 16, 16, F32, 91, False)
+    S0, dS = torch.randn(3, 2, 16, 16, device="cuda"), torch.randn(3, 2, 16, 16, device="cuda")
+    none = torch.zeros(4, dtype=torch.int32, device="cuda")
+    o, last = B.spc_linear_attention_forward(q, k, v, g, none, initial_state=S0, want_state=True)
+    assert o.shape == (0, 2, 16) and torch.equal(last, S0)
+    assert (B.spc_linear_attention_forward(q, k, v, g, none, want_state=True)[1] == 0).all()
+    dq, dk, dv, d0 = B.spc_linear_attention_backward(o, q, k, v, g, none, initial_state=S0, dstate=dS, want_dinitial=True)
+    assert torch.equal(d0, dS) and dq.numel() == dk.numel() == dv.numel() == 0
+    assert B.spc_linear_attention_step(q, k, v, g, S0[:0]).shape == (0, 2, 16)
+
+
+def test_same_bits_every_time_and_on_another_stream():
+    q, k, v, g, offsets, _, S0 = make([5000, 800], 8, 2, 32, 32, BF16, 101, True)
+    do = torch.randn(5800, 8, 32, device="cuda").to(BF16)
+
+    def step():
+        return *B.spc_linear_attention_forward(q, k, v, g, offsets, initial_state=S0, want_state=True), \
+            *B.spc_linear_attention_backward(do, q, k, v, g, offsets, initial_state=S0, want_dinitial=True)
+
+    first = step()
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(other):
+            again = step()
+        other.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+def test_recorded():
+    q, k, v, g, offsets, _, _ = make([900, 300], 4, 2, 32, 32, F16, 111, False, layout="rows")
+    do = torch.randn(1200, 4, 32, device="cuda").half()
+
+    def step():
+        return B.spc_linear_attention_forward(q, k, v, g, offsets)[0], *B.spc_linear_attention_backward(do, q, k, v, g, offsets)[:3]
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        out = step()
+    for r in range(3):
+        q.normal_()
+        offsets.copy_(torch.tensor([0, 500 + 100 * r, 1200], dtype=torch.int32))  # (scenes of other lengths, the same record)
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_rows_far_apart():
+    """Row offsets beyond 32 bits, in and out."""
+    n, pitch = 300, 16_000_000
+    wide = torch.empty(n * pitch, dtype=BF16, device="cuda")
+    q, k, v = (wide.as_strided((n, 2, 32), (pitch, 32, 1), 64 * i) for i in range(3))
+    for t in (q, k, v):
+        t.copy_(torch.randn(n, 2, 32))
+    g = torch.tensor([-0.1, -0.01], device="cuda")
+    near = [t.contiguous() for t in (q, k, v)]
+    far = wide.as_strided((n, 2, 32), (pitch, 32, 1), 64 * 3)
+    B.spc_linear_attention_forward(q, k, v, g, out=far)
+    want = B.spc_linear_attention_forward(*near, g)[0]
+    assert torch.equal(far, want)
+    a, b = B.spc_linear_attention_backward(far, q, k, v, g), B.spc_linear_attention_backward(want, *near, g)
+    assert all(torch.equal(x, y) for x, y in zip(a[:3], b[:3]))
+
+
+def test_broadcast_inputs():
+    q, k, v, g, offsets, at, _ = make([130], 4, 4, 16, 16, BF16, 121, False, layout="rows")
+    one = k[:, :1].expand(130, 4, 16)  # (a pitch of zero between heads)
+    same = one.contiguous()
+    assert torch.equal(B.spc_linear_attention_forward(q, one, v, g, offsets)[0], B.spc_linear_attention_forward(q, same, v, g, offsets)[0])
+    a, b = (B.spc_linear_attention_backward(v, q, t, v, g, offsets) for t in (one, same))
+    assert all(torch.equal(x, y) for x, y in zip(a[:3], b[:3]))
+
+
+@pytest.mark.parametrize("key_bits", [32, 64])
+def test_batch_offsets(key_bits):
+    gen = torch.Generator().manual_seed(2)
+    counts = [300, 0, 1, 5000, 0, 77]
+    rows = torch.cat([torch.cat([torch.full((c, 1), b), torch.randint(0, 60, (c, 3), generator=gen)], 1) for b, c in enumerate(counts)]).to(torch.int32)
+    rows = rows[torch.randperm(len(rows), generator=gen)].cuda()
+    desc = B.spc_pack_desc_fit([0, 0, 0], [59, 59, 59], 6, 1, 1, key_bits)
+    keys, _ = B.spc_pack_coords(rows, desc)
+    assert B.spc_batch_offsets(keys, desc, 6).tolist() == [0] + list(itertools.accumulate(counts))
+    assert B.spc_batch_offsets(keys, desc, 2).tolist() == [0, 300, 300]
+    one = B.spc_pack_desc_fit([0, 0, 0], [59, 59, 59], 1, 1, 1, key_bits)
+    keys, _ = B.spc_pack_coords(rows * torch.tensor([0, 1, 1, 1], dtype=torch.int32, device="cuda"), one)
+    assert B.spc_batch_offsets(keys, one, 1).tolist() == [0, sum(counts)]
+    assert B.spc_batch_offsets(keys[:0], one, 1).tolist() == [0, 0]
+
+
+def test_refusals():
+    q, k, v, g, offsets, _, S0 = make([40], 4, 2, 16, 16, F16, 131, True)
+
+    def refused(code, **change):
+        a = dict(q=q, k=k, v=v, log_decay=g, offsets=offsets)
+        a.update(change)
+        with pytest.raises(B.SpcError) as e:
+            B.spc_linear_attention_forward(**a)
+        assert e.value.code == code
+
+    refused(B.ERR_UNSUPPORTED, q=torch.zeros(40, 4, 129, device="cuda").half(), k=torch.zeros(40, 2, 129, device="cuda").half())
+    refused(B.ERR_UNSUPPORTED, v=torch.zeros(40, 2, 129, device="cuda").half())
+    refused(B.ERR_ARG, k=torch.zeros(40, 3, 16, device="cuda").half(), v=torch.zeros(40, 3, 16, device="cuda").half())  # 4 heads over 3
+    refused(B.ERR_ARG, scale=float("nan"))
+    refused(B.ERR_ARG, out=torch.zeros(40, 1, 16, device="cuda").half().expand(40, 4, 16))  # heads on top of each other
+    refused(B.ERR_ARG, out=torch.zeros(1, 4, 16, device="cuda").half().expand(40, 4, 16))
+    for change in (dict(q=q.float()), dict(k=k[:39]), dict(log_decay=g[:3]), dict(log_decay=g.double()), dict(offsets=offsets.long()),
+                   dict(initial_state=S0[:, :3]), dict(initial_state=S0.half()), dict(q=q.transpose(1, 2).contiguous().transpose(1, 2))):
+        a = dict(q=q, k=k, v=v, log_decay=g, offsets=offsets)
+        a.update(change)
+        with pytest.raises(AssertionError):
+            B.spc_linear_attention_forward(**a)
+    L, p, s = B.lib(), q.data_ptr(), S0.data_ptr()
+    d, r = B.AttnDesc(0, 1, 40, 4, 2, 16, 16, 0.25), B.AttnRows(p, 128, 16)
+    call = lambda d=d, q=r, k=r, v=r, g=g.data_ptr(), at=None, o=r: L.spc_linear_attention_forward(d, q, k, v, g, at, None, o, None, None)
+    assert call(g=None) == B.ERR_ARG and call(d=None) == B.ERR_ARG and call(q=None) == B.ERR_ARG and call(o=B.AttnRows(None, 128, 16)) == B.ERR_ARG
+    assert call(q=B.AttnRows(p + 1, 128, 16)) == B.ERR_ARG and call(k=B.AttnRows(p, -1, 16)) == B.ERR_ARG
+    for bad in ((3, 1, 40, 4, 2, 16, 16), (0, 0, 40, 4, 2, 16, 16), (0, 2, 40, 4, 2, 16, 16), (0, 1, -1, 4, 2, 16, 16), (0, 1, 40, 0, 1, 16, 16), (0, 1, 40, 4, 0, 16, 16),
+                (0, 1, 40, 4, 2, 0, 16)):
+        assert call(d=B.AttnDesc(*bad, 0.25)) == B.ERR_ARG, bad
+    assert call(d=B.AttnDesc(0, 1, 1 << 31, 4, 2, 16, 16, 0.25)) == B.ERR_UNSUPPORTED
+    assert L.spc_linear_attention_step(d, r, r, r, g.data_ptr(), None, r, None) == B.ERR_ARG
+    assert L.spc_linear_attention_backward(d, r, r, r, r, g.data_ptr(), None, None, None, r, r, None, None, None) == B.ERR_ARG
+    assert L.spc_batch_offsets(s, 5, None, 1, s, None) == B.ERR_ARG
