@@ -10,6 +10,7 @@
 // A scene is cut into segments that different workgroups scan at once: a first launch makes every segment's own sum of y z^T, a second
 // turns them into the state in front of every segment, a third scans the segments.  Scenes of one segment take the third alone.
 #include <algorithm>
+#include <type_traits>
 
 #include "spc_internal.h"
 
@@ -37,6 +38,7 @@ struct Job {
   States first, last, between;  // of a scene, after it, after every segment but the last
   int dy, dz;
   bool reverse, out_f32;
+  bool vec_x, vec_y, vec_z, vec_out;  // whether rows can be read in pieces of 16 bytes, written in pieces of four channels
 };
 struct ScanArgs {
   Job job[ATTN_MAX_JOBS];
@@ -72,48 +74,371 @@ struct Segment {
 
 __device__ inline float decay_power(float log_decay, int n) { return n > 0 ? expf(log_decay * n) : 1.f; }
 
-// One token after the other, the state in LDS.
-template <typename T, bool OUT>
-__global__ __launch_bounds__(256) void scan_rows_kernel(const ScanArgs a) {
-  extern __shared__ float lds[];
-  const Job& j = a.job[blockIdx.x % a.n_jobs];
-  const int h = blockIdx.x / a.n_jobs % a.heads, id = blockIdx.x / a.n_jobs / a.heads;
+// Up to four consecutive channels (`left` of them exist).
+template <typename T>
+__device__ inline void store4(T* p, float __attribute__((ext_vector_type(4))) v, bool pieces, int left) {
+  struct alignas(4 * sizeof(T)) Piece { T v[4]; };
+  if (left >= 4 && pieces) {
+    *reinterpret_cast<Piece*>(p) = Piece{{static_cast<T>(v[0]), static_cast<T>(v[1]), static_cast<T>(v[2]), static_cast<T>(v[3])}};
+    return;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (r < left) p[r] = static_cast<T>(v[r]);
+}
+
+// ---------------------------------------------------------------- chunks on the matrix cores
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
+
+constexpr int CHUNK = 64;  // rows whose products with each other are taken directly
+
+// A fragment holds 32 places of a contraction for 16 rows (A) or columns (B): lane l has row l%16 and the places 16 h + 4 (l/16) + r, h < 2, r < 4,
+// as element 4 h + r.  The results of two 16 x 16 products, whose lane l holds column l%16 and rows 4 (l/16) + r, are one as they come: sums of
+// products go from one product into the next without passing through LDS.
+template <typename T>
+struct Ops {
+  using V = std::conditional_t<std::is_same_v<T, _Float16>, half8, bf16x8>;
+  static constexpr int PAD = 8;
+  __device__ static inline floatx4 mma(V a, V b, floatx4 c) {
+    if constexpr (std::is_same_v<T, _Float16>) return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  // places along a row of the tile: p points to (row l%16, place 4 (l/16))
+  __device__ static inline V along(const T* p) {
+    struct alignas(8) Half { T v[4]; };
+    const Half a = *reinterpret_cast<const Half*>(p), b = *reinterpret_cast<const Half*>(p + 16);
+    V f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) f[r] = a.v[r], f[4 + r] = b.v[r];
+    return f;
+  }
+  // places down a column: tile row j0 + place, column c0 + l%16.  (Sixteen lanes read four rows of sixteen, and each receives a column of them.)
+  __device__ static inline V down(const T* tile, int pitch, int j0, int c0, int lane) {
+    const T* p = tile + (j0 + 4 * (lane / 16) + lane % 16 / 4) * pitch + c0 + lane % 4 * 4;
+    using P = __attribute__((address_space(3))) shortx4*;
+    const shortx4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p)), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 16 * pitch));
+    return __builtin_bit_cast(V, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+template <>
+struct Ops<float> {
+  using V = floatx8;
+  static constexpr int PAD = 4;
+  __device__ static inline floatx4 mma(V a, V b, floatx4 c) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[k], b[k], c, 0, 0, 0);
+    return c;
+  }
+  __device__ static inline V along(const float* p) {
+    const floatx4 a = *reinterpret_cast<const floatx4*>(p), b = *reinterpret_cast<const floatx4*>(p + 16);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  __device__ static inline V down(const float* tile, int pitch, int j0, int c0, int lane) {
+    const float* p = tile + (j0 + 4 * (lane / 16)) * pitch + c0 + lane % 16;
+    V f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = p[(16 * (k / 4) + k % 4) * pitch];
+    return f;
+  }
+};
+// x as a sum of N fragments: each holds what the ones before have left of it, times 2^(SHIFT * its number).
+template <typename T, int N, int SHIFT = 0>
+__device__ inline void split(floatx8 x, typename Ops<T>::V (&out)[N]) {
+  if constexpr (N == 1) {
+    out[0] = x;
+  } else {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) out[n][k] = static_cast<T>(x[k]);
+      if (n + 1 == N) break;
+      // (what is left is left by the value that the product takes: without this the compiler rounds it twice, once of an unrounded
+      // product by a conversion that multiplies, and the two differ now and then)
+      intx4 q = __builtin_bit_cast(intx4, out[n]);
+      asm("" : "+v"(q));
+      out[n] = __builtin_bit_cast(typename Ops<T>::V, q);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = (x[k] - static_cast<float>(out[n][k])) * (SHIFT ? float(1 << SHIFT) : 1.f);
+    }
+  }
+}
+__device__ inline float over_quads(float v) {  // maximum over the four lanes of a column (a row of A)
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+
+template <typename T, int D, int THREADS>
+struct TileLoad {
+  static constexpr int VE = 16 / sizeof(T), PER_ROW = D / VE, N = CHUNK * PER_ROW / THREADS, PITCH = D + Ops<T>::PAD;
+  struct alignas(16) Piece { T v[VE]; };
+  Piece q[N];
+  // Rows [first, first + CHUNK) of the scan (those from s.rows on, and channels from `width` on, are zeros)
+  __device__ void load(const Rows& t, bool pieces, int width, const Segment& s, bool reverse, int seg_first, int first, int h) {
+    const T* base = static_cast<const T*>(t.p) + (h / t.group) * t.head;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = (threadIdx.x + n * THREADS) / PER_ROW, c = (threadIdx.x + n * THREADS) % PER_ROW * VE;
+      q[n] = Piece{};
+      if (first + i >= s.rows || c >= width) continue;
+      const T* p = base + s.row(reverse, seg_first + first + i) * t.row + c;
+      if (pieces) q[n] = *reinterpret_cast<const Piece*>(p);
+      else
+#pragma unroll
+        for (int k = 0; k < VE; ++k)
+          if (c + k < width) q[n].v[k] = p[k];
+    }
+  }
+  __device__ void store(T* tile) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = (threadIdx.x + n * THREADS) / PER_ROW, c = (threadIdx.x + n * THREADS) % PER_ROW * VE;
+      *reinterpret_cast<Piece*>(tile + i * PITCH + c) = q[n];
+    }
+  }
+};
+
+// One segment of one head: chunk by chunk, with the state in registers.  NW waves share the chunk's tiles; each owns D / NW columns of z, of
+// the output and of the state, and computes the chunk's products P^T = Y X^T for itself, since they are the next product's operand as they lie.
+//   O^T = Z^T P^T + S^T X^T,   S <- l^n S + Y^T (w o Z)
+// Operands that are no inputs (P, S, w o Z) go into 16-bit products as two pieces, the weighted values of bf16 as three: 16 bits of every sum that is
+// rounded to a 16-bit output in the end, 24 (fp16: 22) of what the state adds up.  fp16's pieces are scaled by powers of two, P by the largest in a row, S by
+// the largest in a column, since sums may leave its range.  fp32 takes fp32 products.
+template <typename T, int D, int NW, bool OUT>
+__global__ __launch_bounds__(64 * NW) void scan_chunks_kernel(const ScanArgs a) {
+  using O = Ops<T>;
+  using V = typename O::V;
+  constexpr bool HALF = std::is_same_v<T, _Float16>, SINGLE = std::is_same_v<T, float>;
+  constexpr int NP = SINGLE ? 1 : 2, NU = SINGLE ? 1 : HALF ? 2 : 3;  // pieces of P and S, of the weighted values
+  constexpr int CT = D / NW / 16, DT = D / 16, KT = D / 32, IT = CHUNK / 16, JT = CHUNK / 32, PITCH = D + O::PAD;
+  extern __shared__ __align__(16) char lds[];
+  T *ys = reinterpret_cast<T*>(lds), *zs = ys + CHUNK * PITCH, *xs = zs + CHUNK * PITCH;
+
+  // workgroups that follow each other go to the eight XCDs in turn: neighbours of one segment share an L2 this way
+  const int total = a.n_ids * a.heads * a.n_jobs, share = (total + 7) / 8, work = blockIdx.x % 8 * share + blockIdx.x / 8;
+  if (work >= total) return;
+  const Job& j = a.job[work % a.n_jobs];
+  const int h = work / a.n_jobs % a.heads, id = work / a.n_jobs / a.heads;
   Segment s;
   if (!s.find(a, id)) return;
   if (!OUT && s.m == s.n - 1) return;  // nobody starts from it
-  const int e = j.dy * j.dz, t = threadIdx.x;
-  float *S = lds, *x = S + e, *y = x + ATTN_MAX_D, *z = y + ATTN_MAX_D;
-  const float l = expf(a.log_decay[h]), upd = j.reverse ? a.scale : 1.f, of = j.reverse ? 1.f : a.scale;
-  for (int i = t; i < e; i += 256) {
-    float v = 0.f;
-    if (OUT && s.m) v = j.between.of(id - 1, a.heads, h)[(i / j.dz) * j.between.r + (i % j.dz) * j.between.c];
-    else if (OUT && j.first.p) v = j.first.of(s.scene, a.heads, h)[(i / j.dz) * j.first.r + (i % j.dz) * j.first.c];
-    S[i] = v;
+  const int lane = threadIdx.x % 64, lc = lane % 16, lr = lane / 16 * 4, c0 = threadIdx.x / 64 * (16 * CT), seg_first = s.m * a.seg_rows;
+  const bool special = j.reverse && !s.m;  // the gradient of the last state meets the last row undecayed
+  const float g = a.log_decay[h];
+  const float p_scale = a.scale, upd = j.reverse ? a.scale : 1.f, inter = j.reverse ? 1.f : a.scale;
+
+  floatx4 S[CT][DT];
+  const bool from = OUT && (s.m || j.first.p);
+  {
+    const States& st = s.m ? j.between : j.first;
+    const float* p = from ? st.of(s.m ? id - 1 : s.scene, a.heads, h) : nullptr;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = 16 * dt + lr + r, col = c0 + 16 * ct + lc;
+          S[ct][dt][r] = from && row < j.dy && col < j.dz ? p[row * st.r + col * st.c] : 0.f;
+        }
   }
-  for (int i = 0; i < s.rows; ++i) {
-    const int64_t row = s.row(j.reverse, s.m * a.seg_rows + i);
+  float W[IT][4], tile_decay[IT], U[JT][8];
+#pragma unroll
+  for (int t = 0; t < IT; ++t) {
+    tile_decay[t] = decay_power(g, 16 * t);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) W[t][r] = p_scale * decay_power(g, 16 * t + lc - lr - r);  // (negative: above the diagonal, not used)
+  }
+  int n_u = -1;
+
+  TileLoad<T, D, 64 * NW> x, y, z;
+  auto fetch = [&](int first) {
+    if (OUT) x.load(j.x, j.vec_x, j.dy, s, j.reverse, seg_first, first, h);
+    y.load(j.y, j.vec_y, j.dy, s, j.reverse, seg_first, first, h);
+    z.load(j.z, j.vec_z, j.dz, s, j.reverse, seg_first, first, h);
+  };
+  fetch(0);
+#pragma unroll 1
+  for (int first = 0; first < s.rows; first += CHUNK) {
+    const int n = min(CHUNK, s.rows - first), e0 = special && !first ? 0 : 1;
     __syncthreads();
-    if (OUT && t < j.dy) x[t] = static_cast<float>(static_cast<const T*>(j.x.p)[j.x.at(row, h) + t]);
-    if (t < j.dy) y[t] = upd * static_cast<float>(static_cast<const T*>(j.y.p)[j.y.at(row, h) + t]);
-    if (t < j.dz) z[t] = static_cast<float>(static_cast<const T*>(j.z.p)[j.z.at(row, h) + t]);
+    if (OUT) x.store(xs);
+    y.store(ys);
+    z.store(zs);
     __syncthreads();
-    const float f = j.reverse && !s.m && !i ? 1.f : l;  // (the gradient of the last state meets the last token undecayed)
-    for (int k = t; k < e; k += 256) S[k] = f * S[k] + y[k / j.dz] * z[k % j.dz];
-    __syncthreads();
-    if (OUT && t < j.dz) {
-      float o = 0.f;
-      for (int r = 0; r < j.dy; ++r) o = fmaf(x[r], S[r * j.dz + t], o);
-      const int64_t at = j.out.at(row, h) + t;
-      if (j.out_f32) static_cast<float*>(j.out.p)[at] = of * o;
-      else static_cast<T*>(j.out.p)[at] = static_cast<T>(of * o);
+    if (first + CHUNK < s.rows) fetch(first + CHUNK);
+    if (n != n_u) {  // (all chunks but a segment's last are full)
+      n_u = n;
+#pragma unroll
+      for (int t = 0; t < JT; ++t)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) U[t][k] = (HALF ? 1.f : upd) * decay_power(g, n - 1 - (32 * t + 16 * (k / 4) + lr + k % 4));
+    }
+    V zf[CT][JT];
+    float odd = 0.f;  // NaN if a value is not finite
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int t = 0; t < JT; ++t) {
+        zf[ct][t] = O::down(zs, PITCH, 32 * t, c0 + 16 * ct, lane);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) odd = fmaf(static_cast<float>(zf[ct][t][k]), 0.f, odd);
+      }
+    if constexpr (OUT) {
+      // Zero times infinity is NaN: where a value is not finite, the zeros of P above the diagonal would bring it to earlier rows.
+      const bool by_rows = __ballot(odd != odd) != 0;
+      V sf[CT][KT][NP];
+      floatx4 s_scale[CT];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        int e = 0;
+        if constexpr (HALF) {
+          float m = 0.f;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(S[ct][dt][r]));
+          e = __builtin_amdgcn_frexp_expf(over_quads(m));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s_scale[ct][r] = ldexpf(1.f, __shfl(e, lr + r, 64));
+        }
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+          floatx8 v = __builtin_shufflevector(S[ct][2 * k], S[ct][2 * k + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+          if constexpr (HALF) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = ldexpf(v[q], -e);
+          }
+          split<T, NP>(v, sf[ct][k]);
+        }
+      }
+      const float f0 = inter * decay_power(g, lc + e0);
+#pragma unroll
+      for (int it = 0; it < IT; ++it) {
+        if (16 * it >= n) break;
+        V xf[KT];
+#pragma unroll
+        for (int k = 0; k < KT; ++k) xf[k] = O::along(xs + (16 * it + lc) * PITCH + 32 * k + lr);
+        floatx8 P[JT];
+        float m = 0.f;
+#pragma unroll
+        for (int jt = 0; jt < IT; ++jt) {
+          floatx4 p = {0.f, 0.f, 0.f, 0.f};
+          if (jt <= it) {
+#pragma unroll
+            for (int k = 0; k < KT; ++k) p = O::mma(O::along(ys + (16 * jt + lc) * PITCH + 32 * k + lr), xf[k], p);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              p[r] *= W[it - jt][r];
+              if (jt == it && lr + r > lc) p[r] = 0.f;
+              if constexpr (HALF) m = fmaxf(m, fabsf(p[r]));
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) P[jt / 2][jt % 2 * 4 + r] = p[r];
+        }
+        float p_up = 1.f;
+        if constexpr (HALF) {
+          const int e = __builtin_amdgcn_frexp_expf(over_quads(m));
+          p_up = ldexpf(1.f, e);
+#pragma unroll
+          for (int t = 0; t < JT; ++t)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) P[t][k] = ldexpf(P[t][k], -e);
+        }
+        V pf[JT][NP];
+#pragma unroll
+        for (int t = 0; t < JT; ++t)
+          if (2 * t <= it) split<T, NP>(P[t], pf[t]);
+        const float f = f0 * tile_decay[it];
+        const int i = 16 * it + lc;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int q = 0; q < NP; ++q) o = O::mma(sf[ct][k][q], xf[k], o);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[r] *= HALF ? f * s_scale[ct][r] : f;
+          if (by_rows) {
+            const int c = c0 + 16 * ct + lr;
+#pragma unroll 1
+            for (int q = 0; q <= i; ++q) {
+              float w = 0.f;
+#pragma unroll 1
+              for (int d = 0; d < j.dy; ++d) w = fmaf(static_cast<float>(xs[i * PITCH + d]), static_cast<float>(ys[q * PITCH + d]), w);
+              w *= p_scale * decay_power(g, i - q);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) o[r] = fmaf(w, static_cast<float>(zs[q * PITCH + c + r]), o[r]);
+            }
+          } else {
+            floatx4 v = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (!HALF) v = o;
+#pragma unroll
+            for (int t = 0; t < JT; ++t)
+              if (2 * t <= it)
+#pragma unroll
+                for (int q = 0; q < NP; ++q) v = O::mma(zf[ct][t], pf[t][q], v);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = HALF ? fmaf(v[r], p_up, o[r]) : v[r];
+          }
+          if (i >= n) continue;
+          const int c = c0 + 16 * ct + lr;
+          const int64_t at = j.out.at(s.row(j.reverse, seg_first + first + i), h) + c;
+          if (j.out_f32) store4(static_cast<float*>(j.out.p) + at, o, j.vec_out, j.dz - c);
+          else store4(static_cast<T*>(j.out.p) + at, o, j.vec_out, j.dz - c);
+        }
+      }
+    }
+    const float whole = decay_power(g, n - 1 + e0);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      V u[JT][NU];
+#pragma unroll
+      for (int t = 0; t < JT; ++t) {
+        floatx8 v;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = static_cast<float>(zf[ct][t][k]) * U[t][k];
+        split<T, NU, HALF ? 11 : 0>(v, u[t]);
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[ct][dt][r] *= whole;
+        if constexpr (!HALF) v = S[ct][dt];
+#pragma unroll
+        for (int q = NU - 1; q >= 0; --q) {
+#pragma unroll
+          for (int t = 0; t < JT; ++t) v = O::mma(O::down(ys, PITCH, 32 * t, 16 * dt, lane), u[t][q], v);
+          if constexpr (HALF)
+            if (q)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) v[r] *= 1.f / 2048.f;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[ct][dt][r] = HALF ? fmaf(upd, v[r], S[ct][dt][r]) : v[r];
+      }
     }
   }
-  __syncthreads();
   const States& to = OUT ? j.last : j.between;
   if (OUT && (s.m != s.n - 1 || !to.p)) return;
-  const float f = OUT && j.reverse && s.hi > s.lo ? l : 1.f;  // (what reaches the state before the first token)
+  const float f = OUT && j.reverse && s.hi > s.lo ? decay_power(g, 1) : 1.f;  // (what reaches the state before the first row)
   float* p = to.of(OUT ? s.scene : id, a.heads, h);
-  for (int i = t; i < e; i += 256) p[(i / j.dz) * to.r + (i % j.dz) * to.c] = f * S[i];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * dt + lr + r, col = c0 + 16 * ct + lc;
+        if (row < j.dy && col < j.dz) p[row * to.r + col * to.c] = f * S[ct][dt][r];
+      }
 }
 
 // Sums of segments -> the state behind every segment but the last of its scene, in place.
@@ -241,20 +566,41 @@ int segment_rows(const spc_attn_desc* d) {
   return static_cast<int>(std::max<int64_t>(64, (want + 63) / 64 * 64));
 }
 
-// The states between segments of `a`'s first `n_sums` jobs lie in `ws`; the jobs behind them have theirs in place.
+bool in_pieces(const Rows& t, int width, int heads, int bytes, int es) {
+  const uintptr_t all = reinterpret_cast<uintptr_t>(t.p) | uintptr_t(t.row) * es | (heads > t.group ? uintptr_t(t.head) * es : 0) | uintptr_t(width) * es;
+  return all % bytes == 0;
+}
+
+template <typename T, int D, int NW>
+void launch_scan(ScanArgs& a, int n_sums, hipStream_t s) {
+  const size_t tile = size_t(CHUNK) * (D + Ops<T>::PAD) * sizeof(T);
+  auto grid = [&] { return dim3((a.n_ids * a.heads * a.n_jobs + 7) / 8 * 8); };
+  if (a.n_rows > a.seg_rows) {
+    const int jobs = a.n_jobs;
+    a.n_jobs = n_sums;
+    hipLaunchKernelGGL((scan_chunks_kernel<T, D, NW, false>), grid(), dim3(64 * NW), 2 * tile, s, a);
+    hipLaunchKernelGGL(scan_states_kernel, dim3((a.job[0].dy * a.job[0].dz + 255) / 256, a.n_scenes * a.heads, n_sums), dim3(256), 0, s, a);
+    a.n_jobs = jobs;
+  }
+  hipLaunchKernelGGL((scan_chunks_kernel<T, D, NW, true>), grid(), dim3(64 * NW), 3 * tile, s, a);
+}
+
+// The states between segments are made for the first n_sums jobs; the jobs behind them share theirs.
 int run_scan(ScanArgs& a, int n_sums, int32_t dtype, hipStream_t s) {
-  const size_t e = size_t(a.job[0].dy) * a.job[0].dz;
+  const int d = std::max(a.job[0].dy, a.job[0].dz);
   by_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    const size_t lds = (e + 3 * ATTN_MAX_D) * sizeof(float);
-    const int jobs = a.n_jobs;
-    if (n_sums && a.n_rows > a.seg_rows) {
-      a.n_jobs = n_sums;
-      hipLaunchKernelGGL((scan_rows_kernel<T, false>), dim3(a.n_ids * a.heads * n_sums), dim3(256), lds, s, a);
-      hipLaunchKernelGGL(scan_states_kernel, dim3((e + 255) / 256, a.n_scenes * a.heads, n_sums), dim3(256), 0, s, a);
-      a.n_jobs = jobs;
+    for (int q = 0; q < a.n_jobs; ++q) {
+      Job& j = a.job[q];
+      j.vec_x = in_pieces(j.x, j.dy, a.heads, 16, sizeof(T));
+      j.vec_y = in_pieces(j.y, j.dy, a.heads, 16, sizeof(T));
+      j.vec_z = in_pieces(j.z, j.dz, a.heads, 16, sizeof(T));
+      const int es = j.out_f32 ? 4 : sizeof(T);
+      j.vec_out = in_pieces(j.out, j.dz, a.heads, 4 * es, es);
     }
-    hipLaunchKernelGGL((scan_rows_kernel<T, true>), dim3(a.n_ids * a.heads * jobs), dim3(256), lds, s, a);
+    if (d <= 32) launch_scan<T, 32, 2>(a, n_sums, s);
+    else if (d <= 64) launch_scan<T, 64, 4>(a, n_sums, s);
+    else launch_scan<T, 128, 4>(a, n_sums, s);
   });
   SPC_HIP_CHECK(hipGetLastError());
   return SPC_OK;
