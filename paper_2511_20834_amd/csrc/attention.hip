@@ -14,6 +14,9 @@
 
 #include "spc_internal.h"
 
+#ifndef SPC_MINW
+#define SPC_MINW 2
+#endif
 namespace spc {
 namespace {
 
@@ -46,6 +49,7 @@ struct ScanArgs {
   const int32_t* offsets;  // n_scenes + 1, or NULL: one scene of all rows
   int n_rows, n_scenes, heads, n_jobs;
   int seg_rows, n_ids;
+  int n_cols;  // workgroups that share a head's columns of z
   float scale;
 };
 
@@ -117,6 +121,11 @@ struct Ops {
     for (int r = 0; r < 4; ++r) f[r] = a.v[r], f[4 + r] = b.v[r];
     return f;
   }
+  __device__ static inline void put(T* p, V f) {
+    struct alignas(8) Half { T v[4]; };
+    *reinterpret_cast<Half*>(p) = Half{{f[0], f[1], f[2], f[3]}};
+    *reinterpret_cast<Half*>(p + 16) = Half{{f[4], f[5], f[6], f[7]}};
+  }
   // places down a column: tile row j0 + place, column c0 + l%16.  (Sixteen lanes read four rows of sixteen, and each receives a column of them.)
   __device__ static inline V down(const T* tile, int pitch, int j0, int c0, int lane) {
     const T* p = tile + (j0 + 4 * (lane / 16) + lane % 16 / 4) * pitch + c0 + lane % 4 * 4;
@@ -137,6 +146,10 @@ struct Ops<float> {
   __device__ static inline V along(const float* p) {
     const floatx4 a = *reinterpret_cast<const floatx4*>(p), b = *reinterpret_cast<const floatx4*>(p + 16);
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  __device__ static inline void put(float* p, V f) {
+    *reinterpret_cast<floatx4*>(p) = __builtin_shufflevector(f, f, 0, 1, 2, 3);
+    *reinterpret_cast<floatx4*>(p + 16) = __builtin_shufflevector(f, f, 4, 5, 6, 7);
   }
   __device__ static inline V down(const float* tile, int pitch, int j0, int c0, int lane) {
     const float* p = tile + (j0 + 4 * (lane / 16)) * pitch + c0 + lane % 16;
@@ -172,157 +185,191 @@ __device__ inline float over_quads(float v) {  // maximum over the four lanes of
   return fmaxf(v, __shfl_xor(v, 32, 64));
 }
 
-template <typename T, int D, int THREADS>
+// A chunk's rows of one tensor on their way from memory to LDS, in registers.  A segment's last chunk, where it is not full, lies in the tile's last rows;
+// the rows in front of it, and channels behind the head's last, are zeros.
+template <typename T, int D>
 struct TileLoad {
-  static constexpr int VE = 16 / sizeof(T), PER_ROW = D / VE, N = CHUNK * PER_ROW / THREADS, PITCH = D + Ops<T>::PAD;
+  static constexpr int VE = 16 / sizeof(T), PER_ROW = D / VE, STEP = 256 / PER_ROW, N = CHUNK / STEP, PITCH = D + Ops<T>::PAD;
   struct alignas(16) Piece { T v[VE]; };
   Piece q[N];
-  // Rows [first, first + CHUNK) of the scan (those from s.rows on, and channels from `width` on, are zeros)
-  __device__ void load(const Rows& t, bool pieces, int width, const Segment& s, bool reverse, int seg_first, int first, int h) {
-    const T* base = static_cast<const T*>(t.p) + (h / t.group) * t.head;
+  const T* p;    // this thread's place in the next chunk's first STEP rows
+  int64_t row;   // the next row of the scan
+  int left;      // channels from its first on
+  bool pieces;
+  __device__ void start(const Rows& t, bool in_pieces, int first_channel, int width, const Segment& s, bool reverse, int seg_first, int h) {
+    const int c = threadIdx.x % PER_ROW * VE + first_channel;
+    left = width - c;
+    pieces = in_pieces;
+    row = reverse ? -t.row : t.row;
+    p = static_cast<const T*>(t.p) + (h / t.group) * t.head + s.row(reverse, seg_first + int(threadIdx.x) / PER_ROW) * t.row + c;
+  }
+  __device__ void load(int rows) {
+    const int i = threadIdx.x / PER_ROW, shift = max(CHUNK - rows, 0);
+    const T* at = p - shift * row;
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const int i = (threadIdx.x + n * THREADS) / PER_ROW, c = (threadIdx.x + n * THREADS) % PER_ROW * VE;
+    for (int n = 0; n < N; ++n, at += STEP * row) {
       q[n] = Piece{};
-      if (first + i >= s.rows || c >= width) continue;
-      const T* p = base + s.row(reverse, seg_first + first + i) * t.row + c;
-      if (pieces) q[n] = *reinterpret_cast<const Piece*>(p);
-      else
+      if (i + n * STEP >= shift && left > 0) {
+        if (pieces) q[n] = *reinterpret_cast<const Piece*>(at);
+        else
 #pragma unroll
-        for (int k = 0; k < VE; ++k)
-          if (c + k < width) q[n].v[k] = p[k];
+          for (int k = 0; k < VE; ++k)
+            if (k < left) q[n].v[k] = at[k];
+      }
     }
+    p = at;
   }
   __device__ void store(T* tile) const {
+    T* to = tile + threadIdx.x / PER_ROW * PITCH + threadIdx.x % PER_ROW * VE;
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const int i = (threadIdx.x + n * THREADS) / PER_ROW, c = (threadIdx.x + n * THREADS) % PER_ROW * VE;
-      *reinterpret_cast<Piece*>(tile + i * PITCH + c) = q[n];
-    }
+    for (int n = 0; n < N; ++n) *reinterpret_cast<Piece*>(to + n * STEP * PITCH) = q[n];
+  }
+  __device__ bool finite() const {
+    using Bits = std::conditional_t<sizeof(T) == 2, unsigned short, unsigned>;
+    typedef Bits BitsV __attribute__((ext_vector_type(VE)));
+    constexpr Bits magnitude = static_cast<Bits>(~Bits(0)) >> 1;
+    constexpr Bits infinity = std::is_same_v<T, _Float16> ? Bits(0x7c00) : std::is_same_v<T, __bf16> ? Bits(0x7f80) : Bits(0x7f800000);
+    BitsV m = 0;
+#pragma unroll
+    for (int n = 0; n < N; ++n) m = __builtin_elementwise_max(m, __builtin_bit_cast(BitsV, q[n]) & magnitude);
+    Bits most = 0;
+#pragma unroll
+    for (int k = 0; k < VE; ++k) most = m[k] > most ? m[k] : most;
+    return most < infinity;
   }
 };
+__device__ inline float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
 
-// One segment of one head: chunk by chunk, with the state in registers.  NW waves share the chunk's tiles; each owns D / NW columns of z, of
-// the output and of the state, and computes the chunk's products P^T = Y X^T for itself, since they are the next product's operand as they lie.
-//   O^T = Z^T P^T + S^T X^T,   S <- l^n S + Y^T (w o Z)
+template <typename T, int DY, int DZ, bool OUT>
+constexpr size_t scan_lds() {
+  constexpr int py = DY + Ops<T>::PAD, pz = DZ + Ops<T>::PAD, pieces = sizeof(T) == 2 ? 2 : 1;
+  return sizeof(T) * (CHUNK * (py + pz) + (OUT ? CHUNK * py + pieces * DZ * py : 0)) + (OUT ? sizeof(float) * (DZ + 4) : 0);
+}
+
+// One segment of one head and DZ columns of z: chunk by chunk, with the state in registers.
+//   O^T = Z^T P^T + S^T X^T,  P^T = (Y X^T) o l^(i-j),   S <- l^n S + Y^T (w o Z)
+// Each of the four waves makes 16 rows of the chunk's output, whose products P^T are the next product's operand as they lie in its registers, and (the first
+// DZ / 16 of them) keeps 16 columns of the state, which all waves read from LDS as the pieces they multiply.
 // Operands that are no inputs (P, S, w o Z) go into 16-bit products as two pieces, the weighted values of bf16 as three: 16 bits of every sum that is
-// rounded to a 16-bit output in the end, 24 (fp16: 22) of what the state adds up.  fp16's pieces are scaled by powers of two, P by the largest in a row, S by
-// the largest in a column, since sums may leave its range.  fp32 takes fp32 products.
-template <typename T, int D, int NW, bool OUT>
-__global__ __launch_bounds__(64 * NW) void scan_chunks_kernel(const ScanArgs a) {
+// rounded to a 16-bit output in the end, 24 (fp16: 22) of what the state adds up.  fp16's pieces are scaled by powers of two, P by the largest of a row, S by
+// the largest of a column, since sums may leave its range.  fp32 takes fp32 products.
+template <typename T, int DY, int DZ, bool OUT>
+__global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanArgs a) {
   using O = Ops<T>;
   using V = typename O::V;
   constexpr bool HALF = std::is_same_v<T, _Float16>, SINGLE = std::is_same_v<T, float>;
   constexpr int NP = SINGLE ? 1 : 2, NU = SINGLE ? 1 : HALF ? 2 : 3;  // pieces of P and S, of the weighted values
-  constexpr int CT = D / NW / 16, DT = D / 16, KT = D / 32, IT = CHUNK / 16, JT = CHUNK / 32, PITCH = D + O::PAD;
+  constexpr int CT = DZ / 16, DT = DY / 16, KT = DY / 32, IT = CHUNK / 16, JT = CHUNK / 32, PY = DY + O::PAD, PZ = DZ + O::PAD;
   extern __shared__ __align__(16) char lds[];
-  T *ys = reinterpret_cast<T*>(lds), *zs = ys + CHUNK * PITCH, *xs = zs + CHUNK * PITCH;
+  T *ys = reinterpret_cast<T*>(lds), *zs = ys + CHUNK * PY, *xs = zs + CHUNK * PZ, *sp = xs + CHUNK * PY;
+  float* s_scale = reinterpret_cast<float*>(sp + NP * DZ * PY);  // by column, of the pieces of S
+  int* odd = reinterpret_cast<int*>(s_scale + DZ);               // the last chunk with a value that is not finite, from 1 on
 
   // workgroups that follow each other go to the eight XCDs in turn: neighbours of one segment share an L2 this way
-  const int total = a.n_ids * a.heads * a.n_jobs, share = (total + 7) / 8, work = blockIdx.x % 8 * share + blockIdx.x / 8;
+  const int total = a.n_ids * a.heads * a.n_jobs * a.n_cols, share = (total + 7) / 8, work = blockIdx.x % 8 * share + blockIdx.x / 8;
   if (work >= total) return;
-  const Job& j = a.job[work % a.n_jobs];
-  const int h = work / a.n_jobs % a.heads, id = work / a.n_jobs / a.heads;
+  const Job& j = a.job[work / a.n_cols % a.n_jobs];
+  const int h = work / a.n_cols / a.n_jobs % a.heads, id = work / a.n_cols / a.n_jobs / a.heads;
+  const int col0 = work % a.n_cols * DZ, dz = j.dz - col0;
+  if (dz <= 0) return;
   Segment s;
   if (!s.find(a, id)) return;
   if (!OUT && s.m == s.n - 1) return;  // nobody starts from it
-  const int lane = threadIdx.x % 64, lc = lane % 16, lr = lane / 16 * 4, c0 = threadIdx.x / 64 * (16 * CT), seg_first = s.m * a.seg_rows;
+  const int lane = threadIdx.x % 64, lc = lane % 16, lr = lane / 16 * 4, seg_first = s.m * a.seg_rows;
+  // (which rows and columns are a wave's changes from workgroup to workgroup: the waves of a SIMD have unlike shares of the work)
+  const int it = __builtin_amdgcn_readfirstlane((threadIdx.x / 64 + work) % 4), ct_s = (it + 2) % 4;
+  const bool owner = ct_s < CT;
   const bool special = j.reverse && !s.m;  // the gradient of the last state meets the last row undecayed
   const float g = a.log_decay[h];
   const float p_scale = a.scale, upd = j.reverse ? a.scale : 1.f, inter = j.reverse ? 1.f : a.scale;
 
-  floatx4 S[CT][DT];
-  const bool from = OUT && (s.m || j.first.p);
+  floatx4 S[DT];
   {
+    const bool from = OUT && owner && (s.m || j.first.p);
     const States& st = s.m ? j.between : j.first;
     const float* p = from ? st.of(s.m ? id - 1 : s.scene, a.heads, h) : nullptr;
+    const int col = 16 * ct_s + lc;
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = 16 * dt + lr + r, col = c0 + 16 * ct + lc;
-          S[ct][dt][r] = from && row < j.dy && col < j.dz ? p[row * st.r + col * st.c] : 0.f;
-        }
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * dt + lr + r;
+        S[dt][r] = from && row < j.dy && col < dz ? p[row * st.r + (col0 + col) * st.c] : 0.f;
+      }
   }
-  float W[IT][4], tile_decay[IT], U[JT][8];
+  // decays: of P (its columns are rows 16 it + lc of the chunk), of the state on the way to an output row, of a row's product on the way into the state
+  float W[IT][4], u[4], u_tile[IT];
 #pragma unroll
   for (int t = 0; t < IT; ++t) {
-    tile_decay[t] = decay_power(g, 16 * t);
+    u_tile[t] = uniform((HALF ? 1.f : upd) * decay_power(g, 48 - 16 * t));
 #pragma unroll
-    for (int r = 0; r < 4; ++r) W[t][r] = p_scale * decay_power(g, 16 * t + lc - lr - r);  // (negative: above the diagonal, not used)
+    for (int r = 0; r < 4; ++r) {
+      W[t][r] = p_scale * decay_power(g, 16 * (it - t) + lc - lr - r);  // (above the diagonal: not used)
+      if (!t) u[r] = decay_power(g, 15 - lr - r);
+    }
   }
-  int n_u = -1;
+  const float f_full = inter * decay_power(g, 16 * it + lc + 1), whole_full = decay_power(g, CHUNK);
 
-  TileLoad<T, D, 64 * NW> x, y, z;
-  auto fetch = [&](int first) {
-    if (OUT) x.load(j.x, j.vec_x, j.dy, s, j.reverse, seg_first, first, h);
-    y.load(j.y, j.vec_y, j.dy, s, j.reverse, seg_first, first, h);
-    z.load(j.z, j.vec_z, j.dz, s, j.reverse, seg_first, first, h);
+  TileLoad<T, DY> x, y;
+  TileLoad<T, DZ> z;
+  if (OUT) x.start(j.x, j.vec_x, 0, j.dy, s, j.reverse, seg_first, h);
+  y.start(j.y, j.vec_y, 0, j.dy, s, j.reverse, seg_first, h);
+  z.start(j.z, j.vec_z, col0, j.dz, s, j.reverse, seg_first, h);
+  auto fetch = [&](int rows) {
+    if (OUT) x.load(rows);
+    y.load(rows);
+    z.load(rows);
   };
-  fetch(0);
+  if (s.rows > 0) fetch(s.rows);
+  const bool out_f32 = j.out_f32, out_pieces = j.vec_out;
+  const int es = out_f32 ? 4 : sizeof(T);
+  const int64_t out_row = (j.reverse ? -j.out.row : j.out.row) * es;
+  char* out = nullptr;  // row 16 it + lc of the chunk, channel lr of these columns
+  if (OUT) out = static_cast<char*>(j.out.p) + (j.out.at(s.row(j.reverse, seg_first), h) + col0 + lr) * es + (16 * it + lc) * out_row;
+  if (OUT && !threadIdx.x) *odd = 0;
+
 #pragma unroll 1
   for (int first = 0; first < s.rows; first += CHUNK) {
-    const int n = min(CHUNK, s.rows - first), e0 = special && !first ? 0 : 1;
+    const int n = min(CHUNK, s.rows - first), shift = CHUNK - n, e0 = special && !first ? 0 : 1;
     __syncthreads();
-    if (OUT) x.store(xs);
     y.store(ys);
     z.store(zs);
-    __syncthreads();
-    if (first + CHUNK < s.rows) fetch(first + CHUNK);
-    if (n != n_u) {  // (all chunks but a segment's last are full)
-      n_u = n;
-#pragma unroll
-      for (int t = 0; t < JT; ++t)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) U[t][k] = (HALF ? 1.f : upd) * decay_power(g, n - 1 - (32 * t + 16 * (k / 4) + lr + k % 4));
-    }
-    V zf[CT][JT];
-    float odd = 0.f;  // NaN if a value is not finite
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-      for (int t = 0; t < JT; ++t) {
-        zf[ct][t] = O::down(zs, PITCH, 32 * t, c0 + 16 * ct, lane);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) odd = fmaf(static_cast<float>(zf[ct][t][k]), 0.f, odd);
-      }
     if constexpr (OUT) {
-      // Zero times infinity is NaN: where a value is not finite, the zeros of P above the diagonal would bring it to earlier rows.
-      const bool by_rows = __ballot(odd != odd) != 0;
-      V sf[CT][KT][NP];
-      floatx4 s_scale[CT];
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
+      x.store(xs);
+      if (!z.finite()) *odd = first + 1;
+      if (owner) {
         int e = 0;
         if constexpr (HALF) {
           float m = 0.f;
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(S[ct][dt][r]));
+            for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(S[dt][r]));
           e = __builtin_amdgcn_frexp_expf(over_quads(m));
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s_scale[ct][r] = ldexpf(1.f, __shfl(e, lr + r, 64));
+          if (lane < 16) s_scale[16 * ct_s + lc] = ldexpf(1.f, e);
         }
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
-          floatx8 v = __builtin_shufflevector(S[ct][2 * k], S[ct][2 * k + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+          floatx8 v = __builtin_shufflevector(S[2 * k], S[2 * k + 1], 0, 1, 2, 3, 4, 5, 6, 7);
           if constexpr (HALF) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] = ldexpf(v[q], -e);
           }
-          split<T, NP>(v, sf[ct][k]);
+          V f[NP];
+          split<T, NP>(v, f);
+#pragma unroll
+          for (int q = 0; q < NP; ++q) O::put(sp + (q * DZ + 16 * ct_s + lc) * PY + 32 * k + lr, f[q]);
         }
       }
-      const float f0 = inter * decay_power(g, lc + e0);
-#pragma unroll
-      for (int it = 0; it < IT; ++it) {
-        if (16 * it >= n) break;
+    }
+    __syncthreads();
+    if (first + CHUNK < s.rows) fetch(s.rows - first - CHUNK);
+    if constexpr (OUT) {
+      if (16 * it + 15 >= shift) {
+        const int i = 16 * it + lc;
         V xf[KT];
 #pragma unroll
-        for (int k = 0; k < KT; ++k) xf[k] = O::along(xs + (16 * it + lc) * PITCH + 32 * k + lr);
+        for (int k = 0; k < KT; ++k) xf[k] = O::along(xs + i * PY + 32 * k + lr);
         floatx8 P[JT];
         float m = 0.f;
 #pragma unroll
@@ -330,11 +377,10 @@ __global__ __launch_bounds__(64 * NW) void scan_chunks_kernel(const ScanArgs a) 
           floatx4 p = {0.f, 0.f, 0.f, 0.f};
           if (jt <= it) {
 #pragma unroll
-            for (int k = 0; k < KT; ++k) p = O::mma(O::along(ys + (16 * jt + lc) * PITCH + 32 * k + lr), xf[k], p);
+            for (int k = 0; k < KT; ++k) p = O::mma(O::along(ys + (16 * jt + lc) * PY + 32 * k + lr), xf[k], p);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              p[r] *= W[it - jt][r];
-              if (jt == it && lr + r > lc) p[r] = 0.f;
+              p[r] = jt < it || lr + r <= lc ? p[r] * W[jt][r] : 0.f;
               if constexpr (HALF) m = fmaxf(m, fabsf(p[r]));
             }
           }
@@ -352,93 +398,101 @@ __global__ __launch_bounds__(64 * NW) void scan_chunks_kernel(const ScanArgs a) 
         }
         V pf[JT][NP];
 #pragma unroll
-        for (int t = 0; t < JT; ++t)
-          if (2 * t <= it) split<T, NP>(P[t], pf[t]);
-        const float f = f0 * tile_decay[it];
-        const int i = 16 * it + lc;
+        for (int t = 0; t < JT; ++t) split<T, NP>(P[t], pf[t]);
+        const float f = shift || !e0 ? inter * decay_power(g, i - shift + e0) : f_full;
+        floatx4 o[CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          floatx4 o = {0.f, 0.f, 0.f, 0.f};
+          o[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int k = 0; k < KT; ++k)
 #pragma unroll
-            for (int q = 0; q < NP; ++q) o = O::mma(sf[ct][k][q], xf[k], o);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) o[r] *= HALF ? f * s_scale[ct][r] : f;
-          if (by_rows) {
-            const int c = c0 + 16 * ct + lr;
+            for (int q = 0; q < NP; ++q) o[ct] = O::mma(O::along(sp + (q * DZ + 16 * ct + lc) * PY + 32 * k + lr), xf[k], o[ct]);
+          if constexpr (HALF) o[ct] *= *reinterpret_cast<const floatx4*>(s_scale + 16 * ct + lr);
+          o[ct] *= f;
+        }
+        // Zero times infinity is NaN: where a value is not finite, the zeros of P above the diagonal would bring it to earlier rows.
+        if (*odd == first + 1) {
 #pragma unroll 1
-            for (int q = 0; q <= i; ++q) {
-              float w = 0.f;
+          for (int q = 0; q <= i; ++q) {
+            float w = 0.f;
 #pragma unroll 1
-              for (int d = 0; d < j.dy; ++d) w = fmaf(static_cast<float>(xs[i * PITCH + d]), static_cast<float>(ys[q * PITCH + d]), w);
-              w *= p_scale * decay_power(g, i - q);
+            for (int d = 0; d < j.dy; ++d) w = fmaf(static_cast<float>(xs[i * PY + d]), static_cast<float>(ys[q * PY + d]), w);
+            w *= p_scale * decay_power(g, i - q);
 #pragma unroll
-              for (int r = 0; r < 4; ++r) o[r] = fmaf(w, static_cast<float>(zs[q * PITCH + c + r]), o[r]);
-            }
-          } else {
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) o[ct][r] = fmaf(w, static_cast<float>(zs[q * PZ + 16 * ct + lr + r]), o[ct][r]);
+          }
+        } else {
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
             floatx4 v = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (!HALF) v = o;
+            if constexpr (!HALF) v = o[ct];
 #pragma unroll
             for (int t = 0; t < JT; ++t)
-              if (2 * t <= it)
+              if (2 * t <= it) {
+                const V zf = O::down(zs, PZ, 32 * t, 16 * ct, lane);
 #pragma unroll
-                for (int q = 0; q < NP; ++q) v = O::mma(zf[ct][t], pf[t][q], v);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = HALF ? fmaf(v[r], p_up, o[r]) : v[r];
+                for (int q = 0; q < NP; ++q) v = O::mma(zf, pf[t][q], v);
+              }
+            if constexpr (HALF) o[ct] += v * p_up;
+            else o[ct] = v;
           }
-          if (i >= n) continue;
-          const int c = c0 + 16 * ct + lr;
-          const int64_t at = j.out.at(s.row(j.reverse, seg_first + first + i), h) + c;
-          if (j.out_f32) store4(static_cast<float*>(j.out.p) + at, o, j.vec_out, j.dz - c);
-          else store4(static_cast<T*>(j.out.p) + at, o, j.vec_out, j.dz - c);
+        }
+        if (i >= shift) {
+          char* at = out - shift * out_row;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            if (out_f32) store4(reinterpret_cast<float*>(at) + 16 * ct, o[ct], out_pieces, dz - 16 * ct - lr);
+            else store4(reinterpret_cast<T*>(at) + 16 * ct, o[ct], out_pieces, dz - 16 * ct - lr);
+          }
         }
       }
+      out += CHUNK * out_row;
     }
-    const float whole = decay_power(g, n - 1 + e0);
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      V u[JT][NU];
+    if (owner) {
+      V uf[JT][NU];
 #pragma unroll
       for (int t = 0; t < JT; ++t) {
+        const V zf = O::down(zs, PZ, 32 * t, 16 * ct_s, lane);
         floatx8 v;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = static_cast<float>(zf[ct][t][k]) * U[t][k];
-        split<T, NU, HALF ? 11 : 0>(v, u[t]);
+        for (int k = 0; k < 8; ++k) v[k] = static_cast<float>(zf[k]) * (u[k % 4] * u_tile[2 * t + k / 4]);
+        split<T, NU, HALF ? 11 : 0>(v, uf[t]);
       }
+      const float whole = shift || !e0 ? decay_power(g, n - 1 + e0) : whole_full;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        floatx4 v = {0.f, 0.f, 0.f, 0.f};
+        V yf[JT];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[ct][dt][r] *= whole;
-        if constexpr (!HALF) v = S[ct][dt];
+        for (int t = 0; t < JT; ++t) yf[t] = O::down(ys, PY, 32 * t, 16 * dt, lane);
+        floatx4 v = {0.f, 0.f, 0.f, 0.f};
+        S[dt] *= whole;
+        if constexpr (!HALF) v = S[dt];
 #pragma unroll
         for (int q = NU - 1; q >= 0; --q) {
 #pragma unroll
-          for (int t = 0; t < JT; ++t) v = O::mma(O::down(ys, PITCH, 32 * t, 16 * dt, lane), u[t][q], v);
-          if constexpr (HALF)
-            if (q)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) v[r] *= 1.f / 2048.f;
+          for (int t = 0; t < JT; ++t) v = O::mma(yf[t], uf[t][q], v);
+          if (HALF && q) v *= 1.f / 2048.f;
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[ct][dt][r] = HALF ? fmaf(upd, v[r], S[ct][dt][r]) : v[r];
+        if constexpr (HALF) S[dt] += v * upd;
+        else S[dt] = v;
       }
     }
   }
   const States& to = OUT ? j.last : j.between;
-  if (OUT && (s.m != s.n - 1 || !to.p)) return;
+  if (!owner || (OUT && (s.m != s.n - 1 || !to.p))) return;
   const float f = OUT && j.reverse && s.hi > s.lo ? decay_power(g, 1) : 1.f;  // (what reaches the state before the first row)
   float* p = to.of(OUT ? s.scene : id, a.heads, h);
+  const int col = 16 * ct_s + lc;
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct)
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * dt + lr + r, col = c0 + 16 * ct + lc;
-        if (row < j.dy && col < j.dz) p[row * to.r + col * to.c] = f * S[ct][dt][r];
-      }
+    for (int r = 0; r < 4; ++r) {
+      const int row = 16 * dt + lr + r;
+      if (row < j.dy && col < dz) p[row * to.r + (col0 + col) * to.c] = f * S[dt][r];
+    }
 }
 
 // Sums of segments -> the state behind every segment but the last of its scene, in place.
@@ -454,10 +508,20 @@ __global__ __launch_bounds__(256) void scan_states_kernel(const ScanArgs a) {
   const int r = i / j.dz, c = i % j.dz;
   float S = j.first.p ? j.first.of(scene, a.heads, h)[r * j.first.r + c * j.first.c] : 0.f;
   const float whole = decay_power(l, a.seg_rows);
-  for (int m = 0; m + 1 < s.n; ++m) {
-    float* p = j.between.of(id + m, a.heads, h) + r * j.between.r + c * j.between.c;
-    S = (j.reverse && !m ? decay_power(l, a.seg_rows - 1) : whole) * S + *p;
-    *p = S;
+  const int64_t step = a.heads * j.between.each;
+  float* p = j.between.of(id, a.heads, h) + r * j.between.r + c * j.between.c;
+  constexpr int AHEAD = 16;  // (the loads of a chain's links do not depend on each other)
+  for (int m = 0; m + 1 < s.n; m += AHEAD) {
+    float v[AHEAD];
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) v[q] = m + q + 1 < s.n ? p[q * step] : 0.f;
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) {
+      if (m + q + 1 >= s.n) break;
+      S = (j.reverse && !(m + q) ? decay_power(l, a.seg_rows - 1) : whole) * S + v[q];
+      p[q * step] = S;
+    }
+    p += AHEAD * step;
   }
 }
 
@@ -571,23 +635,33 @@ bool in_pieces(const Rows& t, int width, int heads, int bytes, int es) {
   return all % bytes == 0;
 }
 
-template <typename T, int D, int NW>
-void launch_scan(ScanArgs& a, int n_sums, hipStream_t s) {
-  const size_t tile = size_t(CHUNK) * (D + Ops<T>::PAD) * sizeof(T);
-  auto grid = [&] { return dim3((a.n_ids * a.heads * a.n_jobs + 7) / 8 * 8); };
+template <typename T, int DY, int DZ>
+int launch_scan(ScanArgs& a, int n_sums, hipStream_t s) {
+  int dz = 0;
+  for (int q = 0; q < a.n_jobs; ++q) dz = std::max(dz, a.job[q].dz);
+  a.n_cols = (dz + DZ - 1) / DZ;
+  auto grid = [&] { return dim3((a.n_ids * a.heads * a.n_jobs * a.n_cols + 7) / 8 * 8); };
   if (a.n_rows > a.seg_rows) {
     const int jobs = a.n_jobs;
     a.n_jobs = n_sums;
-    hipLaunchKernelGGL((scan_chunks_kernel<T, D, NW, false>), grid(), dim3(64 * NW), 2 * tile, s, a);
+    hipLaunchKernelGGL((scan_chunks_kernel<T, DY, DZ, false>), grid(), dim3(256), (scan_lds<T, DY, DZ, false>()), s, a);
     hipLaunchKernelGGL(scan_states_kernel, dim3((a.job[0].dy * a.job[0].dz + 255) / 256, a.n_scenes * a.heads, n_sums), dim3(256), 0, s, a);
     a.n_jobs = jobs;
   }
-  hipLaunchKernelGGL((scan_chunks_kernel<T, D, NW, true>), grid(), dim3(64 * NW), 3 * tile, s, a);
+  constexpr size_t lds = scan_lds<T, DY, DZ, true>();
+  if constexpr (lds > 64 * 1024) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&scan_chunks_kernel<T, DY, DZ, true>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+    SPC_HIP_CHECK(attr);
+  }
+  hipLaunchKernelGGL((scan_chunks_kernel<T, DY, DZ, true>), grid(), dim3(256), lds, s, a);
+  return SPC_OK;
 }
 
 // The states between segments are made for the first n_sums jobs; the jobs behind them share theirs.
 int run_scan(ScanArgs& a, int n_sums, int32_t dtype, hipStream_t s) {
-  const int d = std::max(a.job[0].dy, a.job[0].dz);
+  int dy = 0, dz = 0, rc = SPC_OK;
+  for (int q = 0; q < a.n_jobs; ++q) dy = std::max(dy, a.job[q].dy), dz = std::max(dz, a.job[q].dz);
   by_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     for (int q = 0; q < a.n_jobs; ++q) {
@@ -598,10 +672,10 @@ int run_scan(ScanArgs& a, int n_sums, int32_t dtype, hipStream_t s) {
       const int es = j.out_f32 ? 4 : sizeof(T);
       j.vec_out = in_pieces(j.out, j.dz, a.heads, 4 * es, es);
     }
-    if (d <= 32) launch_scan<T, 32, 2>(a, n_sums, s);
-    else if (d <= 64) launch_scan<T, 64, 4>(a, n_sums, s);
-    else launch_scan<T, 128, 4>(a, n_sums, s);
+    if (dz <= 32) rc = dy <= 32 ? launch_scan<T, 32, 32>(a, n_sums, s) : dy <= 64 ? launch_scan<T, 64, 32>(a, n_sums, s) : launch_scan<T, 128, 32>(a, n_sums, s);
+    else rc = dy <= 32 ? launch_scan<T, 32, 64>(a, n_sums, s) : dy <= 64 ? launch_scan<T, 64, 64>(a, n_sums, s) : launch_scan<T, 128, 64>(a, n_sums, s);
   });
+  SPC_RETURN_IF(rc);
   SPC_HIP_CHECK(hipGetLastError());
   return SPC_OK;
 }
