@@ -14,8 +14,8 @@
 
 #include "spc_internal.h"
 
-#ifndef SPC_MINW
-#define SPC_MINW 2
+#ifndef SPC_ROUNDS
+#define SPC_ROUNDS 1
 #endif
 namespace spc {
 namespace {
@@ -76,7 +76,8 @@ struct Segment {
   __device__ int64_t row(bool reverse, int i) const { return reverse ? int64_t(hi) - 1 - i : int64_t(lo) + i; }
 };
 
-__device__ inline float decay_power(float log_decay, int n) { return n > 0 ? expf(log_decay * n) : 1.f; }
+// 2^(g n), n >= 0 (g: the decay's logarithm to base 2, perhaps -infinity)
+__device__ inline float decay_power(float g, int n) { return n > 0 ? __builtin_amdgcn_exp2f(g * n) : 1.f; }
 
 // Up to four consecutive channels (`left` of them exist).
 template <typename T>
@@ -101,62 +102,87 @@ typedef int intx4 __attribute__((ext_vector_type(4)));
 
 constexpr int CHUNK = 64;  // rows whose products with each other are taken directly
 
+// Tiles in LDS have rows of D channels in pieces of 16 bytes, whose order is another in every row: piece q of row r lies at q ^ f(r).  Lanes that read the same
+// piece of 16 rows, or two pieces of eight rows, then meet all 64 banks once, without padding.
+template <typename T, int D>
+struct Tile {
+  static constexpr int VE = 16 / sizeof(T), PIECES = D / VE;
+  static constexpr int SAME = PIECES >= 16 ? 0 : PIECES == 8 ? 1 : 2;  // log2 of the rows that meet different banks as they are
+  __device__ static inline int turn(int r) { return ((r >> SAME) & (7 >> SAME)) * 2 + ((r >> 3) & 1); }
+  __device__ static inline int at(int r, int c) { return r * D + ((c / VE ^ turn(r)) * VE + c % VE); }
+};
+
 // A fragment holds 32 places of a contraction for 16 rows (A) or columns (B): lane l has row l%16 and the places 16 h + 4 (l/16) + r, h < 2, r < 4,
 // as element 4 h + r.  The results of two 16 x 16 products, whose lane l holds column l%16 and rows 4 (l/16) + r, are one as they come: sums of
 // products go from one product into the next without passing through LDS.
 template <typename T>
 struct Ops {
   using V = std::conditional_t<std::is_same_v<T, _Float16>, half8, bf16x8>;
-  static constexpr int PAD = 8;
+  using LDS4 = __attribute__((address_space(3))) shortx4*;
   __device__ static inline floatx4 mma(V a, V b, floatx4 c) {
     if constexpr (std::is_same_v<T, _Float16>) return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
-  // places along a row of the tile: p points to (row l%16, place 4 (l/16))
-  __device__ static inline V along(const T* p) {
-    struct alignas(8) Half { T v[4]; };
-    const Half a = *reinterpret_cast<const Half*>(p), b = *reinterpret_cast<const Half*>(p + 16);
-    V f;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) f[r] = a.v[r], f[4 + r] = b.v[r];
-    return f;
-  }
-  __device__ static inline void put(T* p, V f) {
-    struct alignas(8) Half { T v[4]; };
-    *reinterpret_cast<Half*>(p) = Half{{f[0], f[1], f[2], f[3]}};
-    *reinterpret_cast<Half*>(p + 16) = Half{{f[4], f[5], f[6], f[7]}};
-  }
-  // places down a column: tile row j0 + place, column c0 + l%16.  (Sixteen lanes read four rows of sixteen, and each receives a column of them.)
-  __device__ static inline V down(const T* tile, int pitch, int j0, int c0, int lane) {
-    const T* p = tile + (j0 + 4 * (lane / 16) + lane % 16 / 4) * pitch + c0 + lane % 4 * 4;
-    using P = __attribute__((address_space(3))) shortx4*;
-    const shortx4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p)), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 16 * pitch));
-    return __builtin_bit_cast(V, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-  }
+  __device__ static inline V both(shortx4 a, shortx4 b) { return __builtin_bit_cast(V, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)); }
 };
 template <>
 struct Ops<float> {
   using V = floatx8;
-  static constexpr int PAD = 4;
   __device__ static inline floatx4 mma(V a, V b, floatx4 c) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[k], b[k], c, 0, 0, 0);
     return c;
   }
-  __device__ static inline V along(const float* p) {
-    const floatx4 a = *reinterpret_cast<const floatx4*>(p), b = *reinterpret_cast<const floatx4*>(p + 16);
-    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+};
+// Fragments of a tile whose places lie along its rows: row l%16 (of 16 that start at a multiple of 16), places from 32 k on.  (Channels that are multiples of
+// two pieces change other bits of a place than the lane does.)
+template <typename T, int D>
+struct Along {
+  using V = typename Ops<T>::V;
+  int at;
+  __device__ Along(int lane) : at(Tile<T, D>::at(lane % 16, lane / 16 * 4)) {}
+  __device__ V get(const T* rows, int k) const {
+    const T *p = rows + (at ^ 32 * k), *q = rows + (at ^ (32 * k + 16));
+    if constexpr (sizeof(T) == 2) return Ops<T>::both(*reinterpret_cast<const shortx4*>(p), *reinterpret_cast<const shortx4*>(q));
+    else return __builtin_shufflevector(*reinterpret_cast<const floatx4*>(p), *reinterpret_cast<const floatx4*>(q), 0, 1, 2, 3, 4, 5, 6, 7);
   }
-  __device__ static inline void put(float* p, V f) {
-    *reinterpret_cast<floatx4*>(p) = __builtin_shufflevector(f, f, 0, 1, 2, 3);
-    *reinterpret_cast<floatx4*>(p + 16) = __builtin_shufflevector(f, f, 4, 5, 6, 7);
+  __device__ void put(T* rows, int k, V f) const {
+    T *p = rows + (at ^ 32 * k), *q = rows + (at ^ (32 * k + 16));
+    if constexpr (sizeof(T) == 2) {
+      typedef short shortx8 __attribute__((ext_vector_type(8)));
+      const shortx8 v = __builtin_bit_cast(shortx8, f);
+      *reinterpret_cast<shortx4*>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+      *reinterpret_cast<shortx4*>(q) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+    } else {
+      *reinterpret_cast<floatx4*>(p) = __builtin_shufflevector(f, f, 0, 1, 2, 3);
+      *reinterpret_cast<floatx4*>(q) = __builtin_shufflevector(f, f, 4, 5, 6, 7);
+    }
   }
-  __device__ static inline V down(const float* tile, int pitch, int j0, int c0, int lane) {
-    const float* p = tile + (j0 + 4 * (lane / 16)) * pitch + c0 + lane % 16;
-    V f;
+};
+// Fragments whose places lie down its columns: column l%16 of the 16 from c on, rows from a multiple of 32 on.  (16-bit types: sixteen lanes read
+// four rows of sixteen, and each receives a column of them.)
+template <typename T, int D>
+struct Down {
+  using V = typename Ops<T>::V;
+  static constexpr int N = sizeof(T) == 2 ? 1 : 4;
+  int at[N];
+  __device__ Down(int lane) {
+    if constexpr (sizeof(T) == 2) at[0] = Tile<T, D>::at(lane / 16 * 4 + lane % 16 / 4, lane % 4 * 4);
+    else
 #pragma unroll
-    for (int k = 0; k < 8; ++k) f[k] = p[(16 * (k / 4) + k % 4) * pitch];
-    return f;
+      for (int r = 0; r < 4; ++r) at[r] = Tile<T, D>::at(lane / 16 * 4 + r, lane % 16);
+  }
+  __device__ V get(const T* rows, int c) const {
+    if constexpr (sizeof(T) == 2) {
+      using P = typename Ops<T>::LDS4;
+      const T* p = rows + (at[0] ^ c);
+      return Ops<T>::both(__builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p)), __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 16 * D)));
+    } else {
+      V f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f[k] = rows[k / 4 * 16 * D + (at[k % 4] ^ c)];
+      return f;
+    }
   }
 };
 // x as a sum of N fragments: each holds what the ones before have left of it, times 2^(SHIFT * its number).
@@ -167,16 +193,15 @@ __device__ inline void split(floatx8 x, typename Ops<T>::V (&out)[N]) {
   } else {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) out[n][k] = static_cast<T>(x[k]);
+      out[n] = __builtin_convertvector(x, typename Ops<T>::V);
       if (n + 1 == N) break;
       // (what is left is left by the value that the product takes: without this the compiler rounds it twice, once of an unrounded
       // product by a conversion that multiplies, and the two differ now and then)
       intx4 q = __builtin_bit_cast(intx4, out[n]);
       asm("" : "+v"(q));
       out[n] = __builtin_bit_cast(typename Ops<T>::V, q);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = (x[k] - static_cast<float>(out[n][k])) * (SHIFT ? float(1 << SHIFT) : 1.f);
+      x -= __builtin_convertvector(out[n], floatx8);
+      if (SHIFT) x *= float(1 << SHIFT);
     }
   }
 }
@@ -184,85 +209,101 @@ __device__ inline float over_quads(float v) {  // maximum over the four lanes of
   v = fmaxf(v, __shfl_xor(v, 16, 64));
   return fmaxf(v, __shfl_xor(v, 32, 64));
 }
+__device__ inline float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
 
-// A chunk's rows of one tensor on their way from memory to LDS, in registers.  A segment's last chunk, where it is not full, lies in the tile's last rows;
-// the rows in front of it, and channels behind the head's last, are zeros.
+// A chunk's rows of one tensor on their way from memory to LDS.  A segment's last chunk, where it is not full, lies in the tile's last rows; the rows in
+// front of it, and channels behind the head's last, are zeros.  Rows that can be read in pieces of 16 bytes are in registers while the chunk before is worked
+// on; others are read channel by channel when they are due.
 template <typename T, int D>
 struct TileLoad {
-  static constexpr int VE = 16 / sizeof(T), PER_ROW = D / VE, STEP = 256 / PER_ROW, N = CHUNK / STEP, PITCH = D + Ops<T>::PAD;
-  struct alignas(16) Piece { T v[VE]; };
-  Piece q[N];
-  const T* p;    // this thread's place in the next chunk's first STEP rows
-  int64_t row;   // the next row of the scan
-  int left;      // channels from its first on
+  static constexpr int VE = 16 / sizeof(T), PER_ROW = D / VE, STEP = 256 / PER_ROW, N = CHUNK / STEP;
+  static constexpr bool ONCE = STEP % 16 == 0;  // a thread's rows have the same order of pieces
+  using Bits = std::conditional_t<sizeof(T) == 2, unsigned short, unsigned>;
+  typedef Bits BitsV __attribute__((ext_vector_type(VE)));
+  static constexpr Bits MAGNITUDE = static_cast<Bits>(~Bits(0)) >> 1;
+  static constexpr Bits INFINITE = std::is_same_v<T, _Float16> ? Bits(0x7c00) : std::is_same_v<T, __bf16> ? Bits(0x7f80) : Bits(0x7f800000);
+  intx4 q[N];
+  const T* origin;  // channel 0 of the columns, row 0 of the next chunk
+  int64_t row;      // the next row of the scan
+  int width;        // channels of these columns that there are
   bool pieces;
-  __device__ void start(const Rows& t, bool in_pieces, int first_channel, int width, const Segment& s, bool reverse, int seg_first, int h) {
-    const int c = threadIdx.x % PER_ROW * VE + first_channel;
-    left = width - c;
+  __device__ void start(const Rows& t, bool in_pieces, int first_channel, int channels, const Segment& s, bool reverse, int seg_first, int h) {
+    width = min(channels - first_channel, D);
     pieces = in_pieces;
     row = reverse ? -t.row : t.row;
-    p = static_cast<const T*>(t.p) + (h / t.group) * t.head + s.row(reverse, seg_first + int(threadIdx.x) / PER_ROW) * t.row + c;
+    origin = static_cast<const T*>(t.p) + (h / t.group) * t.head + s.row(reverse, seg_first) * t.row + first_channel;
   }
   __device__ void load(int rows) {
-    const int i = threadIdx.x / PER_ROW, shift = max(CHUNK - rows, 0);
-    const T* at = p - shift * row;
+    const int i = threadIdx.x / PER_ROW, c = threadIdx.x % PER_ROW * VE, shift = max(CHUNK - rows, 0);
+    origin -= shift * row;
+    if (!pieces) return;
+    const T* at = origin + (i * row + c);
 #pragma unroll
     for (int n = 0; n < N; ++n, at += STEP * row) {
-      q[n] = Piece{};
-      if (i + n * STEP >= shift && left > 0) {
-        if (pieces) q[n] = *reinterpret_cast<const Piece*>(at);
-        else
+      q[n] = intx4{0, 0, 0, 0};
+      if (i + n * STEP >= shift && c < width) q[n] = *reinterpret_cast<const intx4*>(at);
+    }
+  }
+  // CHECK: returns whether what this thread has stored is finite
+  template <bool CHECK>
+  __device__ bool store(T* tile, int shift) {
+    BitsV m = 0;
+    if (pieces) {
+      const int i = threadIdx.x / PER_ROW, c = threadIdx.x % PER_ROW * VE;
+      T* to = tile + Tile<T, D>::at(i, c);
 #pragma unroll
-          for (int k = 0; k < VE; ++k)
-            if (k < left) q[n].v[k] = at[k];
+      for (int n = 0; n < N; ++n) {
+        *reinterpret_cast<intx4*>(ONCE ? to + n * STEP * D : tile + Tile<T, D>::at(i + n * STEP, c)) = q[n];
+        if (CHECK) m = __builtin_elementwise_max(m, __builtin_bit_cast(BitsV, q[n]) & MAGNITUDE);
+      }
+    } else {
+      int e = threadIdx.x;
+      asm volatile("" : "+v"(e));  // (no places of this loop are kept in registers from chunk to chunk)
+#pragma unroll 4
+      for (; e < CHUNK * D; e += 256) {
+        const int r = e / D, c = e % D;
+        const T v = r >= shift && c < width ? origin[r * row + c] : T(0.f);
+        tile[Tile<T, D>::at(r, c)] = v;
+        if (CHECK) m[0] = max(m[0], static_cast<Bits>(__builtin_bit_cast(Bits, v) & MAGNITUDE));
       }
     }
-    p = at;
-  }
-  __device__ void store(T* tile) const {
-    T* to = tile + threadIdx.x / PER_ROW * PITCH + threadIdx.x % PER_ROW * VE;
-#pragma unroll
-    for (int n = 0; n < N; ++n) *reinterpret_cast<Piece*>(to + n * STEP * PITCH) = q[n];
-  }
-  __device__ bool finite() const {
-    using Bits = std::conditional_t<sizeof(T) == 2, unsigned short, unsigned>;
-    typedef Bits BitsV __attribute__((ext_vector_type(VE)));
-    constexpr Bits magnitude = static_cast<Bits>(~Bits(0)) >> 1;
-    constexpr Bits infinity = std::is_same_v<T, _Float16> ? Bits(0x7c00) : std::is_same_v<T, __bf16> ? Bits(0x7f80) : Bits(0x7f800000);
-    BitsV m = 0;
-#pragma unroll
-    for (int n = 0; n < N; ++n) m = __builtin_elementwise_max(m, __builtin_bit_cast(BitsV, q[n]) & magnitude);
+    origin += CHUNK * row;
     Bits most = 0;
+    if (CHECK)
 #pragma unroll
-    for (int k = 0; k < VE; ++k) most = m[k] > most ? m[k] : most;
-    return most < infinity;
+      for (int k = 0; k < VE; ++k) most = max(most, m[k]);
+    return most < INFINITE;
   }
 };
-__device__ inline float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
 
 template <typename T, int DY, int DZ, bool OUT>
 constexpr size_t scan_lds() {
-  constexpr int py = DY + Ops<T>::PAD, pz = DZ + Ops<T>::PAD, pieces = sizeof(T) == 2 ? 2 : 1;
-  return sizeof(T) * (CHUNK * (py + pz) + (OUT ? CHUNK * py + pieces * DZ * py : 0)) + (OUT ? sizeof(float) * (DZ + 4) : 0);
+  return sizeof(T) * (CHUNK * (DY + DZ) + (OUT ? CHUNK * DY + (sizeof(T) == 2 ? 2 : 1) * DZ * DY : 0)) + (OUT ? sizeof(float) * (DZ + 4) : 0);
+}
+
+// Workgroups (a wave on every SIMD) that a CU holds, by registers and LDS.
+template <typename T, int DY, int DZ>
+constexpr int scan_waves() {
+  return DY == 128 || (sizeof(T) == 4 && DY == 64) ? 2 : sizeof(T) == 2 && DY == 32 && DZ == 32 ? 4 : 3;
 }
 
 // One segment of one head and DZ columns of z: chunk by chunk, with the state in registers.
 //   O^T = Z^T P^T + S^T X^T,  P^T = (Y X^T) o l^(i-j),   S <- l^n S + Y^T (w o Z)
-// Each of the four waves makes 16 rows of the chunk's output, whose products P^T are the next product's operand as they lie in its registers, and (the first
-// DZ / 16 of them) keeps 16 columns of the state, which all waves read from LDS as the pieces they multiply.
+// Each of the four waves makes 16 rows of the chunk's output, whose products P^T are the next product's operand as they lie in its registers, and (DZ / 16 of
+// them) keeps 16 columns of the state, which all waves read from LDS as the pieces they multiply.
 // Operands that are no inputs (P, S, w o Z) go into 16-bit products as two pieces, the weighted values of bf16 as three: 16 bits of every sum that is
 // rounded to a 16-bit output in the end, 24 (fp16: 22) of what the state adds up.  fp16's pieces are scaled by powers of two, P by the largest of a row, S by
 // the largest of a column, since sums may leave its range.  fp32 takes fp32 products.
 template <typename T, int DY, int DZ, bool OUT>
-__global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanArgs a) {
+__global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_kernel(const ScanArgs a) {
   using O = Ops<T>;
   using V = typename O::V;
   constexpr bool HALF = std::is_same_v<T, _Float16>, SINGLE = std::is_same_v<T, float>;
   constexpr int NP = SINGLE ? 1 : 2, NU = SINGLE ? 1 : HALF ? 2 : 3;  // pieces of P and S, of the weighted values
-  constexpr int CT = DZ / 16, DT = DY / 16, KT = DY / 32, IT = CHUNK / 16, JT = CHUNK / 32, PY = DY + O::PAD, PZ = DZ + O::PAD;
+  constexpr int CT = DZ / 16, DT = DY / 16, KT = DY / 32, IT = CHUNK / 16, JT = CHUNK / 32;
   extern __shared__ __align__(16) char lds[];
-  T *ys = reinterpret_cast<T*>(lds), *zs = ys + CHUNK * PY, *xs = zs + CHUNK * PZ, *sp = xs + CHUNK * PY;
-  float* s_scale = reinterpret_cast<float*>(sp + NP * DZ * PY);  // by column, of the pieces of S
+  T *ys = reinterpret_cast<T*>(lds), *zs = ys + CHUNK * DY, *xs = zs + CHUNK * DZ, *sp = xs + CHUNK * DY;
+  float* s_scale = reinterpret_cast<float*>(sp + NP * DZ * DY);  // by column, of the pieces of S
   int* odd = reinterpret_cast<int*>(s_scale + DZ);               // the last chunk with a value that is not finite, from 1 on
 
   // workgroups that follow each other go to the eight XCDs in turn: neighbours of one segment share an L2 this way
@@ -280,8 +321,20 @@ __global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanAr
   const int it = __builtin_amdgcn_readfirstlane((threadIdx.x / 64 + work) % 4), ct_s = (it + 2) % 4;
   const bool owner = ct_s < CT;
   const bool special = j.reverse && !s.m;  // the gradient of the last state meets the last row undecayed
-  const float g = a.log_decay[h];
+  const float g = a.log_decay[h] * 1.44269504f;
   const float p_scale = a.scale, upd = j.reverse ? a.scale : 1.f, inter = j.reverse ? 1.f : a.scale;
+
+  TileLoad<T, DY> x, y;
+  TileLoad<T, DZ> z;
+  if (OUT) x.start(j.x, j.vec_x, 0, j.dy, s, j.reverse, seg_first, h);
+  y.start(j.y, j.vec_y, 0, j.dy, s, j.reverse, seg_first, h);
+  z.start(j.z, j.vec_z, col0, j.dz, s, j.reverse, seg_first, h);
+  auto fetch = [&](int rows) {
+    if (OUT) x.load(rows);
+    y.load(rows);
+    z.load(rows);
+  };
+  if (s.rows > 0) fetch(s.rows);
 
   floatx4 S[DT];
   {
@@ -295,32 +348,21 @@ __global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanAr
       for (int r = 0; r < 4; ++r) {
         const int row = 16 * dt + lr + r;
         S[dt][r] = from && row < j.dy && col < dz ? p[row * st.r + (col0 + col) * st.c] : 0.f;
+        __builtin_amdgcn_sched_barrier(0);  // (few addresses at a time)
       }
   }
-  // decays: of P (its columns are rows 16 it + lc of the chunk), of the state on the way to an output row, of a row's product on the way into the state
-  float W[IT][4], u[4], u_tile[IT];
+  // decays: of P (on the diagonal, and below it as a product of two; its columns are rows 16 it + lc of the chunk), and of a row's product on the way into
+  // the state, as a product of two
+  float w_same[4], w[4], w_tile[IT - 1], u[4], u_tile[IT];
 #pragma unroll
-  for (int t = 0; t < IT; ++t) {
-    u_tile[t] = uniform((HALF ? 1.f : upd) * decay_power(g, 48 - 16 * t));
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      W[t][r] = p_scale * decay_power(g, 16 * (it - t) + lc - lr - r);  // (above the diagonal: not used)
-      if (!t) u[r] = decay_power(g, 15 - lr - r);
-    }
+  for (int r = 0; r < 4; ++r) {
+    w_same[r] = p_scale * decay_power(g, lc - lr - r);  // (above the diagonal: not used)
+    w[r] = p_scale * decay_power(g, 15 + lc - lr - r);
+    u[r] = decay_power(g, 15 - lr - r);
+    u_tile[r] = uniform((HALF ? 1.f : upd) * decay_power(g, 48 - 16 * r));
+    if (r + 1 < IT) w_tile[r] = uniform(decay_power(g, 16 * (it - r) - 15));
   }
-  const float f_full = inter * decay_power(g, 16 * it + lc + 1), whole_full = decay_power(g, CHUNK);
-
-  TileLoad<T, DY> x, y;
-  TileLoad<T, DZ> z;
-  if (OUT) x.start(j.x, j.vec_x, 0, j.dy, s, j.reverse, seg_first, h);
-  y.start(j.y, j.vec_y, 0, j.dy, s, j.reverse, seg_first, h);
-  z.start(j.z, j.vec_z, col0, j.dz, s, j.reverse, seg_first, h);
-  auto fetch = [&](int rows) {
-    if (OUT) x.load(rows);
-    y.load(rows);
-    z.load(rows);
-  };
-  if (s.rows > 0) fetch(s.rows);
+  const float f_full = inter * decay_power(g, 16 * it + lc + 1), whole_full = uniform(decay_power(g, CHUNK));
   const bool out_f32 = j.out_f32, out_pieces = j.vec_out;
   const int es = out_f32 ? 4 : sizeof(T);
   const int64_t out_row = (j.reverse ? -j.out.row : j.out.row) * es;
@@ -331,12 +373,18 @@ __global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanAr
 #pragma unroll 1
   for (int first = 0; first < s.rows; first += CHUNK) {
     const int n = min(CHUNK, s.rows - first), shift = CHUNK - n, e0 = special && !first ? 0 : 1;
+    int here = lane;  // (places are made anew in every chunk, of few registers, and not all of them once)
+    asm volatile("" : "+v"(here));
+    const Along<T, DY> along(here);
+    const Down<T, DY> down_y(here);
+    const Down<T, DZ> down_z(here);
+    const int lc = here % 16, lr = here / 16 * 4;
     __syncthreads();
-    y.store(ys);
-    z.store(zs);
+    y.template store<false>(ys, shift);
+    const bool finite = z.template store<OUT>(zs, shift);
     if constexpr (OUT) {
-      x.store(xs);
-      if (!z.finite()) *odd = first + 1;
+      x.template store<false>(xs, shift);
+      if (!finite) *odd = first + 1;
       if (owner) {
         int e = 0;
         if constexpr (HALF) {
@@ -358,7 +406,7 @@ __global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanAr
           V f[NP];
           split<T, NP>(v, f);
 #pragma unroll
-          for (int q = 0; q < NP; ++q) O::put(sp + (q * DZ + 16 * ct_s + lc) * PY + 32 * k + lr, f[q]);
+          for (int q = 0; q < NP; ++q) along.put(sp + (q * DZ + 16 * ct_s) * DY, k, f[q]);
         }
       }
     }
@@ -369,7 +417,7 @@ __global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanAr
         const int i = 16 * it + lc;
         V xf[KT];
 #pragma unroll
-        for (int k = 0; k < KT; ++k) xf[k] = O::along(xs + i * PY + 32 * k + lr);
+        for (int k = 0; k < KT; ++k) xf[k] = along.get(xs + 16 * it * DY, k);
         floatx8 P[JT];
         float m = 0.f;
 #pragma unroll
@@ -377,10 +425,11 @@ __global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanAr
           floatx4 p = {0.f, 0.f, 0.f, 0.f};
           if (jt <= it) {
 #pragma unroll
-            for (int k = 0; k < KT; ++k) p = O::mma(O::along(ys + (16 * jt + lc) * PY + 32 * k + lr), xf[k], p);
+            for (int k = 0; k < KT; ++k) p = O::mma(along.get(ys + 16 * jt * DY, k), xf[k], p);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              p[r] = jt < it || lr + r <= lc ? p[r] * W[jt][r] : 0.f;
+              p[r] *= jt < it ? w[r] * w_tile[jt % 3] : w_same[r];
+              if (jt == it && lr + r > lc) p[r] = 0.f;
               if constexpr (HALF) m = fmaxf(m, fabsf(p[r]));
             }
           }
@@ -399,6 +448,7 @@ __global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanAr
         V pf[JT][NP];
 #pragma unroll
         for (int t = 0; t < JT; ++t) split<T, NP>(P[t], pf[t]);
+        __builtin_amdgcn_sched_barrier(0);  // (here and below: fragments are read when they are due, 168 registers have to do)
         const float f = shift || !e0 ? inter * decay_power(g, i - shift + e0) : f_full;
         floatx4 o[CT];
 #pragma unroll
@@ -407,46 +457,63 @@ __global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanAr
 #pragma unroll
           for (int k = 0; k < KT; ++k)
 #pragma unroll
-            for (int q = 0; q < NP; ++q) o[ct] = O::mma(O::along(sp + (q * DZ + 16 * ct + lc) * PY + 32 * k + lr), xf[k], o[ct]);
+            for (int q = 0; q < NP; ++q) o[ct] = O::mma(along.get(sp + (q * DZ + 16 * ct) * DY, k), xf[k], o[ct]);
           if constexpr (HALF) o[ct] *= *reinterpret_cast<const floatx4*>(s_scale + 16 * ct + lr);
           o[ct] *= f;
+          __builtin_amdgcn_sched_barrier(0);
         }
-        // Zero times infinity is NaN: where a value is not finite, the zeros of P above the diagonal would bring it to earlier rows.
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          floatx4 v = {0.f, 0.f, 0.f, 0.f};
+          if constexpr (!HALF) v = o[ct];
+#pragma unroll
+          for (int t = 0; t < JT; ++t)
+            if (2 * t <= it) {
+              const V zf = down_z.get(zs + 32 * t * DZ, 16 * ct);
+#pragma unroll
+              for (int q = 0; q < NP; ++q) v = O::mma(zf, pf[t][q], v);
+            }
+          if constexpr (HALF) o[ct] += v * p_up;
+          else o[ct] = v;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        char* at = out - shift * out_row;
+        auto put = [&](int ct, floatx4 v) {
+          if (i < shift) return;
+          if (out_f32) store4(reinterpret_cast<float*>(at) + 16 * ct, v, out_pieces, dz - 16 * ct - lr);
+          else store4(reinterpret_cast<T*>(at) + 16 * ct, v, out_pieces, dz - 16 * ct - lr);
+        };
+        // Zero times infinity is NaN: where a value is not finite, the zeros of P above the diagonal bring it to earlier rows.  Such a chunk's outputs are
+        // computed from their own pairs alone.
         if (*odd == first + 1) {
 #pragma unroll 1
-          for (int q = 0; q <= i; ++q) {
-            float w = 0.f;
+          for (int ct = 0; ct < CT; ++ct) {
+            floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-            for (int d = 0; d < j.dy; ++d) w = fmaf(static_cast<float>(xs[i * PY + d]), static_cast<float>(ys[q * PY + d]), w);
-            w *= p_scale * decay_power(g, i - q);
+            for (int d = 0; d < j.dy; ++d) {
+              const float w = f * static_cast<float>(xs[Tile<T, DY>::at(i, d)]);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
+              for (int r = 0; r < 4; ++r) {
+                const int c = 16 * ct + lr + r;
+                float st = static_cast<float>(sp[Tile<T, DY>::at(c, d)]);
+                if (NP > 1) st += static_cast<float>(sp[DZ * DY + Tile<T, DY>::at(c, d)]);
+                v[r] = fmaf(w, HALF ? st * s_scale[c] : st, v[r]);
+              }
+            }
+#pragma unroll 1
+            for (int q = 0; q <= i; ++q) {
+              float w = 0.f;
+#pragma unroll 1
+              for (int d = 0; d < j.dy; ++d) w = fmaf(static_cast<float>(xs[Tile<T, DY>::at(i, d)]), static_cast<float>(ys[Tile<T, DY>::at(q, d)]), w);
+              w *= p_scale * decay_power(g, i - q);
 #pragma unroll
-              for (int r = 0; r < 4; ++r) o[ct][r] = fmaf(w, static_cast<float>(zs[q * PZ + 16 * ct + lr + r]), o[ct][r]);
+              for (int r = 0; r < 4; ++r) v[r] = fmaf(w, static_cast<float>(zs[Tile<T, DZ>::at(q, 16 * ct + lr + r)]), v[r]);
+            }
+            put(ct, v);
           }
         } else {
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            floatx4 v = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (!HALF) v = o[ct];
-#pragma unroll
-            for (int t = 0; t < JT; ++t)
-              if (2 * t <= it) {
-                const V zf = O::down(zs, PZ, 32 * t, 16 * ct, lane);
-#pragma unroll
-                for (int q = 0; q < NP; ++q) v = O::mma(zf, pf[t][q], v);
-              }
-            if constexpr (HALF) o[ct] += v * p_up;
-            else o[ct] = v;
-          }
-        }
-        if (i >= shift) {
-          char* at = out - shift * out_row;
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            if (out_f32) store4(reinterpret_cast<float*>(at) + 16 * ct, o[ct], out_pieces, dz - 16 * ct - lr);
-            else store4(reinterpret_cast<T*>(at) + 16 * ct, o[ct], out_pieces, dz - 16 * ct - lr);
-          }
+          for (int ct = 0; ct < CT; ++ct) put(ct, o[ct]);
         }
       }
       out += CHUNK * out_row;
@@ -455,18 +522,17 @@ __global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanAr
       V uf[JT][NU];
 #pragma unroll
       for (int t = 0; t < JT; ++t) {
-        const V zf = O::down(zs, PZ, 32 * t, 16 * ct_s, lane);
-        floatx8 v;
+        floatx8 v = __builtin_convertvector(down_z.get(zs + 32 * t * DZ, 16 * ct_s), floatx8);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = static_cast<float>(zf[k]) * (u[k % 4] * u_tile[2 * t + k / 4]);
+        for (int k = 0; k < 8; ++k) v[k] *= u[k % 4] * u_tile[2 * t + k / 4];
         split<T, NU, HALF ? 11 : 0>(v, uf[t]);
       }
-      const float whole = shift || !e0 ? decay_power(g, n - 1 + e0) : whole_full;
+      const float whole = shift || !e0 ? uniform(decay_power(g, n - 1 + e0)) : whole_full;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         V yf[JT];
 #pragma unroll
-        for (int t = 0; t < JT; ++t) yf[t] = O::down(ys, PY, 32 * t, 16 * dt, lane);
+        for (int t = 0; t < JT; ++t) yf[t] = down_y.get(ys + 32 * t * DY, 16 * dt);
         floatx4 v = {0.f, 0.f, 0.f, 0.f};
         S[dt] *= whole;
         if constexpr (!HALF) v = S[dt];
@@ -484,14 +550,16 @@ __global__ __launch_bounds__(256, SPC_MINW) void scan_chunks_kernel(const ScanAr
   const States& to = OUT ? j.last : j.between;
   if (!owner || (OUT && (s.m != s.n - 1 || !to.p))) return;
   const float f = OUT && j.reverse && s.hi > s.lo ? decay_power(g, 1) : 1.f;  // (what reaches the state before the first row)
-  float* p = to.of(OUT ? s.scene : id, a.heads, h);
-  const int col = 16 * ct_s + lc;
+  int there = lane;  // (places are not those of the load above, kept over the chunks)
+  asm volatile("" : "+v"(there));
+  const int col = 16 * ct_s + there % 16;
+  float* p = to.of(OUT ? s.scene : id, a.heads, h) + int64_t(col0 + col) * to.c;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int row = 16 * dt + lr + r;
-      if (row < j.dy && col < dz) p[row * to.r + (col0 + col) * to.c] = f * S[dt][r];
+      const int row = 16 * dt + there / 16 * 4 + r;
+      if (row < j.dy && col < dz) p[row * to.r] = f * S[dt][r];
     }
 }
 
@@ -504,7 +572,7 @@ __global__ __launch_bounds__(256) void scan_states_kernel(const ScanArgs a) {
   const int id = lo / a.seg_rows + scene;
   Segment s;
   if (!s.find(a, id) || s.scene != scene) return;
-  const float l = a.log_decay[h];
+  const float l = a.log_decay[h] * 1.44269504f;
   const int r = i / j.dz, c = i % j.dz;
   float S = j.first.p ? j.first.of(scene, a.heads, h)[r * j.first.r + c * j.first.c] : 0.f;
   const float whole = decay_power(l, a.seg_rows);
@@ -624,9 +692,27 @@ void by_dtype(int32_t dtype, F&& f) {
   else f(0.f);
 }
 
-// Rows of a segment: multiples of 64, as few as give some 1024 workgroups a job.
-int segment_rows(const spc_attn_desc* d) {
-  const int64_t want = (d->n_rows * d->heads + 1023) / 1024;
+// Calls f(type, DY, DZ) with the kernels' tile widths for rows of y of dy channels and of z of dz.
+template <typename F>
+void by_shape(int32_t dtype, int dy, int dz, F&& f) {
+  by_dtype(dtype, [&](auto t) {
+    auto with = [&](auto w) {
+      if (dz <= 32) f(t, w, std::integral_constant<int, 32>{});
+      else f(t, w, std::integral_constant<int, 64>{});
+    };
+    if (dy <= 32) with(std::integral_constant<int, 32>{});
+    else if (dy <= 64) with(std::integral_constant<int, 64>{});
+    else with(std::integral_constant<int, 128>{});
+  });
+}
+
+// Rows of a segment: multiples of 64, as few as give the workgroups that 256 CUs hold at once.
+int segment_rows(const spc_attn_desc* d, int dy, int dz) {
+  int64_t at_once = 256;
+  by_shape(d->dtype, dy, dz, [&](auto t, auto y, auto z) {
+    at_once = SPC_ROUNDS * 256 * scan_waves<decltype(t), decltype(y)::value, decltype(z)::value>() / ((dz + decltype(z)::value - 1) / decltype(z)::value);
+  });
+  const int64_t want = (d->n_rows * d->heads + at_once - 1) / at_once;
   return static_cast<int>(std::max<int64_t>(64, (want + 63) / 64 * 64));
 }
 
@@ -662,7 +748,7 @@ int launch_scan(ScanArgs& a, int n_sums, hipStream_t s) {
 int run_scan(ScanArgs& a, int n_sums, int32_t dtype, hipStream_t s) {
   int dy = 0, dz = 0, rc = SPC_OK;
   for (int q = 0; q < a.n_jobs; ++q) dy = std::max(dy, a.job[q].dy), dz = std::max(dz, a.job[q].dz);
-  by_dtype(dtype, [&](auto t) {
+  by_shape(dtype, dy, dz, [&](auto t, auto y, auto z) {
     using T = decltype(t);
     for (int q = 0; q < a.n_jobs; ++q) {
       Job& j = a.job[q];
@@ -672,8 +758,7 @@ int run_scan(ScanArgs& a, int n_sums, int32_t dtype, hipStream_t s) {
       const int es = j.out_f32 ? 4 : sizeof(T);
       j.vec_out = in_pieces(j.out, j.dz, a.heads, 4 * es, es);
     }
-    if (dz <= 32) rc = dy <= 32 ? launch_scan<T, 32, 32>(a, n_sums, s) : dy <= 64 ? launch_scan<T, 64, 32>(a, n_sums, s) : launch_scan<T, 128, 32>(a, n_sums, s);
-    else rc = dy <= 32 ? launch_scan<T, 32, 64>(a, n_sums, s) : dy <= 64 ? launch_scan<T, 64, 64>(a, n_sums, s) : launch_scan<T, 128, 64>(a, n_sums, s);
+    rc = launch_scan<T, decltype(y)::value, decltype(z)::value>(a, n_sums, s);
   });
   SPC_RETURN_IF(rc);
   SPC_HIP_CHECK(hipGetLastError());
@@ -710,7 +795,7 @@ extern "C" int spc_linear_attention_forward(const spc_attn_desc* d, const spc_at
   j.last = {state_out, e, d->dv, 1};
   a.log_decay = log_decay, a.offsets = offsets, a.n_rows = static_cast<int>(d->n_rows), a.n_scenes = d->n_scenes, a.heads = d->heads, a.n_jobs = 1;
   a.scale = d->scale;
-  a.seg_rows = segment_rows(d);
+  a.seg_rows = segment_rows(d, d->dk, d->dv);
   a.n_ids = a.n_rows / a.seg_rows + a.n_scenes;
   float* ws = nullptr;
   if (a.n_rows > a.seg_rows) {
@@ -749,7 +834,7 @@ extern "C" int spc_linear_attention_backward(const spc_attn_desc* d, const spc_a
   ScanArgs a{};
   a.log_decay = log_decay, a.offsets = offsets, a.n_rows = static_cast<int>(d->n_rows), a.n_scenes = d->n_scenes, a.heads = d->heads, a.n_jobs = 3;
   a.scale = d->scale;
-  a.seg_rows = segment_rows(d);
+  a.seg_rows = segment_rows(d, std::max(d->dk, d->dv), std::max(d->dk, d->dv));
   a.n_ids = a.n_rows / a.seg_rows + a.n_scenes;
   const size_t states = a.n_rows > a.seg_rows ? size_t(a.n_ids) * a.heads * e : 0;
   const size_t parts = group > 1 ? size_t(a.n_rows) * a.heads : 0;  // gradients of shared keys and values, by head
