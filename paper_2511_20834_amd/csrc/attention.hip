@@ -51,6 +51,7 @@ struct ScanArgs {
   int seg_rows, n_ids;
   int n_cols;  // workgroups that share a head's columns of z
   float scale;
+  bool keep;  // whether a state is returned
 };
 
 // Segment `id` of all scenes.  Scene b's segments have the numbers lo(b) / seg_rows + b and following: floor(x) + floor(y) <= floor(x + y)
@@ -134,20 +135,22 @@ struct Ops<float> {
     return c;
   }
 };
-// Fragments of a tile whose places lie along its rows: row l%16 (of 16 that start at a multiple of 16), places from 32 k on.  (Channels that are multiples of
-// two pieces change other bits of a place than the lane does.)
+// Fragments of a tile whose places lie along its rows: row l%16 (of 16 that start at a multiple of 16), 32 places from 32 k on.  Read, a lane holds
+// the eight places from 8 (l/16) on: both operands of a product do.  Written as it comes out of a product, it holds those above.  (Channels that are
+// multiples of a piece, or two, change other bits of a place than the lane does.)
 template <typename T, int D>
 struct Along {
   using V = typename Ops<T>::V;
-  int at;
-  __device__ Along(int lane) : at(Tile<T, D>::at(lane % 16, lane / 16 * 4)) {}
+  int at, to;
+  __device__ Along(int lane) : at(Tile<T, D>::at(lane % 16, lane / 16 * 8)), to(Tile<T, D>::at(lane % 16, lane / 16 * 4)) {}
+  __device__ void renew() { asm volatile("" : "+v"(at), "+v"(to)); }  // (the places made of these before are not to be kept in registers)
   __device__ V get(const T* rows, int k) const {
-    const T *p = rows + (at ^ 32 * k), *q = rows + (at ^ (32 * k + 16));
-    if constexpr (sizeof(T) == 2) return Ops<T>::both(*reinterpret_cast<const shortx4*>(p), *reinterpret_cast<const shortx4*>(q));
-    else return __builtin_shufflevector(*reinterpret_cast<const floatx4*>(p), *reinterpret_cast<const floatx4*>(q), 0, 1, 2, 3, 4, 5, 6, 7);
+    if constexpr (sizeof(T) == 2) return *reinterpret_cast<const V*>(rows + (at ^ 32 * k));
+    else return __builtin_shufflevector(*reinterpret_cast<const floatx4*>(rows + (at ^ 32 * k)), *reinterpret_cast<const floatx4*>(rows + (at ^ (32 * k + 4))), 0,
+                                        1, 2, 3, 4, 5, 6, 7);
   }
   __device__ void put(T* rows, int k, V f) const {
-    T *p = rows + (at ^ 32 * k), *q = rows + (at ^ (32 * k + 16));
+    T *p = rows + (to ^ 32 * k), *q = rows + (to ^ (32 * k + 16));
     if constexpr (sizeof(T) == 2) {
       typedef short shortx8 __attribute__((ext_vector_type(8)));
       const shortx8 v = __builtin_bit_cast(shortx8, f);
@@ -171,6 +174,10 @@ struct Down {
     else
 #pragma unroll
       for (int r = 0; r < 4; ++r) at[r] = Tile<T, D>::at(lane / 16 * 4 + r, lane % 16);
+  }
+  __device__ void renew() {
+#pragma unroll
+    for (int r = 0; r < N; ++r) asm volatile("" : "+v"(at[r]));
   }
   __device__ V get(const T* rows, int c) const {
     if constexpr (sizeof(T) == 2) {
@@ -218,10 +225,6 @@ template <typename T, int D>
 struct TileLoad {
   static constexpr int VE = 16 / sizeof(T), PER_ROW = D / VE, STEP = 256 / PER_ROW, N = CHUNK / STEP;
   static constexpr bool ONCE = STEP % 16 == 0;  // a thread's rows have the same order of pieces
-  using Bits = std::conditional_t<sizeof(T) == 2, unsigned short, unsigned>;
-  typedef Bits BitsV __attribute__((ext_vector_type(VE)));
-  static constexpr Bits MAGNITUDE = static_cast<Bits>(~Bits(0)) >> 1;
-  static constexpr Bits INFINITE = std::is_same_v<T, _Float16> ? Bits(0x7c00) : std::is_same_v<T, __bf16> ? Bits(0x7f80) : Bits(0x7f800000);
   intx4 q[N];
   const T* origin;  // channel 0 of the columns, row 0 of the next chunk
   int64_t row;      // the next row of the scan
@@ -238,47 +241,39 @@ struct TileLoad {
     origin -= shift * row;
     if (!pieces) return;
     const T* at = origin + (i * row + c);
+    if (!shift && width == D) {
+#pragma unroll
+      for (int n = 0; n < N; ++n, at += STEP * row) q[n] = *reinterpret_cast<const intx4*>(at);
+      return;
+    }
 #pragma unroll
     for (int n = 0; n < N; ++n, at += STEP * row) {
       q[n] = intx4{0, 0, 0, 0};
       if (i + n * STEP >= shift && c < width) q[n] = *reinterpret_cast<const intx4*>(at);
     }
   }
-  // CHECK: returns whether what this thread has stored is finite
-  template <bool CHECK>
-  __device__ bool store(T* tile, int shift) {
-    BitsV m = 0;
+  __device__ void store(T* tile, int shift) {
     if (pieces) {
       const int i = threadIdx.x / PER_ROW, c = threadIdx.x % PER_ROW * VE;
       T* to = tile + Tile<T, D>::at(i, c);
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        *reinterpret_cast<intx4*>(ONCE ? to + n * STEP * D : tile + Tile<T, D>::at(i + n * STEP, c)) = q[n];
-        if (CHECK) m = __builtin_elementwise_max(m, __builtin_bit_cast(BitsV, q[n]) & MAGNITUDE);
-      }
+      for (int n = 0; n < N; ++n) *reinterpret_cast<intx4*>(ONCE ? to + n * STEP * D : tile + Tile<T, D>::at(i + n * STEP, c)) = q[n];
     } else {
       int e = threadIdx.x;
       asm volatile("" : "+v"(e));  // (no places of this loop are kept in registers from chunk to chunk)
 #pragma unroll 4
       for (; e < CHUNK * D; e += 256) {
         const int r = e / D, c = e % D;
-        const T v = r >= shift && c < width ? origin[r * row + c] : T(0.f);
-        tile[Tile<T, D>::at(r, c)] = v;
-        if (CHECK) m[0] = max(m[0], static_cast<Bits>(__builtin_bit_cast(Bits, v) & MAGNITUDE));
+        tile[Tile<T, D>::at(r, c)] = r >= shift && c < width ? origin[r * row + c] : T(0.f);
       }
     }
     origin += CHUNK * row;
-    Bits most = 0;
-    if (CHECK)
-#pragma unroll
-      for (int k = 0; k < VE; ++k) most = max(most, m[k]);
-    return most < INFINITE;
   }
 };
 
 template <typename T, int DY, int DZ, bool OUT>
 constexpr size_t scan_lds() {
-  return sizeof(T) * (CHUNK * (DY + DZ) + (OUT ? CHUNK * DY + (sizeof(T) == 2 ? 2 : 1) * DZ * DY : 0)) + (OUT ? sizeof(float) * (DZ + 4) : 0);
+  return sizeof(T) * (CHUNK * (DY + DZ) + (OUT ? CHUNK * DY + (sizeof(T) == 2 ? 2 : 1) * DZ * DY : 0)) + (OUT ? sizeof(float) * DZ : 0);
 }
 
 // Workgroups (a wave on every SIMD) that a CU holds, by registers and LDS.
@@ -304,7 +299,6 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
   extern __shared__ __align__(16) char lds[];
   T *ys = reinterpret_cast<T*>(lds), *zs = ys + CHUNK * DY, *xs = zs + CHUNK * DZ, *sp = xs + CHUNK * DY;
   float* s_scale = reinterpret_cast<float*>(sp + NP * DZ * DY);  // by column, of the pieces of S
-  int* odd = reinterpret_cast<int*>(s_scale + DZ);               // the last chunk with a value that is not finite, from 1 on
 
   // workgroups that follow each other go to the eight XCDs in turn: neighbours of one segment share an L2 this way
   const int total = a.n_ids * a.heads * a.n_jobs * a.n_cols, share = (total + 7) / 8, work = blockIdx.x % 8 * share + blockIdx.x / 8;
@@ -360,7 +354,7 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
     w[r] = p_scale * decay_power(g, 15 + lc - lr - r);
     u[r] = decay_power(g, 15 - lr - r);
     u_tile[r] = uniform((HALF ? 1.f : upd) * decay_power(g, 48 - 16 * r));
-    if (r + 1 < IT) w_tile[r] = uniform(decay_power(g, 16 * (it - r) - 15));
+    if (r + 1 < IT) w_tile[r] = uniform(decay_power(g, 16 * r + 1));
   }
   const float f_full = inter * decay_power(g, 16 * it + lc + 1), whole_full = uniform(decay_power(g, CHUNK));
   const bool out_f32 = j.out_f32, out_pieces = j.vec_out;
@@ -368,23 +362,24 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
   const int64_t out_row = (j.reverse ? -j.out.row : j.out.row) * es;
   char* out = nullptr;  // row 16 it + lc of the chunk, channel lr of these columns
   if (OUT) out = static_cast<char*>(j.out.p) + (j.out.at(s.row(j.reverse, seg_first), h) + col0 + lr) * es + (16 * it + lc) * out_row;
-  if (OUT && !threadIdx.x) *odd = 0;
+  const bool out_whole = out_pieces && !out_f32 && dz >= DZ;
+  const bool keep = a.keep;
+  Along<T, DY> along(lane);
+  Down<T, DY> down_y(lane);
+  Down<T, DZ> down_z(lane);
 
 #pragma unroll 1
   for (int first = 0; first < s.rows; first += CHUNK) {
     const int n = min(CHUNK, s.rows - first), shift = CHUNK - n, e0 = special && !first ? 0 : 1;
-    int here = lane;  // (places are made anew in every chunk, of few registers, and not all of them once)
+    along.renew(), down_y.renew(), down_z.renew();
+    int here = lane;
     asm volatile("" : "+v"(here));
-    const Along<T, DY> along(here);
-    const Down<T, DY> down_y(here);
-    const Down<T, DZ> down_z(here);
     const int lc = here % 16, lr = here / 16 * 4;
     __syncthreads();
-    y.template store<false>(ys, shift);
-    const bool finite = z.template store<OUT>(zs, shift);
+    y.store(ys, shift);
+    z.store(zs, shift);
     if constexpr (OUT) {
-      x.template store<false>(xs, shift);
-      if (!finite) *odd = first + 1;
+      x.store(xs, shift);
       if (owner) {
         int e = 0;
         if constexpr (HALF) {
@@ -413,23 +408,25 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
     __syncthreads();
     if (first + CHUNK < s.rows) fetch(s.rows - first - CHUNK);
     if constexpr (OUT) {
-      if (16 * it + 15 >= shift) {
-        const int i = 16 * it + lc;
+      // rows 16 IT_ + lc of the chunk
+      auto output = [&](auto rows) {
+        constexpr int IT_ = decltype(rows)::value, JN = IT_ / 2 + 1;
+        const int i = 16 * IT_ + lc;
         V xf[KT];
 #pragma unroll
-        for (int k = 0; k < KT; ++k) xf[k] = along.get(xs + 16 * it * DY, k);
-        floatx8 P[JT];
+        for (int k = 0; k < KT; ++k) xf[k] = along.get(xs + 16 * IT_ * DY, k);
+        floatx8 P[JN];
         float m = 0.f;
 #pragma unroll
-        for (int jt = 0; jt < IT; ++jt) {
+        for (int jt = 0; jt < 2 * JN; ++jt) {
           floatx4 p = {0.f, 0.f, 0.f, 0.f};
-          if (jt <= it) {
+          if (jt <= IT_) {
 #pragma unroll
             for (int k = 0; k < KT; ++k) p = O::mma(along.get(ys + 16 * jt * DY, k), xf[k], p);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              p[r] *= jt < it ? w[r] * w_tile[jt % 3] : w_same[r];
-              if (jt == it && lr + r > lc) p[r] = 0.f;
+              p[r] *= jt < IT_ ? w[r] * w_tile[IT_ - jt - 1] : w_same[r];
+              if (jt == IT_ && lr + r > lc) p[r] = 0.f;
               if constexpr (HALF) m = fmaxf(m, fabsf(p[r]));
             }
           }
@@ -441,14 +438,14 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
           const int e = __builtin_amdgcn_frexp_expf(over_quads(m));
           p_up = ldexpf(1.f, e);
 #pragma unroll
-          for (int t = 0; t < JT; ++t)
+          for (int t = 0; t < JN; ++t)
 #pragma unroll
             for (int k = 0; k < 8; ++k) P[t][k] = ldexpf(P[t][k], -e);
         }
-        V pf[JT][NP];
+        V pf[JN][NP];
 #pragma unroll
-        for (int t = 0; t < JT; ++t) split<T, NP>(P[t], pf[t]);
-        __builtin_amdgcn_sched_barrier(0);  // (here and below: fragments are read when they are due, 168 registers have to do)
+        for (int t = 0; t < JN; ++t) split<T, NP>(P[t], pf[t]);
+        __builtin_amdgcn_sched_barrier(0);  // (here and below: fragments are read when they are due, few registers have to do)
         const float f = shift || !e0 ? inter * decay_power(g, i - shift + e0) : f_full;
         floatx4 o[CT];
 #pragma unroll
@@ -462,19 +459,20 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
           o[ct] *= f;
           __builtin_amdgcn_sched_barrier(0);
         }
+        bool nan = false;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
           floatx4 v = {0.f, 0.f, 0.f, 0.f};
           if constexpr (!HALF) v = o[ct];
 #pragma unroll
-          for (int t = 0; t < JT; ++t)
-            if (2 * t <= it) {
-              const V zf = down_z.get(zs + 32 * t * DZ, 16 * ct);
+          for (int t = 0; t < JN; ++t) {
+            const V zf = down_z.get(zs + 32 * t * DZ, 16 * ct);
 #pragma unroll
-              for (int q = 0; q < NP; ++q) v = O::mma(zf, pf[t][q], v);
-            }
+            for (int q = 0; q < NP; ++q) v = O::mma(zf, pf[t][q], v);
+          }
           if constexpr (HALF) o[ct] += v * p_up;
           else o[ct] = v;
+          nan |= __builtin_isunordered(o[ct][0], o[ct][1]) | __builtin_isunordered(o[ct][2], o[ct][3]);
           __builtin_amdgcn_sched_barrier(0);
         }
         char* at = out - shift * out_row;
@@ -483,38 +481,49 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
           if (out_f32) store4(reinterpret_cast<float*>(at) + 16 * ct, v, out_pieces, dz - 16 * ct - lr);
           else store4(reinterpret_cast<T*>(at) + 16 * ct, v, out_pieces, dz - 16 * ct - lr);
         };
-        // Zero times infinity is NaN: where a value is not finite, the zeros of P above the diagonal bring it to earlier rows.  Such a chunk's outputs are
-        // computed from their own pairs alone.
-        if (*odd == first + 1) {
+        if (__ballot(nan)) {
+          // Zero times infinity is NaN: where a value is not finite, the zeros of P above the diagonal have brought it to earlier rows.  Outputs that are not
+          // numbers are computed from their own pairs alone.
 #pragma unroll 1
           for (int ct = 0; ct < CT; ++ct) {
             floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
             for (int d = 0; d < j.dy; ++d) {
-              const float w = f * static_cast<float>(xs[Tile<T, DY>::at(i, d)]);
+              const float xd = f * static_cast<float>(xs[Tile<T, DY>::at(i, d)]);
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 const int c = 16 * ct + lr + r;
                 float st = static_cast<float>(sp[Tile<T, DY>::at(c, d)]);
                 if (NP > 1) st += static_cast<float>(sp[DZ * DY + Tile<T, DY>::at(c, d)]);
-                v[r] = fmaf(w, HALF ? st * s_scale[c] : st, v[r]);
+                v[r] = fmaf(xd, HALF ? st * s_scale[c] : st, v[r]);
               }
             }
+            // (a state that is not finite makes these outputs what they are: nothing has to be added)
+            if (__ballot(!__builtin_isunordered(v[0], v[1]) || !__builtin_isunordered(v[2], v[3])))
 #pragma unroll 1
-            for (int q = 0; q <= i; ++q) {
-              float w = 0.f;
+              for (int q = 0; q <= i; ++q) {
+                float pq = 0.f;
 #pragma unroll 1
-              for (int d = 0; d < j.dy; ++d) w = fmaf(static_cast<float>(xs[Tile<T, DY>::at(i, d)]), static_cast<float>(ys[Tile<T, DY>::at(q, d)]), w);
-              w *= p_scale * decay_power(g, i - q);
+                for (int d = 0; d < j.dy; ++d) pq = fmaf(static_cast<float>(xs[Tile<T, DY>::at(i, d)]), static_cast<float>(ys[Tile<T, DY>::at(q, d)]), pq);
+                pq *= p_scale * decay_power(g, i - q);
 #pragma unroll
-              for (int r = 0; r < 4; ++r) v[r] = fmaf(w, static_cast<float>(zs[Tile<T, DZ>::at(q, 16 * ct + lr + r)]), v[r]);
-            }
+                for (int r = 0; r < 4; ++r) v[r] = fmaf(pq, static_cast<float>(zs[Tile<T, DZ>::at(q, 16 * ct + lr + r)]), v[r]);
+              }
             put(ct, v);
           }
+        } else if (out_whole && !shift) {
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) store4(reinterpret_cast<T*>(at) + 16 * ct, o[ct], true, 4);
         } else {
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) put(ct, o[ct]);
         }
+      };
+      if (16 * it + 15 >= shift) {
+        if (it == 0) output(std::integral_constant<int, 0>{});
+        else if (it == 1) output(std::integral_constant<int, 1>{});
+        else if (it == 2) output(std::integral_constant<int, 2>{});
+        else output(std::integral_constant<int, 3>{});
       }
       out += CHUNK * out_row;
     }
@@ -538,8 +547,9 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
         if constexpr (!HALF) v = S[dt];
 #pragma unroll
         for (int q = NU - 1; q >= 0; --q) {
+          if (q < 2 || keep)
 #pragma unroll
-          for (int t = 0; t < JT; ++t) v = O::mma(yf[t], uf[t][q], v);
+            for (int t = 0; t < JT; ++t) v = O::mma(yf[t], uf[t][q], v);
           if (HALF && q) v *= 1.f / 2048.f;
         }
         if constexpr (HALF) S[dt] += v * upd;
@@ -795,6 +805,7 @@ extern "C" int spc_linear_attention_forward(const spc_attn_desc* d, const spc_at
   j.last = {state_out, e, d->dv, 1};
   a.log_decay = log_decay, a.offsets = offsets, a.n_rows = static_cast<int>(d->n_rows), a.n_scenes = d->n_scenes, a.heads = d->heads, a.n_jobs = 1;
   a.scale = d->scale;
+  a.keep = state_out != nullptr;
   a.seg_rows = segment_rows(d, d->dk, d->dv);
   a.n_ids = a.n_rows / a.seg_rows + a.n_scenes;
   float* ws = nullptr;
@@ -834,6 +845,7 @@ extern "C" int spc_linear_attention_backward(const spc_attn_desc* d, const spc_a
   ScanArgs a{};
   a.log_decay = log_decay, a.offsets = offsets, a.n_rows = static_cast<int>(d->n_rows), a.n_scenes = d->n_scenes, a.heads = d->heads, a.n_jobs = 3;
   a.scale = d->scale;
+  a.keep = dstate_in != nullptr;
   a.seg_rows = segment_rows(d, std::max(d->dk, d->dv), std::max(d->dk, d->dv));
   a.n_ids = a.n_rows / a.seg_rows + a.n_scenes;
   const size_t states = a.n_rows > a.seg_rows ? size_t(a.n_ids) * a.heads * e : 0;
