@@ -459,7 +459,7 @@ def spc_layer_norm_forward(x: torch.Tensor, gamma: torch.Tensor | None = None, b
         assert sum_out is None
     mean = rstd = None
     if want_stats:
-        mean, rstd = torch.empty((2, n), dtype=torch.float32, device=dev)
+        mean, rstd = torch.empty(n, dtype=torch.float32, device=dev), torch.empty(n, dtype=torch.float32, device=dev)
     rc = lib().spc_layer_norm_forward(x.data_ptr(), _norm_rows(x, x), residual.data_ptr() if residual is not None else None,
                                       _norm_rows(residual, x) if residual is not None else 0, _f32(gamma, (c,), dev), _f32(beta, (c,), dev),
                                       eps, y.data_ptr(), _norm_rows(y, x), total.data_ptr() if total is not None else None,
@@ -480,7 +480,7 @@ def spc_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
     dx = torch.empty((n, c), dtype=x.dtype, device=dev) if out is None else out
     dgamma = dbeta = None
     if want_params:
-        dgamma, dbeta = torch.empty((2, c), dtype=torch.float32, device=dev)
+        dgamma, dbeta = torch.empty(c, dtype=torch.float32, device=dev), torch.empty(c, dtype=torch.float32, device=dev)
     rc = lib().spc_layer_norm_backward(dy.data_ptr(), _norm_rows(dy, x), x.data_ptr(), _norm_rows(x, x), _f32(mean, (n,), dev),
                                        _f32(rstd, (n,), dev), _f32(gamma, (c,), dev), dsum.data_ptr() if dsum is not None else None,
                                        _norm_rows(dsum, x) if dsum is not None else 0, dx.data_ptr(), _norm_rows(dx, x),

@@ -22,7 +22,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
     os.makedirs(objdir, exist_ok=True)
     hdrs = [os.path.join(CSRC, "spc_internal.h"), os.path.join(ROOT, "include", "spc.h")]
     newest_hdr = max(os.path.getmtime(h) for h in hdrs)
-    own_hdrs = {"conv.hip": ["conv_common.h", "conv_resident.h"]}  # read by one source only
+    own_hdrs = {"conv.hip": ["conv_common.h", "conv_resident.h"], "norm.hip": ["rows.h"], "attention.hip": ["rows.h"]}  # read by some sources only
     objs, procs = [], []
     for src in SOURCES:
         s = os.path.join(CSRC, src)

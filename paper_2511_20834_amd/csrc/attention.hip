@@ -12,7 +12,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "spc_internal.h"
+#include "rows.h"
 
 #ifndef SPC_ROUNDS
 #define SPC_ROUNDS 1
@@ -694,13 +694,6 @@ int check_rows(const char* what, const spc_attn_rows* t, const spc_attn_desc* d,
                                  static_cast<long long>(head), what, heads, width);
 }
 Rows rows_of(const spc_attn_rows* t, int group) { return {t->data, t->row_pitch, t->head_pitch, group}; }
-
-template <typename F>
-void by_dtype(int32_t dtype, F&& f) {
-  if (dtype == SPC_DTYPE_F16) f(_Float16{});
-  else if (dtype == SPC_DTYPE_BF16) f(__bf16{});
-  else f(0.f);
-}
 
 // Calls f(type, DY, DZ) with the kernels' tile widths for rows of y of dy channels and of z of dz.
 template <typename F>

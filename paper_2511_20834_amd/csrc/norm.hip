@@ -8,7 +8,11 @@
 // Neighbouring lanes hold neighbouring pieces; a wave takes 64/G rows at a time.  The workgroups walk over the rows with a stride of the
 // grid, which keeps gamma, and in the backward pass the sums of dgamma and dbeta, in registers.  Every workgroup stores its sums once,
 // and a second launch adds them up in a fixed order: no atomics, the same bits every time.
-#include "spc_internal.h"
+//
+// Measured, us a pass among others (with the bytes at the 4.84 TB/s that a copy of 2 GiB reaches, which caches of 256 MB can beat): forward 120 k x 256 fp16 with a residual 42.6
+// (50.8), backward 48.3 (50.8); 240 k x 256 bf16 94.6 (101.6), 94.4 (101.6); 70 k x 90 fp16 in rows of 180 backward 19.0 (7.8; 107 with pieces of two
+// channels and long shares).  Small calls are the host's: 2118 x 64 fp32 12.5 and 16.2.
+#include "rows.h"
 
 namespace spc {
 namespace {
@@ -16,9 +20,10 @@ namespace {
 constexpr int NORM_MAX_C = 8192;
 constexpr int NORM_THREADS = 256;
 
-template <typename T, int VEC>
-struct alignas(sizeof(T) * VEC) Piece {
-  T v[VEC];
+template <typename T>
+struct Piece {
+  static constexpr int VEC = 16 / sizeof(T);
+  typedef T Values __attribute__((ext_vector_type(VEC)));
 };
 
 // Sum over the G lanes of a row (G = 256: of the workgroup), the same bits in all of them.
@@ -45,44 +50,73 @@ struct NormArgs {
   float eps;
 };
 
-template <typename T, int VEC, int NV, int G>
+// How a row's channels are dealt to pieces: all pieces whole; the last piece moved back to end with the row, over channels of the one before it; less than one
+// piece.
+enum Fit { WHOLE, MOVED, FEW };
+
+template <typename T, int NV, int G, Fit FIT>
 struct Row {
-  static constexpr int E = VEC * NV;
-  int c, first;  // channels, and the first of this lane
+  static constexpr int VEC = Piece<T>::VEC, E = VEC * NV;
+  typedef typename Piece<T>::Values Values;
+  int c, first;  // channels, and where this lane's first piece would start
   __device__ Row(int channels) : c(channels), first((threadIdx.x % G) * VEC) {}
-  __device__ bool has(int i) const { return first + i * (G * VEC) < c; }  // (VEC divides c)
+  __device__ bool has(int i) const { return first + i * (G * VEC) < c; }
+  __device__ int place(int i) const { return FIT == MOVED ? min(first + i * (G * VEC), c - VEC) : first + i * (G * VEC); }
+  // whether element k counts in sums: it is a channel of the row, and no other piece's
+  __device__ bool counts(int k) const {
+    const int at = first + (k / VEC) * (G * VEC);
+    return FIT == WHOLE ? at < c : FIT == FEW ? at + k < c : at < c && k % VEC >= at - place(k / VEC);
+  }
+  __device__ int channel(int k) const { return place(k / VEC) + k % VEC; }
   __device__ void load(float (&f)[E], const void* p, int64_t row, int64_t ld) const {
-    const T* at = static_cast<const T*>(p) + row * ld + first;
+    const T* at = static_cast<const T*>(p) + row * ld;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      Piece<T, VEC> q{};
-      if (has(i)) q = *reinterpret_cast<const Piece<T, VEC>*>(at + i * (G * VEC));
+      Values q{};
+      if (FIT == FEW) {
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) f[i * VEC + k] = static_cast<float>(q.v[k]);
+        for (int k = 0; k < VEC - 1; ++k)
+          if (first + k < c) q[k] = at[first + k];
+      } else if (has(i)) {
+        q = __builtin_bit_cast(Values, static_cast<Words4>(*reinterpret_cast<const AnyWords4*>(at + place(i))));
+      }
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) f[i * VEC + k] = static_cast<float>(q[k]);
     }
   }
+  // (a moved piece stores the channels it shares with the one before it as that one does: the same values)
   __device__ void store(const float (&f)[E], void* p, int64_t row, int64_t ld) const {
-    T* at = static_cast<T*>(p) + row * ld + first;
+    T* at = static_cast<T*>(p) + row * ld;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (has(i)) {
-        Piece<T, VEC> q;
+    for (int i = 0; i < NV; ++i) {
+      Values q;
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) q.v[k] = static_cast<T>(f[i * VEC + k]);
-        *reinterpret_cast<Piece<T, VEC>*>(at + i * (G * VEC)) = q;
+      for (int k = 0; k < VEC; ++k) q[k] = static_cast<T>(f[i * VEC + k]);
+      if (FIT == FEW) {
+#pragma unroll
+        for (int k = 0; k < VEC - 1; ++k)
+          if (first + k < c) at[first + k] = q[k];
+      } else if (has(i)) {
+        *reinterpret_cast<AnyWords4*>(at + place(i)) = __builtin_bit_cast(Words4, q);
       }
+    }
   }
   __device__ void load_param(float (&f)[E], const float* p, float none) const {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int k = 0; k < E; ++k) f[k] = p ? 0.f : none;
+    if (!p) return;
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) f[i * VEC + k] = !p ? none : has(i) ? p[first + i * (G * VEC) + k] : 0.f;
+    for (int i = 0; i < NV; ++i)
+      if (has(i))
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+          if (FIT != FEW || first + k < c) f[i * VEC + k] = p[place(i) + k];
   }
 };
 
-template <typename T, int VEC, int NV, int G>
+template <typename T, int NV, int G, Fit FIT>
 __global__ __launch_bounds__(NORM_THREADS) void norm_forward_kernel(const NormArgs a) {
-  using R = Row<T, VEC, NV, G>;
+  using R = Row<T, NV, G, FIT>;
   constexpr int ROWS = NORM_THREADS / G;
   __shared__ float lds[4];
   const R me(a.c);
@@ -102,13 +136,13 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_forward_kernel(const NormAr
     }
     float s = 0.f;
 #pragma unroll
-    for (int k = 0; k < R::E; ++k) s += z[k];
+    for (int k = 0; k < R::E; ++k) s += FIT != MOVED || me.counts(k) ? z[k] : 0.f;  // (places behind the last channel hold zeros)
     const float mean = row_sum<G>(s, lds) / c;
     s = 0.f;
 #pragma unroll
     for (int k = 0; k < R::E; ++k) {
       z[k] -= mean;
-      s += me.has(k / VEC) ? z[k] * z[k] : 0.f;
+      s += me.counts(k) ? z[k] * z[k] : 0.f;
     }
     const float rstd = 1.f / sqrtf(row_sum<G>(s, lds) / c + a.eps);
 #pragma unroll
@@ -121,9 +155,9 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_forward_kernel(const NormAr
   }
 }
 
-template <typename T, int VEC, int NV, int G>
+template <typename T, int NV, int G, Fit FIT>
 __global__ __launch_bounds__(NORM_THREADS) void norm_backward_kernel(const NormArgs a) {
-  using R = Row<T, VEC, NV, G>;
+  using R = Row<T, NV, G, FIT>;
   constexpr int ROWS = NORM_THREADS / G;
   __shared__ float lds[4];
   extern __shared__ float sums[];  // G <= 64: 2 c floats
@@ -139,14 +173,12 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_backward_kernel(const NormA
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int k = 0; k < R::E; ++k) {
-      h[k] = (h[k] - mean) * rstd;
-      // (a lane's places behind the last channel hold dy = 0 and gamma = 0, but an h that is not zero, or not finite)
-      if (!me.has(k / VEC)) h[k] = 0.f;
+      h[k] = me.has(k / R::VEC) ? (h[k] - mean) * rstd : 0.f;  // (behind the last channel dy is zero, but this may be infinite)
       dgamma[k] = fmaf(dy[k], h[k], dgamma[k]);
       dbeta[k] += dy[k];
       dy[k] *= gamma[k];
-      s1 += dy[k];
-      s2 = fmaf(dy[k], h[k], s2);
+      s1 += FIT != MOVED || me.counts(k) ? dy[k] : 0.f;
+      s2 += FIT != MOVED || me.counts(k) ? dy[k] * h[k] : 0.f;
     }
     s1 = row_sum<G>(s1, lds) / c;
     s2 = row_sum<G>(s2, lds) / c;
@@ -176,8 +208,8 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_backward_kernel(const NormA
       if (int(threadIdx.x) / 64 == w && threadIdx.x % 64 < G)
 #pragma unroll
         for (int k = 0; k < R::E; ++k)
-          if (me.has(k / VEC)) {
-            const int at = me.first + (k / VEC) * (G * VEC) + k % VEC;
+          if (me.counts(k)) {
+            const int at = me.channel(k);
             sums[at] = w ? sums[at] + dgamma[k] : dgamma[k];
             sums[a.c + at] = w ? sums[a.c + at] + dbeta[k] : dbeta[k];
           }
@@ -187,26 +219,30 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_backward_kernel(const NormA
   } else {
 #pragma unroll
     for (int k = 0; k < R::E; ++k)
-      if (me.has(k / VEC)) {
-        const int at = me.first + (k / VEC) * (G * VEC) + k % VEC;
+      if (me.counts(k)) {
+        const int at = me.channel(k);
         out[at] = dgamma[k];
         out[a.c + at] = dbeta[k];
       }
   }
 }
 
-// dgamma and dbeta from the workgroups' sums: 32 columns a workgroup, eight shares of the rows added up in LDS.
-__global__ __launch_bounds__(256) void norm_params_kernel(const float* __restrict__ partial, int parts, int c, float* dgamma, float* dbeta) {
-  __shared__ float lds[8][33];
+// dgamma and dbeta from the workgroups' sums: 32 columns a workgroup, 32 shares of the rows added up in LDS.
+__global__ __launch_bounds__(1024) void norm_params_kernel(const float* __restrict__ partial, int parts, int c, float* dgamma, float* dbeta) {
+  __shared__ float lds[32][33];
   const int col = blockIdx.x * 32 + threadIdx.x % 32, share = threadIdx.x / 32;
   float s = 0.f;
-  if (col < 2 * c)
-    for (int p = share; p < parts; p += 8) s += partial[int64_t(p) * (2 * c) + col];
+  if (col < 2 * c) {
+    const float* p = partial + col;
+#pragma unroll 8
+    for (int q = share; q < parts; q += 32) s += p[int64_t(q) * (2 * c)];
+  }
   lds[share][threadIdx.x % 32] = s;
   __syncthreads();
   if (share || col >= 2 * c) return;
+  s = 0.f;
 #pragma unroll
-  for (int q = 1; q < 8; ++q) s += lds[q][threadIdx.x];
+  for (int q = 0; q < 32; ++q) s += lds[q][threadIdx.x];
   float* to = col < c ? dgamma : dbeta;
   if (to) to[col < c ? col : col - c] = s;
 }
@@ -224,15 +260,20 @@ int norm_check_rows(const char* what, const void* p, int64_t ld, int32_t c, int 
   return SPC_OK;
 }
 
-// Calls f(VEC, NV, G) as integral constants for rows of c channels whose pointers and pitches allow pieces of `vec` channels.  Up to 64 pieces
-// one lane holds one; longer rows are held by whole waves with up to 32 channels a lane, and beyond by whole workgroups.
-template <int VEC, typename F>
+// Calls f(NV, G, FIT) as integral constants for rows of c channels.  Up to 64 pieces one lane holds one; longer rows are held by whole waves with up to 32
+// channels a lane, and beyond by whole workgroups.
+template <typename T, typename F>
 void norm_shape(int c, F&& f) {
   using std::integral_constant;
+  constexpr int VEC = Piece<T>::VEC;
   const int pieces = (c + VEC - 1) / VEC;
-  auto go = [&](auto nv, auto g) { f(integral_constant<int, VEC>{}, nv, g); };
+  auto with = [&](auto nv, auto g) {
+    if (c % VEC == 0) f(nv, g, integral_constant<Fit, WHOLE>{});
+    else f(nv, g, integral_constant<Fit, MOVED>{});
+  };
+  if (c < VEC) return f(integral_constant<int, 1>{}, integral_constant<int, 4>{}, integral_constant<Fit, FEW>{});
 #define SPC_NORM_CASE(NV, G) \
-  if (NV * VEC <= 32 && pieces <= NV * G) return go(integral_constant<int, NV * VEC <= 32 ? NV : 1>{}, integral_constant<int, G>{})
+  if (NV * VEC <= 32 && pieces <= NV * G) return with(integral_constant<int, NV * VEC <= 32 ? NV : 1>{}, integral_constant<int, G>{})
   SPC_NORM_CASE(1, 4);
   SPC_NORM_CASE(1, 8);
   SPC_NORM_CASE(1, 16);
@@ -241,46 +282,38 @@ void norm_shape(int c, F&& f) {
   SPC_NORM_CASE(2, 64);
   SPC_NORM_CASE(4, 64);
   SPC_NORM_CASE(8, 64);
+  SPC_NORM_CASE(2, 256);
   SPC_NORM_CASE(4, 256);
   SPC_NORM_CASE(8, 256);
-  SPC_NORM_CASE(16, 256);
-  SPC_NORM_CASE(32, 256);
 #undef SPC_NORM_CASE
 }
-// The widest pieces that divide the channels, every pitch and every address.
-template <typename T, typename F>
-void norm_dispatch(const NormArgs& a, F&& f) {
-  uintptr_t all = static_cast<uintptr_t>(a.c) * sizeof(T);
-  const std::pair<const void*, int64_t> rows[] = {{a.x, a.ld_x}, {a.r, a.ld_r}, {a.dy, a.ld_dy}, {a.e, a.ld_e}, {a.y, a.ld_y}, {a.z, a.ld_z}};
-  for (const auto& r : rows)
-    if (r.first) all |= reinterpret_cast<uintptr_t>(r.first) | static_cast<uintptr_t>(r.second) * sizeof(T);
-  if (all % 16 == 0) return norm_shape<16 / sizeof(T)>(a.c, f);
-  if constexpr (sizeof(T) == 2) {
-    if (all % 4 == 0) return norm_shape<2>(a.c, f);
-  }
-  norm_shape<1>(a.c, f);
-}
 
+// The grid: workgroups that 256 CUs hold at once, and no more than there are rows for.  The forward pass is short of registers nowhere (120 k x 256 fp16: 1024
+// workgroups 43.3 us, 2048 42.6; 8000 x 8192 bf16: 51.8, 46.2).  The backward pass holds 8, 16 or 32 channels a lane several times over, and each workgroup stores
+// sums: four to a CU, three, two (240 k x 256 bf16: 512 in all 125 us, 1024 97; 30 k x 1024: 512 46, 1024 58), of four turns each at least.
+int norm_grid(int32_t dtype, int c, int64_t n, bool backward) {
+  int64_t rows = 1, most = 2048;
+  by_dtype(dtype, [&](auto t) {
+    norm_shape<decltype(t)>(c, [&](auto nv, auto g, auto) {
+      rows = NORM_THREADS / decltype(g)::value;
+      constexpr int channels = decltype(nv)::value * Piece<decltype(t)>::VEC;
+      if (backward) rows *= 4, most = channels <= 8 ? 1024 : channels <= 16 ? 768 : 512;
+    });
+  });
+  return static_cast<int>(std::min(most, (n + rows - 1) / rows));
+}
 template <typename T>
-void norm_forward(const NormArgs& a, hipStream_t s) {
-  norm_dispatch<T>(a, [&](auto vec, auto nv, auto g) {
-    constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, G = decltype(g)::value;
-    const int64_t wgs = (a.n + NORM_THREADS / G - 1) / (NORM_THREADS / G);
-    hipLaunchKernelGGL((norm_forward_kernel<T, VEC, NV, G>), dim3(std::min<int64_t>(wgs, 4096)), dim3(NORM_THREADS), 0, s, a);
+void norm_forward(const NormArgs& a, int wgs, hipStream_t s) {
+  norm_shape<T>(a.c, [&](auto nv, auto g, auto fit) {
+    hipLaunchKernelGGL((norm_forward_kernel<T, decltype(nv)::value, decltype(g)::value, decltype(fit)::value>), dim3(wgs), dim3(NORM_THREADS), 0, s, a);
   });
 }
 template <typename T>
 void norm_backward(const NormArgs& a, int wgs, hipStream_t s) {
-  norm_dispatch<T>(a, [&](auto vec, auto nv, auto g) {
-    constexpr int VEC = decltype(vec)::value, NV = decltype(nv)::value, G = decltype(g)::value;
-    hipLaunchKernelGGL((norm_backward_kernel<T, VEC, NV, G>), dim3(wgs), dim3(NORM_THREADS), G <= 64 ? 8 * a.c : 0, s, a);
+  norm_shape<T>(a.c, [&](auto nv, auto g, auto fit) {
+    constexpr int G = decltype(g)::value;
+    hipLaunchKernelGGL((norm_backward_kernel<T, decltype(nv)::value, G, decltype(fit)::value>), dim3(wgs), dim3(NORM_THREADS), G <= 64 ? 8 * a.c : 0, s, a);
   });
-}
-template <typename F>
-void by_dtype(int32_t dtype, F&& f) {
-  if (dtype == SPC_DTYPE_F16) f(_Float16{});
-  else if (dtype == SPC_DTYPE_BF16) f(__bf16{});
-  else f(0.f);
 }
 
 }  // namespace
@@ -303,7 +336,8 @@ extern "C" int spc_layer_norm_forward(const void* x, int64_t ld_x, const void* r
   NormArgs a{};
   a.x = x, a.ld_x = ld_x, a.r = residual, a.ld_r = ld_r, a.gamma = gamma, a.beta = beta, a.eps = eps;
   a.y = y, a.ld_y = ld_y, a.z = sum, a.ld_z = ld_s, a.mean = mean, a.rstd = rstd, a.n = n, a.c = c;
-  by_dtype(dtype, [&](auto t) { norm_forward<decltype(t)>(a, static_cast<hipStream_t>(stream)); });
+  const int wgs = norm_grid(dtype, c, n, false);
+  by_dtype(dtype, [&](auto t) { norm_forward<decltype(t)>(a, wgs, static_cast<hipStream_t>(stream)); });
   SPC_HIP_CHECK(hipGetLastError());
   return SPC_OK;
 }
@@ -322,19 +356,17 @@ extern "C" int spc_layer_norm_backward(const void* dy, int64_t ld_dy, const void
   const StreamId s(static_cast<hipStream_t>(stream));
   const StreamWorkNote note{s};
   const bool params = dgamma || dbeta;
-  // Workgroups: four to a CU, and each at least 64 rows of 16 lanes or as many values of others, so that the sums stored are a small part of what is read.
-  const int64_t rows = std::max<int64_t>(1, 8192 / c) * 4;
-  const int wgs = static_cast<int>(std::min<int64_t>(1024, (n + rows - 1) / rows));
   NormArgs a{};
   a.dy = dy, a.ld_dy = ld_dy, a.x = x, a.ld_x = ld_x, a.mean_in = mean, a.rstd_in = rstd, a.gamma = gamma, a.e = dsum, a.ld_e = ld_ds;
   a.y = dx, a.ld_y = ld_dx, a.n = n, a.c = c;
+  const int wgs = norm_grid(dtype, c, n, true);
   if (params && n) {
     a.partial = static_cast<float*>(pool_alloc(size_t(wgs) * 2 * c * sizeof(float), s));
     if (!a.partial) return SPC_ERR_NOMEM;
   }
   if (n) by_dtype(dtype, [&](auto t) { norm_backward<decltype(t)>(a, wgs, s); });
   if (params)
-    hipLaunchKernelGGL(norm_params_kernel, dim3((2 * c + 31) / 32), dim3(256), 0, s, a.partial, n ? wgs : 0, c, dgamma, dbeta);
+    hipLaunchKernelGGL(norm_params_kernel, dim3((2 * c + 31) / 32), dim3(1024), 0, s, a.partial, n ? wgs : 0, c, dgamma, dbeta);
   pool_free(a.partial, s);
   SPC_HIP_CHECK(hipGetLastError());
   return SPC_OK;
