@@ -41,7 +41,6 @@ struct Job {
   States first, last, between;  // of a scene, after it, after every segment but the last
   int dy, dz;
   bool reverse, out_f32;
-  bool vec_x, vec_y, vec_z, vec_out;  // whether rows can be read in pieces of 16 bytes, written in pieces of four channels
 };
 struct ScanArgs {
   Job job[ATTN_MAX_JOBS];
@@ -82,15 +81,17 @@ __device__ inline float decay_power(float g, int n) { return n > 0 ? __builtin_a
 
 // Up to four consecutive channels (`left` of them exist).
 template <typename T>
-__device__ inline void store4(T* p, float __attribute__((ext_vector_type(4))) v, bool pieces, int left) {
-  struct alignas(4 * sizeof(T)) Piece { T v[4]; };
-  if (left >= 4 && pieces) {
-    *reinterpret_cast<Piece*>(p) = Piece{{static_cast<T>(v[0]), static_cast<T>(v[1]), static_cast<T>(v[2]), static_cast<T>(v[3])}};
+__device__ inline void store4(T* p, float __attribute__((ext_vector_type(4))) v, int left) {
+  typedef T Values __attribute__((ext_vector_type(4)));
+  const Values q = __builtin_convertvector(v, Values);
+  if (left >= 4) {
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<AnyWords2*>(p) = __builtin_bit_cast(Words2, q);
+    else *reinterpret_cast<AnyWords4*>(p) = __builtin_bit_cast(Words4, q);
     return;
   }
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
-    if (r < left) p[r] = static_cast<T>(v[r]);
+  for (int r = 0; r < 3; ++r)
+    if (r < left) p[r] = q[r];
 }
 
 // ---------------------------------------------------------------- chunks on the matrix cores
@@ -219,8 +220,8 @@ __device__ inline float over_quads(float v) {  // maximum over the four lanes of
 __device__ inline float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
 
 // A chunk's rows of one tensor on their way from memory to LDS.  A segment's last chunk, where it is not full, lies in the tile's last rows; the rows in
-// front of it, and channels behind the head's last, are zeros.  Rows that can be read in pieces of 16 bytes are in registers while the chunk before is worked
-// on; others are read channel by channel when they are due.
+// front of it, and channels behind the head's last, are zeros.  Heads of whole pieces of 16 bytes, at any address, are in registers while the chunk before is
+// worked on; others are read channel by channel when they are due.
 template <typename T, int D>
 struct TileLoad {
   static constexpr int VE = 16 / sizeof(T), PER_ROW = D / VE, STEP = 256 / PER_ROW, N = CHUNK / STEP;
@@ -230,9 +231,9 @@ struct TileLoad {
   int64_t row;      // the next row of the scan
   int width;        // channels of these columns that there are
   bool pieces;
-  __device__ void start(const Rows& t, bool in_pieces, int first_channel, int channels, const Segment& s, bool reverse, int seg_first, int h) {
+  __device__ void start(const Rows& t, int first_channel, int channels, const Segment& s, bool reverse, int seg_first, int h) {
     width = min(channels - first_channel, D);
-    pieces = in_pieces;
+    pieces = channels % VE == 0;
     row = reverse ? -t.row : t.row;
     origin = static_cast<const T*>(t.p) + (h / t.group) * t.head + s.row(reverse, seg_first) * t.row + first_channel;
   }
@@ -243,13 +244,13 @@ struct TileLoad {
     const T* at = origin + (i * row + c);
     if (!shift && width == D) {
 #pragma unroll
-      for (int n = 0; n < N; ++n, at += STEP * row) q[n] = *reinterpret_cast<const intx4*>(at);
+      for (int n = 0; n < N; ++n, at += STEP * row) q[n] = *reinterpret_cast<const AnyWords4*>(at);
       return;
     }
 #pragma unroll
     for (int n = 0; n < N; ++n, at += STEP * row) {
       q[n] = intx4{0, 0, 0, 0};
-      if (i + n * STEP >= shift && c < width) q[n] = *reinterpret_cast<const intx4*>(at);
+      if (i + n * STEP >= shift && c < width) q[n] = *reinterpret_cast<const AnyWords4*>(at);
     }
   }
   __device__ void store(T* tile, int shift) {
@@ -320,9 +321,9 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
 
   TileLoad<T, DY> x, y;
   TileLoad<T, DZ> z;
-  if (OUT) x.start(j.x, j.vec_x, 0, j.dy, s, j.reverse, seg_first, h);
-  y.start(j.y, j.vec_y, 0, j.dy, s, j.reverse, seg_first, h);
-  z.start(j.z, j.vec_z, col0, j.dz, s, j.reverse, seg_first, h);
+  if (OUT) x.start(j.x, 0, j.dy, s, j.reverse, seg_first, h);
+  y.start(j.y, 0, j.dy, s, j.reverse, seg_first, h);
+  z.start(j.z, col0, j.dz, s, j.reverse, seg_first, h);
   auto fetch = [&](int rows) {
     if (OUT) x.load(rows);
     y.load(rows);
@@ -357,12 +358,12 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
     if (r + 1 < IT) w_tile[r] = uniform(decay_power(g, 16 * r + 1));
   }
   const float f_full = inter * decay_power(g, 16 * it + lc + 1), whole_full = uniform(decay_power(g, CHUNK));
-  const bool out_f32 = j.out_f32, out_pieces = j.vec_out;
+  const bool out_f32 = j.out_f32;
   const int es = out_f32 ? 4 : sizeof(T);
   const int64_t out_row = (j.reverse ? -j.out.row : j.out.row) * es;
   char* out = nullptr;  // row 16 it + lc of the chunk, channel lr of these columns
   if (OUT) out = static_cast<char*>(j.out.p) + (j.out.at(s.row(j.reverse, seg_first), h) + col0 + lr) * es + (16 * it + lc) * out_row;
-  const bool out_whole = out_pieces && !out_f32 && dz >= DZ;
+  const bool out_whole = !out_f32 && dz >= DZ;
   const bool keep = a.keep;
   Along<T, DY> along(lane);
   Down<T, DY> down_y(lane);
@@ -478,8 +479,8 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
         char* at = out - shift * out_row;
         auto put = [&](int ct, floatx4 v) {
           if (i < shift) return;
-          if (out_f32) store4(reinterpret_cast<float*>(at) + 16 * ct, v, out_pieces, dz - 16 * ct - lr);
-          else store4(reinterpret_cast<T*>(at) + 16 * ct, v, out_pieces, dz - 16 * ct - lr);
+          if (out_f32) store4(reinterpret_cast<float*>(at) + 16 * ct, v, dz - 16 * ct - lr);
+          else store4(reinterpret_cast<T*>(at) + 16 * ct, v, dz - 16 * ct - lr);
         };
         if (__ballot(nan)) {
           // Zero times infinity is NaN: where a value is not finite, the zeros of P above the diagonal have brought it to earlier rows.  Outputs that are not
@@ -513,7 +514,7 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
           }
         } else if (out_whole && !shift) {
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) store4(reinterpret_cast<T*>(at) + 16 * ct, o[ct], true, 4);
+          for (int ct = 0; ct < CT; ++ct) store4(reinterpret_cast<T*>(at) + 16 * ct, o[ct], 4);
         } else {
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) put(ct, o[ct]);
@@ -719,11 +720,6 @@ int segment_rows(const spc_attn_desc* d, int dy, int dz) {
   return static_cast<int>(std::max<int64_t>(64, (want + 63) / 64 * 64));
 }
 
-bool in_pieces(const Rows& t, int width, int heads, int bytes, int es) {
-  const uintptr_t all = reinterpret_cast<uintptr_t>(t.p) | uintptr_t(t.row) * es | (heads > t.group ? uintptr_t(t.head) * es : 0) | uintptr_t(width) * es;
-  return all % bytes == 0;
-}
-
 template <typename T, int DY, int DZ>
 int launch_scan(ScanArgs& a, int n_sums, hipStream_t s) {
   int dz = 0;
@@ -752,16 +748,7 @@ int run_scan(ScanArgs& a, int n_sums, int32_t dtype, hipStream_t s) {
   int dy = 0, dz = 0, rc = SPC_OK;
   for (int q = 0; q < a.n_jobs; ++q) dy = std::max(dy, a.job[q].dy), dz = std::max(dz, a.job[q].dz);
   by_shape(dtype, dy, dz, [&](auto t, auto y, auto z) {
-    using T = decltype(t);
-    for (int q = 0; q < a.n_jobs; ++q) {
-      Job& j = a.job[q];
-      j.vec_x = in_pieces(j.x, j.dy, a.heads, 16, sizeof(T));
-      j.vec_y = in_pieces(j.y, j.dy, a.heads, 16, sizeof(T));
-      j.vec_z = in_pieces(j.z, j.dz, a.heads, 16, sizeof(T));
-      const int es = j.out_f32 ? 4 : sizeof(T);
-      j.vec_out = in_pieces(j.out, j.dz, a.heads, 4 * es, es);
-    }
-    rc = launch_scan<T, decltype(y)::value, decltype(z)::value>(a, n_sums, s);
+    rc = launch_scan<decltype(t), decltype(y)::value, decltype(z)::value>(a, n_sums, s);
   });
   SPC_RETURN_IF(rc);
   SPC_HIP_CHECK(hipGetLastError());
