@@ -104,13 +104,13 @@ typedef int intx4 __attribute__((ext_vector_type(4)));
 
 constexpr int CHUNK = 64;  // rows whose products with each other are taken directly
 
-// Tiles in LDS have rows of D channels in pieces of 16 bytes, whose order is another in every row: piece q of row r lies at q ^ f(r).  Lanes that read the same
-// piece of 16 rows, or two pieces of eight rows, then meet all 64 banks once, without padding.
+// Tiles in LDS have rows of D channels in pieces of 16 bytes, whose order is another in every row: piece q of row r lies at q ^ turn(r), which spreads lanes that
+// read pieces of different rows over the banks without padding.  Chosen by the conflicts counted for the four kinds of access below, of seven such orders (extra cycles a
+// wave, D = 64 of 16 bits: rows read along 0, written 4, tile stored 0, columns 0; 32: 0, 4, 0, 0; 128: 0, 4, 0, 2; fp32 64 and 128: none; 32: 4, 0, 0, 0).
 template <typename T, int D>
 struct Tile {
   static constexpr int VE = 16 / sizeof(T), PIECES = D / VE;
-  static constexpr int SAME = PIECES >= 16 ? 0 : PIECES == 8 ? 1 : 2;  // log2 of the rows that meet different banks as they are
-  __device__ static inline int turn(int r) { return ((r >> SAME) & (7 >> SAME)) * 2 + ((r >> 3) & 1); }
+  __device__ static inline int turn(int r) { return PIECES == 4 ? (r >> 1) & 3 : r & (PIECES < 16 ? PIECES - 1 : 15); }  // (of the row modulo 16)
   __device__ static inline int at(int r, int c) { return r * D + ((c / VE ^ turn(r)) * VE + c % VE); }
 };
 
