@@ -10,13 +10,11 @@
 // A scene is cut into segments that different workgroups scan at once: a first launch makes every segment's own sum of y z^T, a second
 // turns them into the state in front of every segment, a third scans the segments.  Scenes of one segment take the third alone.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "rows.h"
 
-#ifndef SPC_ROUNDS
-#define SPC_ROUNDS 1
-#endif
 namespace spc {
 namespace {
 
@@ -589,7 +587,7 @@ __global__ __launch_bounds__(256) void scan_states_kernel(const ScanArgs a) {
   const float whole = decay_power(l, a.seg_rows);
   const int64_t step = a.heads * j.between.each;
   float* p = j.between.of(id, a.heads, h) + r * j.between.r + c * j.between.c;
-  constexpr int AHEAD = 16;  // (the loads of a chain's links do not depend on each other)
+  constexpr int AHEAD = 32;  // (the loads of a chain's links do not depend on each other)
   for (int m = 0; m + 1 < s.n; m += AHEAD) {
     float v[AHEAD];
 #pragma unroll
@@ -604,17 +602,27 @@ __global__ __launch_bounds__(256) void scan_states_kernel(const ScanArgs a) {
   }
 }
 
-// Gradients of keys and values that `group` heads share.
+// Gradients of keys and values that `group` heads share: sums over the heads, of [row][head][channel] each.
+struct HeadSums {
+  const float* part;
+  Rows out;
+  int d;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void sum_heads_kernel(const float* __restrict__ part, Rows out, int64_t n_rows, int kv_heads, int group, int d) {
-  const int64_t i = blockIdx.x * int64_t(256) + threadIdx.x;
-  if (i >= n_rows * kv_heads * d) return;
-  const int c = static_cast<int>(i % d), h = static_cast<int>(i / d % kv_heads);
-  const int64_t row = i / d / kv_heads;
-  const float* p = part + ((row * kv_heads + h) * group) * d + c;
+__global__ __launch_bounds__(256) void sum_heads_kernel(HeadSums k, HeadSums v, int64_t n_rows, int kv_heads, int group) {
+  int64_t i = blockIdx.x * int64_t(256) + threadIdx.x;
+  const int64_t nk = n_rows * kv_heads * k.d;
+  const bool second = i >= nk;
+  const HeadSums a = second ? v : k;
+  if (second) i -= nk;
+  if (i >= n_rows * kv_heads * a.d) return;
+  const int c = static_cast<int>(i % a.d);
+  const int64_t rh = i / a.d, row = rh / kv_heads;
+  const float* p = a.part + rh * group * a.d + c;
   float s = 0.f;
-  for (int g = 0; g < group; ++g) s += p[int64_t(g) * d];
-  static_cast<T*>(out.p)[row * out.row + h * out.head + c] = static_cast<T>(s);
+#pragma unroll 4
+  for (int g = 0; g < group; ++g) s += p[int64_t(g) * a.d];
+  static_cast<T*>(a.out.p)[row * a.out.row + (rh - row * kv_heads) * a.out.head + c] = static_cast<T>(s);
 }
 
 template <typename T>
@@ -710,14 +718,18 @@ void by_shape(int32_t dtype, int dy, int dz, F&& f) {
   });
 }
 
-// Rows of a segment: multiples of 64, as few as give the workgroups that 256 CUs hold at once.
+// Rows of a segment, a multiple of 64: as few as give the workgroups that 256 CUs hold at once (twice as many workgroups: 120 k rows, 8 heads of 64, bf16 203 us, not
+// 196), but not so few that the chain of a scene's segments takes longer than a segment, which balances at some 64 sqrt(rows / 1200) (us, segments of 64 / 128 / 256
+// rows: 2118 rows, 4 heads of 16, fp32 18.0 / 20.6 / 29.2; 6011 rows, 8 heads of 64, bf16 33.4 / 29.5 / 29.0; 12 k rows, 4 heads of 32 27.6 / 23.5 / 24.6).
 int segment_rows(const spc_attn_desc* d, int dy, int dz) {
   int64_t at_once = 256;
   by_shape(d->dtype, dy, dz, [&](auto t, auto y, auto z) {
-    at_once = SPC_ROUNDS * 256 * scan_waves<decltype(t), decltype(y)::value, decltype(z)::value>() / ((dz + decltype(z)::value - 1) / decltype(z)::value);
+    constexpr int width = decltype(z)::value;
+    at_once = 256 * scan_waves<decltype(t), decltype(y)::value, width>() / ((dz + width - 1) / width);
   });
-  const int64_t want = (d->n_rows * d->heads + at_once - 1) / at_once;
-  return static_cast<int>(std::max<int64_t>(64, (want + 63) / 64 * 64));
+  const int64_t fill = (d->n_rows * d->heads + at_once - 1) / at_once;
+  const double chain = std::sqrt(double(d->n_rows) / d->n_scenes / 1200);
+  return static_cast<int>(64 * std::max<int64_t>({1, (fill + 63) / 64, std::llround(chain)}));
 }
 
 template <typename T, int DY, int DZ>
@@ -858,9 +870,9 @@ extern "C" int spc_linear_attention_backward(const spc_attn_desc* d, const spc_a
   if (rc == SPC_OK && parts) {
     by_dtype(d->dtype, [&](auto t) {
       using T = decltype(t);
-      const int64_t nk = int64_t(a.n_rows) * d->kv_heads * d->dk, nv = int64_t(a.n_rows) * d->kv_heads * d->dv;
-      hipLaunchKernelGGL(sum_heads_kernel<T>, dim3((nk + 255) / 256), dim3(256), 0, s, part_k, rows_of(dk, 1), a.n_rows, d->kv_heads, group, d->dk);
-      hipLaunchKernelGGL(sum_heads_kernel<T>, dim3((nv + 255) / 256), dim3(256), 0, s, part_v, rows_of(dv, 1), a.n_rows, d->kv_heads, group, d->dv);
+      const int64_t n = int64_t(a.n_rows) * d->kv_heads * (d->dk + d->dv);
+      hipLaunchKernelGGL(sum_heads_kernel<T>, dim3((n + 255) / 256), dim3(256), 0, s, HeadSums{part_k, rows_of(dk, 1), d->dk},
+                         HeadSums{part_v, rows_of(dv, 1), d->dv}, a.n_rows, d->kv_heads, group);
     });
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) rc = set_error(SPC_ERR_HIP, "launch failed: %s", hipGetErrorString(err));
