@@ -625,37 +625,60 @@ __global__ __launch_bounds__(256) void sum_heads_kernel(HeadSums k, HeadSums v, 
   static_cast<T*>(a.out.p)[row * a.out.row + (rh - row * kv_heads) * a.out.head + c] = static_cast<T>(s);
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void attention_step_kernel(Rows q, Rows k, Rows v, Rows out, float* state, const float* log_decay, int heads,
-                                                             int dk, int dv, float scale) {
-  __shared__ float qs[ATTN_MAX_D], ks[ATTN_MAX_D], part[256];
-  const int h = blockIdx.x % heads, t = threadIdx.x;
+// One row more: a workgroup updates one head's state of one stream, S <- l S + k v^T, and adds up its columns times q on the way.  Every value of the state is read and
+// written once, in pieces of VEC columns (4; 1 where the columns are no multiple of it) whose loads are all under way before the first is used; the bytes bound it
+// (2048 streams of 8 heads of 64 x 64: 546 MB).  Neighbouring lanes have neighbouring pieces of a row, 2^log_q places of which hold one.
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void attention_step_kernel(Rows q, Rows k, Rows v, Rows out, float* state, const float* log_decay, int heads, int dk, int dv,
+                                                             float scale, int log_q) {
+  typedef float Values __attribute__((ext_vector_type(VEC), aligned(4), may_alias));
+  constexpr int AHEAD = 8;
+  __shared__ float qs[ATTN_MAX_D], ks[ATTN_MAX_D], part[256 * VEC];
+  const int h = blockIdx.x % heads, t = threadIdx.x, c = (t & ((1 << log_q) - 1)) * VEC, step = blockDim.x >> log_q;
   const int64_t row = blockIdx.x / heads;
-  if (t < dk) {
-    qs[t] = scale * static_cast<float>(static_cast<const T*>(q.p)[q.at(row, h) + t]);
-    ks[t] = static_cast<float>(static_cast<const T*>(k.p)[k.at(row, h) + t]);
+  float* S = state + int64_t(blockIdx.x) * dk * dv + c;
+  Values s[AHEAD];
+  auto load = [&](int r0) {
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a)
+      if (r0 + a * step < dk && c < dv) s[a] = *reinterpret_cast<const Values*>(S + (r0 + a * step) * dv);
+  };
+  load(t >> log_q);
+  for (int i = t; i < dk; i += blockDim.x) {
+    qs[i] = scale * static_cast<float>(static_cast<const T*>(q.p)[q.at(row, h) + i]);
+    ks[i] = static_cast<float>(static_cast<const T*>(k.p)[k.at(row, h) + i]);
   }
-  __syncthreads();
+  Values vc, o;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    vc[e] = c < dv ? static_cast<float>(static_cast<const T*>(v.p)[v.at(row, h) + c + e]) : 0.f;
+    o[e] = 0.f;
+  }
   const float l = expf(log_decay[h]);
-  float* S = state + int64_t(blockIdx.x) * dk * dv;
-  for (int c0 = 0; c0 < dv; c0 += 32) {
-    const int c = c0 + t % 32;
-    float o = 0.f;
-    if (c < dv) {
-      const float vc = static_cast<float>(static_cast<const T*>(v.p)[v.at(row, h) + c]);
-      for (int r = t / 32; r < dk; r += 8) {
-        const float s = l * S[r * dv + c] + ks[r] * vc;
-        S[r * dv + c] = s;
-        o = fmaf(qs[r], s, o);
+  __syncthreads();
+  for (int r0 = t >> log_q; r0 < dk; r0 += AHEAD * step) {
+    if (r0 >= AHEAD * step) load(r0);
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const int r = r0 + a * step;
+      if (r < dk && c < dv) {
+        const float kr = ks[r], qr = qs[r];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          s[a][e] = fmaf(l, s[a][e], kr * vc[e]);
+          o[e] = fmaf(qr, s[a][e], o[e]);
+        }
+        *reinterpret_cast<Values*>(S + r * dv) = s[a];
       }
     }
-    part[t] = o;
-    __syncthreads();
-    if (t < 32 && c < dv) {
-      for (int g = 1; g < 8; ++g) o += part[t + 32 * g];
-      static_cast<T*>(out.p)[out.at(row, h) + c] = static_cast<T>(o);
-    }
-    __syncthreads();
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) part[t * VEC + e] = o[e];
+  __syncthreads();
+  for (int i = t; i < dv; i += blockDim.x) {
+    float sum = 0.f;
+    for (int g = 0; g < step; ++g) sum += part[(g * VEC << log_q) + i];
+    static_cast<T*>(out.p)[out.at(row, h) + i] = static_cast<T>(sum);
   }
 }
 
@@ -894,9 +917,18 @@ extern "C" int spc_linear_attention_step(const spc_attn_desc* d, const spc_attn_
   SPC_RETURN_IF(check_rows("v", v, d, d->kv_heads, d->dv, false));
   SPC_RETURN_IF(check_rows("out", out, d, d->heads, d->dv, true));
   const int group = d->heads / d->kv_heads;
+  const int vec = d->dv % 4 ? 1 : 4;
+  int log_q = 0, threads = 64;
+  while ((vec << log_q) < d->dv) ++log_q;
+  while (threads < 256 && threads * 4 * vec < d->dk * d->dv) threads *= 2;  // (some four pieces a lane)
   by_dtype(d->dtype, [&](auto t) {
-    hipLaunchKernelGGL(attention_step_kernel<decltype(t)>, dim3(d->n_rows * d->heads), dim3(256), 0, static_cast<hipStream_t>(stream), rows_of(q, 1),
-                       rows_of(k, group), rows_of(v, group), rows_of(out, 1), state, log_decay, d->heads, d->dk, d->dv, d->scale);
+    using T = decltype(t);
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(d->n_rows * d->heads), dim3(std::max(threads, 1 << log_q)), 0, static_cast<hipStream_t>(stream), rows_of(q, 1), rows_of(k, group),
+                         rows_of(v, group), rows_of(out, 1), state, log_decay, d->heads, d->dk, d->dv, d->scale, log_q);
+    };
+    if (vec == 4) go(attention_step_kernel<T, 4>);
+    else go(attention_step_kernel<T, 1>);
   });
   SPC_HIP_CHECK(hipGetLastError());
   return SPC_OK;
