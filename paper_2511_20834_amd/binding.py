@@ -451,10 +451,10 @@ def spc_layer_norm_forward(x: torch.Tensor, gamma: torch.Tensor | None = None, b
     None without a residual, mean and rstd [n] fp32 are None without want_stats."""
     assert x.is_cuda and x.dim() == 2 and x.dtype in _TORCH_DTYPE
     (n, c), dev = x.shape, x.device
-    y = torch.empty((n, c), dtype=x.dtype, device=dev) if out is None else out
+    y = torch.empty(n, c, dtype=x.dtype, device=dev) if out is None else out
     total = None
     if residual is not None:
-        total = torch.empty((n, c), dtype=x.dtype, device=dev) if sum_out is None else sum_out
+        total = torch.empty(n, c, dtype=x.dtype, device=dev) if sum_out is None else sum_out
     else:
         assert sum_out is None
     mean = rstd = None
@@ -477,7 +477,7 @@ def spc_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
     the norm.  Returns (dx, dgamma, dbeta), the last two [c] fp32, or None without want_params."""
     assert x.is_cuda and x.dim() == 2 and x.dtype in _TORCH_DTYPE
     (n, c), dev = x.shape, x.device
-    dx = torch.empty((n, c), dtype=x.dtype, device=dev) if out is None else out
+    dx = torch.empty(n, c, dtype=x.dtype, device=dev) if out is None else out
     dgamma = dbeta = None
     if want_params:
         dgamma, dbeta = torch.empty(c, dtype=torch.float32, device=dev), torch.empty(c, dtype=torch.float32, device=dev)
@@ -520,7 +520,7 @@ def spc_linear_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tens
     n, heads, dev = d.n_rows, d.heads, q.device
     shape = (d.n_scenes, heads, d.dk, d.dv)
     if out is None:
-        out = torch.empty((n, heads, d.dv), dtype=q.dtype, device=dev)
+        out = torch.empty(n, heads, d.dv, dtype=q.dtype, device=dev)
     if state_out is None and want_state:
         state_out = torch.empty(shape, dtype=torch.float32, device=dev)
     ro = _heads(out, n, heads, d.dv, q)
@@ -540,7 +540,7 @@ def spc_linear_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.
     n, heads, kv, dev = d.n_rows, d.heads, d.kv_heads, q.device
     shape = (d.n_scenes, heads, d.dk, d.dv)
     if out is None:
-        out = tuple(torch.empty(s, dtype=q.dtype, device=dev) for s in ((n, heads, d.dk), (n, kv, d.dk), (n, kv, d.dv)))
+        out = tuple(torch.empty(*s, dtype=q.dtype, device=dev) for s in ((n, heads, d.dk), (n, kv, d.dk), (n, kv, d.dv)))
     dinitial = torch.empty(shape, dtype=torch.float32, device=dev) if want_dinitial else None
     rc = lib().spc_linear_attention_backward(d, _heads(dout, n, heads, d.dv, q), rq, rk, rv, g, at, _f32(initial_state, shape, dev),
                                              _f32(dstate, shape, dev), _heads(out[0], n, heads, d.dk, q), _heads(out[1], n, kv, d.dk, q),
@@ -556,7 +556,7 @@ def spc_linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     """One more row for every stream: q [streams, heads, dk] and so on; state [streams, heads, dk, dv] fp32 is updated in place."""
     d, rq, rk, rv, g, _ = _attention(q, k, v, log_decay, None, scale)
     if out is None:
-        out = torch.empty((d.n_rows, d.heads, d.dv), dtype=q.dtype, device=q.device)
+        out = torch.empty(d.n_rows, d.heads, d.dv, dtype=q.dtype, device=q.device)
     rc = lib().spc_linear_attention_step(d, rq, rk, rv, g, _f32(state, (d.n_rows, d.heads, d.dk, d.dv), q.device),
                                          _heads(out, d.n_rows, d.heads, d.dv, q), current_raw_stream() if stream is None else _stream(stream))
     if rc:

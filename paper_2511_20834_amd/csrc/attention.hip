@@ -272,7 +272,7 @@ struct TileLoad {
 
 template <typename T, int DY, int DZ, bool OUT>
 constexpr size_t scan_lds() {
-  return sizeof(T) * (CHUNK * (DY + DZ) + (OUT ? CHUNK * DY + (sizeof(T) == 2 ? 2 : 1) * DZ * DY : 0)) + (OUT ? sizeof(float) * DZ : 0);
+  return sizeof(T) * (CHUNK * (DY + DZ) + (OUT ? CHUNK * DY + (sizeof(T) == 2 ? 2 : 1) * DZ * DY : 0)) + (OUT && std::is_same_v<T, _Float16> ? sizeof(float) * DZ : 0);
 }
 
 // Workgroups (a wave on every SIMD) that a CU holds, by registers and LDS.
@@ -472,7 +472,6 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
           if constexpr (HALF) o[ct] += v * p_up;
           else o[ct] = v;
           nan |= __builtin_isunordered(o[ct][0], o[ct][1]) | __builtin_isunordered(o[ct][2], o[ct][3]);
-          __builtin_amdgcn_sched_barrier(0);
         }
         char* at = out - shift * out_row;
         auto put = [&](int ct, floatx4 v) {
