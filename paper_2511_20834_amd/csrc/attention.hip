@@ -458,7 +458,7 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
           o[ct] *= f;
           __builtin_amdgcn_sched_barrier(0);
         }
-        bool nan = false;
+        bool some = false;  // whether an output is NaN
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
           floatx4 v = {0.f, 0.f, 0.f, 0.f};
@@ -471,7 +471,7 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
           }
           if constexpr (HALF) o[ct] += v * p_up;
           else o[ct] = v;
-          nan |= __builtin_isunordered(o[ct][0], o[ct][1]) | __builtin_isunordered(o[ct][2], o[ct][3]);
+          some |= __builtin_isunordered(o[ct][0], o[ct][1]) | __builtin_isunordered(o[ct][2], o[ct][3]);
         }
         char* at = out - shift * out_row;
         auto put = [&](int ct, floatx4 v) {
@@ -479,42 +479,46 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
           if (out_f32) store4(reinterpret_cast<float*>(at) + 16 * ct, v, dz - 16 * ct - lr);
           else store4(reinterpret_cast<T*>(at) + 16 * ct, v, dz - 16 * ct - lr);
         };
-        if (__ballot(nan)) {
-          // Zero times infinity is NaN: where a value is not finite, the zeros of P above the diagonal have brought it to earlier rows.  Outputs that are not
-          // numbers are computed from their own pairs alone.
-#pragma unroll 1
-          for (int ct = 0; ct < CT; ++ct) {
-            floatx4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-            for (int d = 0; d < j.dy; ++d) {
-              const float xd = f * static_cast<float>(xs[Tile<T, DY>::at(i, d)]);
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const int c = 16 * ct + lr + r;
-                float st = static_cast<float>(sp[Tile<T, DY>::at(c, d)]);
-                if (NP > 1) st += static_cast<float>(sp[DZ * DY + Tile<T, DY>::at(c, d)]);
-                v[r] = fmaf(xd, HALF ? st * s_scale[c] : st, v[r]);
-              }
-            }
-            // (a state that is not finite makes these outputs what they are: nothing has to be added)
-            if (__ballot(!__builtin_isunordered(v[0], v[1]) || !__builtin_isunordered(v[2], v[3])))
-#pragma unroll 1
-              for (int q = 0; q <= i; ++q) {
-                float pq = 0.f;
-#pragma unroll 1
-                for (int d = 0; d < j.dy; ++d) pq = fmaf(static_cast<float>(xs[Tile<T, DY>::at(i, d)]), static_cast<float>(ys[Tile<T, DY>::at(q, d)]), pq);
-                pq *= p_scale * decay_power(g, i - q);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = fmaf(pq, static_cast<float>(zs[Tile<T, DZ>::at(q, 16 * ct + lr + r)]), v[r]);
-              }
-            put(ct, v);
-          }
-        } else if (out_whole && !shift) {
+        if (out_whole && !shift) {
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) store4(reinterpret_cast<T*>(at) + 16 * ct, o[ct], 4);
         } else {
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) put(ct, o[ct]);
+        }
+        // Zero times infinity is NaN: where a value is not finite, the zeros of P above the diagonal have brought it to earlier rows.  Outputs that are not numbers are
+        // computed once more from their own pairs alone (unless the state has made them so), and replaced.
+        if (!__ballot(some)) return;
+        unsigned nan = 0;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) nan |= o[ct][r] != o[ct][r] ? 1u << (4 * ct + r) : 0u;
+        if (i < shift) return;
+#pragma unroll 1
+        for (int b = 0; b < 4 * CT; ++b) {
+          const int c = b / 4 * 16 + lr + b % 4;
+          if (!(nan >> b & 1) || c >= dz) continue;
+          double v = 0;
+#pragma unroll 1
+          for (int d = 0; d < j.dy; ++d) {
+            float st = static_cast<float>(sp[Tile<T, DY>::at(c, d)]);
+            if (NP > 1) st += static_cast<float>(sp[DZ * DY + Tile<T, DY>::at(c, d)]);
+            v += double(static_cast<float>(xs[Tile<T, DY>::at(i, d)])) * (HALF ? st * s_scale[c] : st);
+          }
+          v *= f;
+          if (v != v) continue;
+#pragma unroll 1
+          for (int q = 0; q <= i; ++q) {
+            double pq = 0;
+#pragma unroll 1
+            for (int d = 0; d < j.dy; ++d)
+              pq += double(static_cast<float>(xs[Tile<T, DY>::at(i, d)])) * static_cast<float>(ys[Tile<T, DY>::at(q, d)]);
+            v += pq * (p_scale * decay_power(g, i - q)) * static_cast<float>(zs[Tile<T, DZ>::at(q, c)]);
+          }
+          const int place = c - lr;
+          if (out_f32) reinterpret_cast<float*>(at)[place] = static_cast<float>(v);
+          else reinterpret_cast<T*>(at)[place] = static_cast<T>(static_cast<float>(v));
         }
       };
       if (16 * it + 15 >= shift) {
