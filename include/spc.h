@@ -394,7 +394,7 @@ int spc_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_
  * Linear attention with a decay for each head, along the rows of every scene in their (sorted) order:
  *   S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T,   out_t = scale S_t^T q_t,   S of dk x dv, in 32 bits.
  * heads query heads, of which heads / kv_heads consecutive ones share a head of keys and values.
- * Heads have 1 to 128 channels (SPC_ERR_UNSUPPORTED above).
+ * Heads have 1 to 128 channels, scenes times heads are at most 200 000 (a step's streams times heads below 2^24): SPC_ERR_UNSUPPORTED above.
  */
 typedef struct spc_attn_desc {
   int32_t dtype;

@@ -20,6 +20,7 @@ namespace {
 
 constexpr int ATTN_MAX_D = 128;
 constexpr int ATTN_MAX_JOBS = 3;
+constexpr int64_t ATTN_MAX_SCENE_HEADS = 200000;
 
 struct Rows {
   void* p;
@@ -577,8 +578,9 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
 
 // Sums of segments -> the state behind every segment but the last of its scene, in place.
 __global__ __launch_bounds__(256) void scan_states_kernel(const ScanArgs a) {
-  const Job& j = a.job[blockIdx.z];
-  const int h = blockIdx.y % a.heads, scene = blockIdx.y / a.heads, i = blockIdx.x * 256 + threadIdx.x;
+  const Job& j = a.job[blockIdx.y];
+  const int share = (j.dy * j.dz + 255) / 256, sh = blockIdx.x / share, h = sh % a.heads, scene = sh / a.heads;
+  const int i = (blockIdx.x - sh * share) * 256 + threadIdx.x;
   if (i >= j.dy * j.dz) return;
   const int lo = a.offsets ? min(max(a.offsets[scene], 0), a.n_rows) : 0;
   const int id = lo / a.seg_rows + scene;
@@ -613,19 +615,18 @@ struct HeadSums {
 };
 template <typename T>
 __global__ __launch_bounds__(256) void sum_heads_kernel(HeadSums k, HeadSums v, int64_t n_rows, int kv_heads, int group) {
-  int64_t i = blockIdx.x * int64_t(256) + threadIdx.x;
-  const int64_t nk = n_rows * kv_heads * k.d;
-  const bool second = i >= nk;
-  const HeadSums a = second ? v : k;
-  if (second) i -= nk;
-  if (i >= n_rows * kv_heads * a.d) return;
-  const int c = static_cast<int>(i % a.d);
-  const int64_t rh = i / a.d, row = rh / kv_heads;
-  const float* p = a.part + rh * group * a.d + c;
-  float s = 0.f;
+  const int64_t nk = n_rows * kv_heads * k.d, n = nk + n_rows * kv_heads * v.d;
+  for (int64_t at = blockIdx.x * int64_t(256) + threadIdx.x; at < n; at += gridDim.x * int64_t(256)) {
+    const bool second = at >= nk;
+    const HeadSums a = second ? v : k;
+    const int64_t i = second ? at - nk : at, rh = i / a.d, row = rh / kv_heads;
+    const int c = static_cast<int>(i - rh * a.d);
+    const float* p = a.part + rh * group * a.d + c;
+    float s = 0.f;
 #pragma unroll 4
-  for (int g = 0; g < group; ++g) s += p[int64_t(g) * a.d];
-  static_cast<T*>(a.out.p)[row * a.out.row + (rh - row * kv_heads) * a.out.head + c] = static_cast<T>(s);
+    for (int g = 0; g < group; ++g) s += p[int64_t(g) * a.d];
+    static_cast<T*>(a.out.p)[row * a.out.row + (rh - row * kv_heads) * a.out.head + c] = static_cast<T>(s);
+  }
 }
 
 // One row more: a workgroup updates one head's state of one stream, S <- l S + k v^T, and adds up its columns times q on the way.  Every value of the state is read and
@@ -710,7 +711,8 @@ int check_desc(const spc_attn_desc* d) {
                      d->heads, d->kv_heads, d->dk, d->dv);
   if (!(d->scale > -3.4e38f && d->scale < 3.4e38f)) return set_error(SPC_ERR_ARG, "scale is not finite");
   if (d->dk > ATTN_MAX_D || d->dv > ATTN_MAX_D) return set_error(SPC_ERR_UNSUPPORTED, "heads of %d and %d channels: at most %d", d->dk, d->dv, ATTN_MAX_D);
-  if (d->n_rows >= (int64_t(1) << 31) || (d->n_rows / 64 + d->n_scenes) * d->heads * ATTN_MAX_JOBS >= (int64_t(1) << 31))
+  // (a launch takes less than 2^32 threads, 64 workgroups of 256 of them to a scene and head; a segment's rows grow with all rows)
+  if (d->n_rows >= (int64_t(1) << 31) || int64_t(d->n_scenes) * d->heads > ATTN_MAX_SCENE_HEADS)
     return set_error(SPC_ERR_UNSUPPORTED, "%lld rows of %d heads in %d scenes", static_cast<long long>(d->n_rows), d->heads, d->n_scenes);
   return SPC_OK;
 }
@@ -768,7 +770,7 @@ int launch_scan(ScanArgs& a, int n_sums, hipStream_t s) {
     const int jobs = a.n_jobs;
     a.n_jobs = n_sums;
     hipLaunchKernelGGL((scan_chunks_kernel<T, DY, DZ, false>), grid(), dim3(256), (scan_lds<T, DY, DZ, false>()), s, a);
-    hipLaunchKernelGGL(scan_states_kernel, dim3((a.job[0].dy * a.job[0].dz + 255) / 256, a.n_scenes * a.heads, n_sums), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(scan_states_kernel, dim3((a.job[0].dy * a.job[0].dz + 255) / 256 * a.n_scenes * a.heads, n_sums), dim3(256), 0, s, a);
     a.n_jobs = jobs;
   }
   constexpr size_t lds = scan_lds<T, DY, DZ, true>();
@@ -897,7 +899,7 @@ extern "C" int spc_linear_attention_backward(const spc_attn_desc* d, const spc_a
     by_dtype(d->dtype, [&](auto t) {
       using T = decltype(t);
       const int64_t n = int64_t(a.n_rows) * d->kv_heads * (d->dk + d->dv);
-      hipLaunchKernelGGL(sum_heads_kernel<T>, dim3((n + 255) / 256), dim3(256), 0, s, HeadSums{part_k, rows_of(dk, 1), d->dk},
+      hipLaunchKernelGGL(sum_heads_kernel<T>, dim3(std::min<int64_t>((n + 255) / 256, 16384)), dim3(256), 0, s, HeadSums{part_k, rows_of(dk, 1), d->dk},
                          HeadSums{part_v, rows_of(dv, 1), d->dv}, a.n_rows, d->kv_heads, group);
     });
     const hipError_t err = hipGetLastError();
@@ -911,7 +913,7 @@ extern "C" int spc_linear_attention_step(const spc_attn_desc* d, const spc_attn_
                                          const float* log_decay, float* state, const spc_attn_rows* out, void* stream) {
   using namespace spc;
   SPC_RETURN_IF(check_desc(d));
-  if (d->n_rows * d->heads >= (int64_t(1) << 31)) return set_error(SPC_ERR_UNSUPPORTED, "%lld streams of %d heads", static_cast<long long>(d->n_rows), d->heads);
+  if (d->n_rows * d->heads >= (int64_t(1) << 24)) return set_error(SPC_ERR_UNSUPPORTED, "%lld streams of %d heads", static_cast<long long>(d->n_rows), d->heads);
   if (!log_decay) return set_error(SPC_ERR_ARG, "log_decay is NULL");
   if (!d->n_rows) return SPC_OK;
   if (!state) return set_error(SPC_ERR_ARG, "state is NULL");
@@ -942,7 +944,7 @@ extern "C" int spc_batch_offsets(const void* keys, int64_t n, const spc_pack_des
   PackInfo pi;
   if (!d || !offsets) return set_error(SPC_ERR_ARG, "NULL argument");
   SPC_RETURN_IF(spc::check_desc(d, &pi));
-  if (n < 0 || n >= (int64_t(1) << 31) || n_batch < 1 || (n && !keys)) return set_error(SPC_ERR_ARG, "%lld keys of %d scenes", static_cast<long long>(n), n_batch);
+  if (n < 0 || n >= (int64_t(1) << 31) || n_batch < 1 || n_batch > (1 << 30) || (n && !keys)) return set_error(SPC_ERR_ARG, "%lld keys of %d scenes", static_cast<long long>(n), n_batch);
   const int sh = pi.bits_b ? pi.sh_b : 64;
   const dim3 grid((n_batch + 256) / 256);
   if (pi.key_bits == 32)

@@ -132,6 +132,7 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_forward_kernel(const NormAr
       me.load(r, a.r, row, a.ld_r);
 #pragma unroll
       for (int k = 0; k < R::E; ++k) z[k] += r[k];
+      if (G > 64 && FIT == MOVED) __syncthreads();  // (z may lie over x or r: another wave's piece is read here too)
       me.store(z, a.z, row, a.ld_z);  // (the norm goes on with the sum as it was before this rounding)
     }
     float s = 0.f;
@@ -187,6 +188,7 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_backward_kernel(const NormA
       me.load(e, a.e, row, a.ld_e);
 #pragma unroll
       for (int k = 0; k < R::E; ++k) dy[k] = fmaf(rstd, dy[k] - s1 - h[k] * s2, e[k]);
+      if (G > 64 && FIT == MOVED) __syncthreads();  // (dx may lie over e)
     } else {
 #pragma unroll
       for (int k = 0; k < R::E; ++k) dy[k] = rstd * (dy[k] - s1 - h[k] * s2);

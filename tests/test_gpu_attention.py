@@ -283,6 +283,25 @@ def test_offsets_that_are_none_stay_inside_the_rows(offsets):
         assert (t[:300] == 5).all() and (t[600:] == 5).all()
 
 
+def test_many_scenes():
+    """More scenes times heads than a grid has rows, three rows each, the last longer than a segment."""
+    b, H, d = 20_000, 4, 16
+    lengths = [3] * b + [300]
+    q, k, v, g, offsets, _, S0 = make(lengths, H, H, d, d, F32, 85, True)
+    o, last = B.spc_linear_attention_forward(q, k, v, g, offsets, scale=0.3, initial_state=S0, want_state=True)
+    l, S = torch.exp(cpu(g))[:, None, None], cpu(S0[:b])
+    qs, ks, vs = (cpu(t[:3 * b]).reshape(b, 3, H, d) for t in (q, k, v))
+    for t in range(3):
+        S = l * S + ks[:, t, :, :, None] * vs[:, t, :, None, :]
+        ref = 0.3 * (qs[:, t, :, :, None] * S).sum(2)
+        assert (cpu(o[t:3 * b:3]) - ref).abs().max() <= 2.0 ** -16 * 16 * 64  # (sixteen products of values below 4 and states below 16)
+    assert (cpu(last[:b]) - S).abs().max() <= 2.0 ** -16 * 64
+    whole, end = recur(cpu(q[3 * b:]), cpu(k[3 * b:]), cpu(v[3 * b:]), cpu(g), [0, 300], 0.3, cpu(S0[b:]))
+    mag, emag = recur(cpu(q[3 * b:]).abs(), cpu(k[3 * b:]).abs(), cpu(v[3 * b:]).abs(), cpu(g), [0, 300], 0.3, cpu(S0[b:]).abs())
+    within(o[3 * b:], whole, mag, F32, "the long scene")
+    within32(last[b:], end, emag, F32, "its state")
+
+
 def test_no_rows_and_empty_scenes():
     q, k, v, g, _, _, _ = make([0], 2, 2, 16, 16, F32, 91, False)
     S0, dS = torch.randn(3, 2, 16, 16, device="cuda"), torch.randn(3, 2, 16, 16, device="cuda")
@@ -410,6 +429,8 @@ def test_refusals():
                 (0, 1, 40, 4, 2, 0, 16)):
         assert call(d=B.AttnDesc(*bad, 0.25)) == B.ERR_ARG, bad
     assert call(d=B.AttnDesc(0, 1, 1 << 31, 4, 2, 16, 16, 0.25)) == B.ERR_UNSUPPORTED
+    assert call(d=B.AttnDesc(0, 50_001, 40, 4, 2, 16, 16, 0.25), at=offsets.data_ptr()) == B.ERR_UNSUPPORTED  # scenes times heads
+    assert L.spc_linear_attention_step(B.AttnDesc(0, 1, 1 << 23, 4, 2, 16, 16, 0.25), r, r, r, g.data_ptr(), s, r, None) == B.ERR_UNSUPPORTED
     assert L.spc_linear_attention_step(d, r, r, r, g.data_ptr(), None, r, None) == B.ERR_ARG
     assert L.spc_linear_attention_backward(d, r, r, r, r, g.data_ptr(), None, None, None, r, r, None, None, None) == B.ERR_ARG
     assert L.spc_batch_offsets(s, 5, None, 1, s, None) == B.ERR_ARG

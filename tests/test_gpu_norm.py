@@ -129,7 +129,7 @@ def test_parameters_may_be_missing():
     assert torch.equal(dx, a[0]) and dgamma is None and dbeta is None
 
 
-@pytest.mark.parametrize("c", [64, 90, 3000])
+@pytest.mark.parametrize("c", [3, 64, 90, 3000, 3001, 7001])
 def test_in_place(c):
     gen = torch.Generator().manual_seed(5)
     x, r = rows(300, c, BF16, gen), rows(300, c, BF16, gen)
