@@ -279,7 +279,8 @@ constexpr size_t scan_lds() {
 // Workgroups (a wave on every SIMD) that a CU holds, by registers and LDS.
 template <typename T, int DY, int DZ>
 constexpr int scan_waves() {
-  return DY == 128 || (sizeof(T) == 4 && DY == 64) ? 2 : sizeof(T) == 2 && DY == 32 && DZ == 32 ? 4 : 3;
+  if (DY == 128) return sizeof(T) == 4 ? 1 : 2;
+  return sizeof(T) == 4 && DY == 64 ? 2 : sizeof(T) == 2 && DY == 32 && DZ == 32 ? 4 : 3;
 }
 
 // One segment of one head and DZ columns of z: chunk by chunk, with the state in registers.
