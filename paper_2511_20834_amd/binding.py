@@ -449,22 +449,28 @@ def spc_layer_norm_forward(x: torch.Tensor, gamma: torch.Tensor | None = None, b
                            want_stats: bool = False, stream=None):
     """Layer norm of the rows of x [n, c] (+ residual); gamma, beta [c] fp32.  Row pitches = stride(0).  Returns (y, sum, mean, rstd): sum is
     None without a residual, mean and rstd [n] fp32 are None without want_stats."""
-    assert x.is_cuda and x.dim() == 2 and x.dtype in _TORCH_DTYPE
-    (n, c), dev = x.shape, x.device
-    y = torch.empty(n, c, dtype=x.dtype, device=dev) if out is None else out
-    total = None
-    if residual is not None:
-        total = torch.empty(n, c, dtype=x.dtype, device=dev) if sum_out is None else sum_out
+    (n, c), dev, dtype, ld = x.shape, x.device, x.dtype, _norm_rows(x, x)
+    code = _TORCH_DTYPE.get(dtype)
+    assert code is not None
+    # (tensors made here need no checks; each costs a call of some 10 us about half of one)
+    y, ld_y, total, ld_s = out, c, None, c
+    if out is None:
+        y = torch.empty(n, c, dtype=dtype, device=dev)
     else:
+        ld_y = _norm_rows(out, x)
+    if residual is None:
         assert sum_out is None
+    elif sum_out is None:
+        total = torch.empty(n, c, dtype=dtype, device=dev)
+    else:
+        total, ld_s = sum_out, _norm_rows(sum_out, x)
     mean = rstd = None
     if want_stats:
         mean, rstd = torch.empty(n, dtype=torch.float32, device=dev), torch.empty(n, dtype=torch.float32, device=dev)
-    rc = lib().spc_layer_norm_forward(x.data_ptr(), _norm_rows(x, x), residual.data_ptr() if residual is not None else None,
+    rc = lib().spc_layer_norm_forward(x.data_ptr(), ld, residual.data_ptr() if residual is not None else None,
                                       _norm_rows(residual, x) if residual is not None else 0, _f32(gamma, (c,), dev), _f32(beta, (c,), dev),
-                                      eps, y.data_ptr(), _norm_rows(y, x), total.data_ptr() if total is not None else None,
-                                      _norm_rows(total, x) if total is not None else 0, mean.data_ptr() if want_stats else None,
-                                      rstd.data_ptr() if want_stats else None, n, c, _TORCH_DTYPE[x.dtype],
+                                      eps, y.data_ptr(), ld_y, total.data_ptr() if total is not None else None, ld_s,
+                                      mean.data_ptr() if want_stats else None, rstd.data_ptr() if want_stats else None, n, c, code,
                                       current_raw_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
@@ -475,39 +481,46 @@ def spc_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
                             dsum: torch.Tensor | None = None, out: torch.Tensor | None = None, want_params: bool = True, stream=None):
     """Gradients of spc_layer_norm_forward; x is its x, or its sum where there was a residual, dsum [n, c] a gradient that reaches that sum past
     the norm.  Returns (dx, dgamma, dbeta), the last two [c] fp32, or None without want_params."""
-    assert x.is_cuda and x.dim() == 2 and x.dtype in _TORCH_DTYPE
-    (n, c), dev = x.shape, x.device
-    dx = torch.empty(n, c, dtype=x.dtype, device=dev) if out is None else out
+    (n, c), dev, ld = x.shape, x.device, _norm_rows(x, x)
+    code = _TORCH_DTYPE.get(x.dtype)
+    assert code is not None
+    dx, ld_dx = out, c
+    if out is None:
+        dx = torch.empty(n, c, dtype=x.dtype, device=dev)
+    else:
+        ld_dx = _norm_rows(out, x)
     dgamma = dbeta = None
     if want_params:
         dgamma, dbeta = torch.empty(c, dtype=torch.float32, device=dev), torch.empty(c, dtype=torch.float32, device=dev)
-    rc = lib().spc_layer_norm_backward(dy.data_ptr(), _norm_rows(dy, x), x.data_ptr(), _norm_rows(x, x), _f32(mean, (n,), dev),
+    rc = lib().spc_layer_norm_backward(dy.data_ptr(), _norm_rows(dy, x), x.data_ptr(), ld, _f32(mean, (n,), dev),
                                        _f32(rstd, (n,), dev), _f32(gamma, (c,), dev), dsum.data_ptr() if dsum is not None else None,
-                                       _norm_rows(dsum, x) if dsum is not None else 0, dx.data_ptr(), _norm_rows(dx, x),
-                                       dgamma.data_ptr() if want_params else None, dbeta.data_ptr() if want_params else None, n, c,
-                                       _TORCH_DTYPE[x.dtype], current_raw_stream() if stream is None else _stream(stream))
+                                       _norm_rows(dsum, x) if dsum is not None else 0, dx.data_ptr(), ld_dx,
+                                       dgamma.data_ptr() if want_params else None, dbeta.data_ptr() if want_params else None, n, c, code,
+                                       current_raw_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return dx, dgamma, dbeta
 
 
-def _heads(t: torch.Tensor, n: int, heads: int, width: int, like: torch.Tensor) -> AttnRows:
-    st = t.stride()
-    assert t.is_cuda and t.device == like.device and t.dtype == like.dtype and t.shape == (n, heads, width) and (st[2] == 1 or width == 1)
-    return AttnRows(t.data_ptr(), st[0], st[1])
+def _heads(t: torch.Tensor, n: int, heads: int, width: int, dtype, dev) -> AttnRows:
+    row, head, channel = t.stride()
+    assert t.dtype == dtype and t.device == dev and t.shape == (n, heads, width) and (channel == 1 or width == 1)
+    return AttnRows(t.data_ptr(), row, head)
 
 
 def _attention(q, k, v, log_decay, offsets, scale):
     """What the calls share: (descriptor, q, k, v in C form, log_decay's and offsets' addresses)."""
-    assert q.is_cuda and q.dim() == 3 and k.dim() == 3 and v.dim() == 3 and q.dtype in _TORCH_DTYPE
-    (n, heads, dk), (kv, dv), dev = q.shape, v.shape[1:], q.device
-    n_scenes = 1
+    n, heads, dk = q.shape
+    _, kv, dv = v.shape
+    dev, dtype, n_scenes, at = q.device, q.dtype, 1, None
+    code = _TORCH_DTYPE.get(dtype)
+    assert q.is_cuda and code is not None
     if offsets is not None:
-        n_scenes = offsets.shape[0] - 1
+        n_scenes, at = offsets.shape[0] - 1, offsets.data_ptr()
         assert offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.is_contiguous() and offsets.device == dev
-    d = AttnDesc(_TORCH_DTYPE[q.dtype], n_scenes, n, heads, kv, dk, dv, dk ** -0.5 if scale is None else scale)
-    return d, _heads(q, n, heads, dk, q), _heads(k, n, kv, dk, q), _heads(v, n, kv, dv, q), _f32(log_decay, (heads,), dev), \
-        None if offsets is None else offsets.data_ptr()
+    d = AttnDesc(code, n_scenes, n, heads, kv, dk, dv, dk ** -0.5 if scale is None else scale)
+    return (d, _heads(q, n, heads, dk, dtype, dev), _heads(k, n, kv, dk, dtype, dev), _heads(v, n, kv, dv, dtype, dev),
+            _f32(log_decay, (heads,), dev), at)
 
 
 def spc_linear_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, offsets: torch.Tensor | None = None,
@@ -519,11 +532,12 @@ def spc_linear_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tens
     d, rq, rk, rv, g, at = _attention(q, k, v, log_decay, offsets, scale)
     n, heads, dev = d.n_rows, d.heads, q.device
     shape = (d.n_scenes, heads, d.dk, d.dv)
+    ro = None if out is None else _heads(out, n, heads, d.dv, q.dtype, dev)
     if out is None:
         out = torch.empty(n, heads, d.dv, dtype=q.dtype, device=dev)
+        ro = AttnRows(out.data_ptr(), heads * d.dv, d.dv)
     if state_out is None and want_state:
         state_out = torch.empty(shape, dtype=torch.float32, device=dev)
-    ro = _heads(out, n, heads, d.dv, q)
     rc = lib().spc_linear_attention_forward(d, rq, rk, rv, g, at, _f32(initial_state, shape, dev), ro, _f32(state_out, shape, dev),
                                             current_raw_stream() if stream is None else _stream(stream))
     if rc:
@@ -542,9 +556,9 @@ def spc_linear_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.
     if out is None:
         out = tuple(torch.empty(*s, dtype=q.dtype, device=dev) for s in ((n, heads, d.dk), (n, kv, d.dk), (n, kv, d.dv)))
     dinitial = torch.empty(shape, dtype=torch.float32, device=dev) if want_dinitial else None
-    rc = lib().spc_linear_attention_backward(d, _heads(dout, n, heads, d.dv, q), rq, rk, rv, g, at, _f32(initial_state, shape, dev),
-                                             _f32(dstate, shape, dev), _heads(out[0], n, heads, d.dk, q), _heads(out[1], n, kv, d.dk, q),
-                                             _heads(out[2], n, kv, d.dv, q), _f32(dinitial, shape, dev),
+    rc = lib().spc_linear_attention_backward(d, _heads(dout, n, heads, d.dv, q.dtype, dev), rq, rk, rv, g, at, _f32(initial_state, shape, dev),
+                                             _f32(dstate, shape, dev), _heads(out[0], n, heads, d.dk, q.dtype, dev), _heads(out[1], n, kv, d.dk, q.dtype, dev),
+                                             _heads(out[2], n, kv, d.dv, q.dtype, dev), _f32(dinitial, shape, dev),
                                              current_raw_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
@@ -555,10 +569,12 @@ def spc_linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                               scale: float | None = None, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """One more row for every stream: q [streams, heads, dk] and so on; state [streams, heads, dk, dv] fp32 is updated in place."""
     d, rq, rk, rv, g, _ = _attention(q, k, v, log_decay, None, scale)
+    n, heads, dk, dv, dev = d.n_rows, d.heads, d.dk, d.dv, q.device
+    ro = None if out is None else _heads(out, n, heads, dv, q.dtype, dev)
     if out is None:
-        out = torch.empty(d.n_rows, d.heads, d.dv, dtype=q.dtype, device=q.device)
-    rc = lib().spc_linear_attention_step(d, rq, rk, rv, g, _f32(state, (d.n_rows, d.heads, d.dk, d.dv), q.device),
-                                         _heads(out, d.n_rows, d.heads, d.dv, q), current_raw_stream() if stream is None else _stream(stream))
+        out = torch.empty(n, heads, dv, dtype=q.dtype, device=dev)
+        ro = AttnRows(out.data_ptr(), heads * dv, dv)
+    rc = lib().spc_linear_attention_step(d, rq, rk, rv, g, _f32(state, (n, heads, dk, dv), dev), ro, current_raw_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return out
