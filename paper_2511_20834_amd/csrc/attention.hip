@@ -838,7 +838,7 @@ extern "C" int spc_linear_attention_forward(const spc_attn_desc* d, const spc_at
   a.n_ids = a.n_rows / a.seg_rows + a.n_scenes;
   float* ws = nullptr;
   if (a.n_rows > a.seg_rows) {
-    ws = static_cast<float*>(pool_alloc(size_t(a.n_ids) * a.heads * e * sizeof(float), s));
+    ws = static_cast<float*>(pool_alloc(scratch_bytes(size_t(a.n_ids) * a.heads * e * sizeof(float)), s));
     if (!ws) return SPC_ERR_NOMEM;
   }
   j.between = {ws, e, d->dv, 1};
@@ -880,7 +880,7 @@ extern "C" int spc_linear_attention_backward(const spc_attn_desc* d, const spc_a
   const size_t parts = group > 1 ? size_t(a.n_rows) * a.heads : 0;  // gradients of shared keys and values, by head
   float* ws = nullptr;
   if (states || parts) {
-    ws = static_cast<float*>(pool_alloc((2 * states + parts * (d->dk + d->dv)) * sizeof(float), s));
+    ws = static_cast<float*>(pool_alloc(scratch_bytes((2 * states + parts * (d->dk + d->dv)) * sizeof(float)), s));
     if (!ws) return SPC_ERR_NOMEM;
   }
   float *part_k = ws + 2 * states, *part_v = part_k + parts * d->dk;

@@ -363,7 +363,7 @@ extern "C" int spc_layer_norm_backward(const void* dy, int64_t ld_dy, const void
   a.y = dx, a.ld_y = ld_dx, a.n = n, a.c = c;
   const int wgs = norm_grid(dtype, c, n, true);
   if (params && n) {
-    a.partial = static_cast<float*>(pool_alloc(size_t(wgs) * 2 * c * sizeof(float), s));
+    a.partial = static_cast<float*>(pool_alloc(scratch_bytes(size_t(wgs) * 2 * c * sizeof(float)), s));
     if (!a.partial) return SPC_ERR_NOMEM;
   }
   if (n) by_dtype(dtype, [&](auto t) { norm_backward<decltype(t)>(a, wgs, s); });

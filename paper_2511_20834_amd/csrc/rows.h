@@ -17,4 +17,11 @@ void by_dtype(int32_t dtype, F&& f) {
   else f(0.f);
 }
 
+// Scratch of about so many bytes: a quarter of a power of two at a time above 1 MiB, so that calls of many sizes share the cache's blocks.
+inline size_t scratch_bytes(size_t bytes) {
+  size_t step = size_t(1) << 18;
+  while (step * 8 <= bytes) step *= 2;
+  return bytes <= (size_t(1) << 20) ? bytes : (bytes + step - 1) / step * step;
+}
+
 }  // namespace spc
