@@ -434,3 +434,20 @@ def test_refusals():
     assert L.spc_linear_attention_step(d, r, r, r, g.data_ptr(), None, r, None) == B.ERR_ARG
     assert L.spc_linear_attention_backward(d, r, r, r, r, g.data_ptr(), None, None, None, r, r, None, None, None) == B.ERR_ARG
     assert L.spc_batch_offsets(s, 5, None, 1, s, None) == B.ERR_ARG
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("decay", [0.0, -1 / 4096, -1 / 256])
+def test_long_memories_keep_their_bits(dtype, decay):
+    """A state of up to some 300 chunks (2-norms over a head).  A chunk's sum: up to 64 roundings of 2^-24 of sums that grow as a random walk, together some 3 of 2^-24.  Adding up the
+    chunks, 2 roundings each of a sum that grows likewise: some sqrt(300) / sqrt(3) / 2 = 5.  Together below 8, 2^-21; a decay whose rounding met all of them would add up to 64 halves, and
+    roundings at every product of a memory of 4096 rows and more some 12."""
+    n, heads, d = 20_000, 64, 16
+    gen = torch.Generator().manual_seed(5)
+    q, k, v = (torch.randn(n, heads, d, generator=gen).to(dtype) for _ in range(3))
+    g = torch.full((heads,), decay)
+    _, last = B.spc_linear_attention_forward(q.cuda(), k.cuda(), v.cuda(), g.cuda(), want_state=True)
+    w = torch.exp(g[0].double() * torch.arange(n - 1, -1, -1))[:, None]
+    for h in range(heads):
+        ref = (k[:, h].double() * w).T @ v[:, h].double()
+        assert (cpu(last[0, h]) - ref).norm() <= 2.0 ** -21 * ref.norm(), h
