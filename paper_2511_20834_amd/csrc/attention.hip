@@ -12,10 +12,10 @@
 //
 // Bytes bound large calls: the sums read k and v (for gradients q and the output's gradient as well), which are read again by the third launch, so a forward
 // pass moves 6 tensors for the 4 it cannot do without, a backward pass 11 for 7.  Measured, us a pass among others (in brackets the latter at a copy's
-// 4.84 TB/s): 120 k rows, 8 heads of 64, fp16 206 (102), its gradients in bf16 414 (178); 240 k rows, 4 heads of 32, bf16, with states 104 (51).  A row at a time
-// through LDS, the first version, took 7033, 13 343 and 3575.  Of the 206: sums 66 (51 for their bytes), states 10, outputs 129 (102).  In the gradients' third launch (287,
+// 4.84 TB/s): 120 k rows, 8 heads of 64, fp16 207 (102), its gradients in bf16 414 (178); 240 k rows, 4 heads of 32, bf16, with states 110 (51).  A row at a time
+// through LDS, the first version, took 7033, 13 343 and 3575.  Of the 207: sums 65 (51 for their bytes), states 10, outputs 132 (102).  In the gradients' third launch (286,
 // with 4 tensors read once for its three jobs, 178) the vector unit is busy 46 %, the matrix cores 20 %, LDS 30 %: three waves to a SIMD wait for each other's
-// fragments and barriers.  Small calls are bound by three launches: 2118 rows, 4 heads of 16, fp32 17.7, of which the kernels take 5.1, 5.1 and 7.7 and an empty one 2.4.
+// fragments and barriers.  Small calls are bound by three launches: 2118 rows, 4 heads of 16, fp32 18.6, of which the kernels take 5.7, 4.9 and 6.9 and an empty one 2.4.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -318,7 +318,7 @@ constexpr int scan_waves() {
 //   O^T = Z^T P^T + S^T X^T,  P^T = (Y X^T) o l^(i-j),   S <- l^n S + Y^T (w o Z)
 // Each of the four waves makes 16 rows of the chunk's output, whose products P^T are the next product's operand as they lie in its registers, and (DZ / 16 of
 // them) keeps 16 columns of the state, which all waves read from LDS as the pieces they multiply.
-// Operands that are no inputs (P, S, w o Z) go into 16-bit products as two pieces, the weighted values of bf16 as three: 16 bits of every sum that is
+// Operands that are no inputs (P, S, w o Z) go into 16-bit products as two pieces, the weighted values of bf16 as three where the state is returned: 16 bits of every sum that is
 // rounded to a 16-bit output in the end, 24 (fp16: 22) of what the state adds up.  fp16's pieces are scaled by powers of two, P by the largest of a row, S by
 // the largest of a column, since sums may leave its range.  fp32 takes fp32 products.
 template <typename T, int DY, int DZ, bool OUT>
@@ -671,7 +671,7 @@ __global__ __launch_bounds__(256) void sum_heads_kernel(HeadSums k, HeadSums v, 
 
 // One row more: a workgroup updates one head's state of one stream, S <- l S + k v^T, and adds up its columns times q on the way.  Every value of the state is read and
 // written once, in pieces of VEC columns (4; 1 where the columns are no multiple of it) whose loads are all under way before the first is used; the bytes bound it
-// (2048 streams of 8 heads of 64 x 64, fp16: 99 us for 546 MB, 5.5 TB/s; one stream 11.2, the host's call).  Neighbouring lanes have neighbouring pieces of a row, 2^log_q places of which hold one.
+// (2048 streams of 8 heads of 64 x 64, fp16: 99 us for 546 MB, 5.5 TB/s; one stream 9.8, the host's call).  Neighbouring lanes have neighbouring pieces of a row, 2^log_q places of which hold one.
 template <typename T, int VEC>
 __global__ __launch_bounds__(256) void attention_step_kernel(Rows q, Rows k, Rows v, Rows out, float* state, const float* log_decay, int heads, int dk, int dv,
                                                              float scale, int log_q) {

@@ -10,8 +10,8 @@
 // and a second launch adds them up in a fixed order: no atomics, the same bits every time.
 //
 // Measured, us a pass among others (with the bytes at the 4.84 TB/s that a copy of 2 GiB reaches, which caches of 256 MB can beat): forward 120 k x 256 fp16 with a residual 42.6
-// (50.8), backward 48.3 (50.8); 240 k x 256 bf16 94.6 (101.6), 94.4 (101.6); 70 k x 90 fp16 in rows of 180 backward 19.0 (7.8; 107 with pieces of two
-// channels and long shares).  Small calls are the host's: 2118 x 64 fp32 12.5 and 16.2.
+// (50.8), backward 48.3 (50.8); 240 k x 256 bf16 94.6 (101.6), 94.4 (101.6); 70 k x 90 fp16 in rows of 180 backward 18.3 (7.8; 107 with pieces of two
+// channels and long shares).  Small calls are the host's: 2118 x 64 fp32 10.7, the gradients of 6011 x 128 bf16 15.3.
 #include "rows.h"
 
 namespace spc {
