@@ -647,20 +647,22 @@ __global__ __launch_bounds__(256) void scan_states_kernel(const ScanArgs a) {
   }
 }
 
-// Gradients of keys and values that `group` heads share: sums over the heads, of [row][head][channel] each.
+// Gradients of keys and values that `group` heads share: sums over the heads, of [row][head][channel] each.  Rows from the first scene's first to the last one's last:
+// the scan makes the parts of no others.
 struct HeadSums {
   const float* part;
   Rows out;
   int d;
 };
 template <typename T>
-__global__ __launch_bounds__(256) void sum_heads_kernel(HeadSums k, HeadSums v, int64_t n_rows, int kv_heads, int group) {
-  const int64_t nk = n_rows * kv_heads * k.d, n = nk + n_rows * kv_heads * v.d;
+__global__ __launch_bounds__(256) void sum_heads_kernel(HeadSums k, HeadSums v, const int32_t* offsets, int n_scenes, int n_rows, int kv_heads, int group) {
+  const int lo = offsets ? min(max(offsets[0], 0), n_rows) : 0, hi = offsets ? min(max(offsets[n_scenes], lo), n_rows) : n_rows;
+  const int64_t first = int64_t(lo) * kv_heads, row_heads = int64_t(hi) * kv_heads - first, nk = row_heads * k.d, n = nk + row_heads * v.d;
   for (int64_t at = blockIdx.x * int64_t(256) + threadIdx.x; at < n; at += gridDim.x * int64_t(256)) {
     const bool second = at >= nk;
     const HeadSums a = second ? v : k;
-    const int64_t i = second ? at - nk : at, rh = i / a.d, row = rh / kv_heads;
-    const int c = static_cast<int>(i - rh * a.d);
+    const int64_t i = second ? at - nk : at, rh = first + i / a.d, row = rh / kv_heads;
+    const int c = static_cast<int>(i - (rh - first) * a.d);
     const float* p = a.part + rh * group * a.d + c;
     float s = 0.f;
 #pragma unroll 4
@@ -940,7 +942,7 @@ extern "C" int spc_linear_attention_backward(const spc_attn_desc* d, const spc_a
       using T = decltype(t);
       const int64_t n = int64_t(a.n_rows) * d->kv_heads * (d->dk + d->dv);
       hipLaunchKernelGGL(sum_heads_kernel<T>, dim3(std::min<int64_t>((n + 255) / 256, 16384)), dim3(256), 0, s, HeadSums{part_k, rows_of(dk, 1), d->dk},
-                         HeadSums{part_v, rows_of(dv, 1), d->dv}, a.n_rows, d->kv_heads, group);
+                         HeadSums{part_v, rows_of(dv, 1), d->dv}, offsets, d->n_scenes, a.n_rows, d->kv_heads, group);
     });
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) rc = set_error(SPC_ERR_HIP, "launch failed: %s", hipGetErrorString(err));

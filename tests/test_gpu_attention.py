@@ -451,3 +451,32 @@ def test_long_memories_keep_their_bits(dtype, decay):
     for h in range(heads):
         ref = (k[:, h].double() * w).T @ v[:, h].double()
         assert (cpu(last[0, h]) - ref).norm() <= 2.0 ** -21 * ref.norm(), h
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("heads,kv", [(2, 2), (2, 1), (6, 2)])
+@pytest.mark.parametrize("at", [[20, 120, 250], [0, 0, 299], [300, 300], [0, 0], [7, 7, 8]], ids=str)
+def test_gradients_of_rows_in_no_scene_are_left_alone(at, heads, kv, dtype):
+    """All three gradients, with heads of their own and with shared ones, whose parts per head lie in scratch that other calls have used.  Rows of scenes are held against
+    the recurrence."""
+    q, k, v, g, _, _, _ = make([300], heads, kv, 16, 24, dtype, 141, False, layout="rows")
+    do = torch.randn(300, heads, 24, generator=torch.Generator().manual_seed(142)).to(dtype).cuda()
+    offsets = torch.tensor(at, dtype=torch.int32, device="cuda")
+    for _ in range(2):  # (scratch full of NaN, if the next call takes its block)
+        B.spc_linear_attention_backward(do * float("nan"), q, k, v, g)
+    lo, hi = at[0], at[-1]
+    inside = [cpu(t)[lo:hi] for t in (do, q, k, v)]
+    for t in (do, q, k, v):
+        t[:lo], t[hi:] = float("nan"), float("nan")
+    outs = tuple(torch.full((300, h, w), 5.0, dtype=dtype, device="cuda") for h, w in ((heads, 16), (kv, 16), (kv, 24)))
+    B.spc_linear_attention_backward(do, q, k, v, g, offsets, scale=0.3, out=outs)
+    for t, what in zip(outs, ("dq", "dk", "dv")):
+        assert (t[:lo] == 5).all() and (t[hi:] == 5).all(), what
+    if hi == lo:
+        return
+    zero = torch.zeros(len(at) - 1, heads, 16, 24, dtype=torch.float64)
+    rel = [a - lo for a in at]
+    refs = reference_gradients(inside[0], *inside[1:], cpu(g), rel, 0.3, zero, zero)
+    mags = reference_gradients(*[t.abs() for t in inside], cpu(g), rel, 0.3, zero, zero)
+    for t, ref, mag, what in zip(outs, refs, mags, ("dq", "dk", "dv")):
+        within(t[lo:hi], ref, mag, dtype, what)
