@@ -75,7 +75,7 @@ struct Segment {
     lo = start(low);
     hi = max(start(low + 1), lo);
     m = id - (lo / a.seg_rows + low);
-    n = max((hi - lo + a.seg_rows - 1) / a.seg_rows, 1);
+    n = hi > lo ? (hi - lo - 1) / a.seg_rows + 1 : 1;  // (a scene's rows and a segment's more may pass 32 bits)
     rows = min(a.seg_rows, hi - lo - m * a.seg_rows);
     return m >= 0 && m < n;
   }

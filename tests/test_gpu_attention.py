@@ -480,3 +480,28 @@ def test_gradients_of_rows_in_no_scene_are_left_alone(at, heads, kv, dtype):
     mags = reference_gradients(*[t.abs() for t in inside], cpu(g), rel, 0.3, zero, zero)
     for t, ref, mag, what in zip(outs, refs, mags, ("dq", "dk", "dv")):
         within(t[lo:hi], ref, mag, dtype, what)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_scenes_of_nearly_all_the_rows_there_can_be(backward):
+    """2^31 - 1 rows of one scene: its rows and one segment's more pass 31 bits.  One row for all inputs; a decay of a half, so the sums are at 2 from row 24 on."""
+    n = (1 << 31) - 1
+    one = torch.ones(1, 1, 1, dtype=F16, device="cuda").expand(n, 1, 1)
+    g = torch.full((1,), 0.5, device="cuda").log()
+    if backward:
+        outs = tuple(torch.full((n, 1, 1), 5.0, dtype=F16, device="cuda") for _ in range(3))
+        dstate = torch.zeros(1, 1, 1, 1, device="cuda")
+        first = B.spc_linear_attention_backward(one, one, one, one, g, scale=1.0, dstate=dstate, want_dinitial=True, out=outs)[3]
+        assert abs(float(first) - 1) < 1e-6
+        checks = [(outs[0], False), (outs[1], True), (outs[2], True)]
+    else:
+        out, last = B.spc_linear_attention_forward(one, one, one, g, scale=1.0, want_state=True)
+        assert abs(float(last) - 2) < 1e-6
+        checks = [(out, False)]
+    for t, reverse in checks:
+        t = t.view(-1)
+        ends = t[-64:].flip(0) if reverse else t[:64]
+        want = 2 - torch.exp2(-torch.arange(64.0)).cuda()
+        assert (ends.float() - want).abs().max() <= 2 * U[F16] * 2
+        inner = t[:-64] if reverse else t[64:]
+        assert inner.min() == 2 and inner.max() == 2
