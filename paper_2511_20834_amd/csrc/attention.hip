@@ -244,9 +244,14 @@ __device__ inline void split(floatx8 x, typename Ops<T>::V (&out)[N]) {
     }
   }
 }
-__device__ inline float over_quads(float v) {  // maximum over the four lanes of a column (a row of A)
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
+// fp16's pieces of values of which the largest in this lane is m: times 2^-e for the e returned, e the same in the four lanes of a column (a row of A), the largest of all
+// is below 2^15 and no less than half of it.  The second piece goes up by 2^11 more (`split`), so what is lost of a value is 2^-51 of that largest one however small it is
+// itself: decays, and features of unlike rows, set values of one row of a product many powers of two apart.
+constexpr int HALF_TOP = 15, HALF_SHIFT = 11;
+__device__ inline int half_exponent(float m) {
+  m = fmaxf(m, __shfl_xor(m, 16, 64));
+  m = fmaxf(m, __shfl_xor(m, 32, 64));
+  return max(__builtin_amdgcn_frexp_expf(m), -100) - HALF_TOP;
 }
 
 // A chunk's rows of one tensor on their way from memory to LDS.  A segment's last chunk, where it is not full, lies in the tile's last rows; the rows in
@@ -319,14 +324,16 @@ constexpr int scan_waves() {
 // Each of the four waves makes 16 rows of the chunk's output, whose products P^T are the next product's operand as they lie in its registers, and (DZ / 16 of
 // them) keeps 16 columns of the state, which all waves read from LDS as the pieces they multiply.
 // Operands that are no inputs (P, S, w o Z) go into 16-bit products as two pieces, the weighted values of bf16 as three where the state is returned: 16 bits of every sum that is
-// rounded to a 16-bit output in the end, 24 (fp16: 22) of what the state adds up.  fp16's pieces are scaled by powers of two, P by the largest of a row, S by
-// the largest of a column, since sums may leave its range.  fp32 takes fp32 products.
+// rounded to a 16-bit output in the end, 24 (fp16: 22) of what the state adds up.  fp16's pieces are scaled by powers of two, P by the largest of a row, S and w o Z by
+// the largest of a column, since sums leave its range upwards and decays downwards (120 k rows, 8 heads of 64: 204 us, gradients 446; with pieces of P and S that lose what lies
+// 2^-25 below the largest, and of w o Z below 2^-36, 200 and 431).  fp32 takes fp32 products.
 template <typename T, int DY, int DZ, bool OUT>
 __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_kernel(const ScanArgs a) {
   using O = Ops<T>;
   using V = typename O::V;
   constexpr bool HALF = std::is_same_v<T, _Float16>, SINGLE = std::is_same_v<T, float>;
   constexpr int NP = SINGLE ? 1 : 2, NU = SINGLE ? 1 : HALF ? 2 : 3;  // pieces of P and S, of the weighted values
+  constexpr int SHIFT = HALF ? HALF_SHIFT : 0;
   constexpr int CT = DZ / 16, DT = DY / 16, KT = DY / 32, IT = CHUNK / 16, JT = CHUNK / 32;
   extern __shared__ __align__(16) char lds[];
   T *ys = reinterpret_cast<T*>(lds), *zs = ys + CHUNK * DY, *xs = zs + CHUNK * DZ, *sp = xs + CHUNK * DY;
@@ -414,14 +421,15 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
     if constexpr (OUT) {
       x.store(xs, shift);
       if (owner) {
-        int e = 0;
+        float down = 1.f;
         if constexpr (HALF) {
           float m = 0.f;
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(S[dt][r]));
-          e = __builtin_amdgcn_frexp_expf(over_quads(m));
+          const int e = half_exponent(m);
+          down = ldexpf(1.f, -e);
           if (lane < 16) s_scale[16 * ct_s + lc] = ldexpf(1.f, e);
         }
 #pragma unroll
@@ -429,10 +437,10 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
           floatx8 v = __builtin_shufflevector(S[2 * k], S[2 * k + 1], 0, 1, 2, 3, 4, 5, 6, 7);
           if constexpr (HALF) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = ldexpf(v[q], -e);
+            for (int q = 0; q < 8; ++q) v[q] *= down;
           }
           V f[NP];
-          split<T, NP>(v, f);
+          split<T, NP, SHIFT>(v, f);
 #pragma unroll
           for (int q = 0; q < NP; ++q) along.put(sp + (q * DZ + 16 * ct_s) * DY, k, f[q]);
         }
@@ -468,16 +476,17 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
         }
         float p_up = 1.f;
         if constexpr (HALF) {
-          const int e = __builtin_amdgcn_frexp_expf(over_quads(m));
+          const int e = half_exponent(m);
+          const float down = ldexpf(1.f, -e);
           p_up = ldexpf(1.f, e);
 #pragma unroll
           for (int t = 0; t < JN; ++t)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) P[t][k] = ldexpf(P[t][k], -e);
+            for (int k = 0; k < 8; ++k) P[t][k] *= down;
         }
         V pf[JN][NP];
 #pragma unroll
-        for (int t = 0; t < JN; ++t) split<T, NP>(P[t], pf[t]);
+        for (int t = 0; t < JN; ++t) split<T, NP, SHIFT>(P[t], pf[t]);
         __builtin_amdgcn_sched_barrier(0);  // (here and below: fragments are read when they are due, few registers have to do)
         const float f = shift || !e0 ? inter * decay_power(g, i - shift + e0) : f_full;
         floatx4 o[CT];
@@ -485,9 +494,11 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
         for (int ct = 0; ct < CT; ++ct) {
           o[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int k = 0; k < KT; ++k)
+          for (int q = NP - 1; q >= 0; --q) {
 #pragma unroll
-            for (int q = 0; q < NP; ++q) o[ct] = O::mma(along.get(sp + (q * DZ + 16 * ct) * DY, k), xf[k], o[ct]);
+            for (int k = 0; k < KT; ++k) o[ct] = O::mma(along.get(sp + (q * DZ + 16 * ct) * DY, k), xf[k], o[ct]);
+            if (HALF && q) o[ct] *= 1.f / (1 << SHIFT);
+          }
           if constexpr (HALF) o[ct] *= *reinterpret_cast<const floatx4*>(s_scale + 16 * ct + lr);
           o[ct] *= f;
           __builtin_amdgcn_sched_barrier(0);
@@ -497,11 +508,14 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
         for (int ct = 0; ct < CT; ++ct) {
           floatx4 v = {0.f, 0.f, 0.f, 0.f};
           if constexpr (!HALF) v = o[ct];
+          V zf[JN];
 #pragma unroll
-          for (int t = 0; t < JN; ++t) {
-            const V zf = down_z.get(zs + 32 * t * DZ, 16 * ct);
+          for (int t = 0; t < JN; ++t) zf[t] = down_z.get(zs + 32 * t * DZ, 16 * ct);
 #pragma unroll
-            for (int q = 0; q < NP; ++q) v = O::mma(zf, pf[t][q], v);
+          for (int q = NP - 1; q >= 0; --q) {
+#pragma unroll
+            for (int t = 0; t < JN; ++t) v = O::mma(zf[t], pf[t][q], v);
+            if (HALF && q) v *= 1.f / (1 << SHIFT);
           }
           if constexpr (HALF) o[ct] += v * p_up;
           else o[ct] = v;
@@ -537,7 +551,7 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
 #pragma unroll 1
           for (int d = 0; d < j.dy; ++d) {
             float st = static_cast<float>(sp[Tile<T, DY>::at(c, d)]);
-            if (NP > 1) st += static_cast<float>(sp[DZ * DY + Tile<T, DY>::at(c, d)]);
+            if (NP > 1) st += static_cast<float>(sp[DZ * DY + Tile<T, DY>::at(c, d)]) * (1.f / (1 << SHIFT));
             v += double(static_cast<float>(xs[Tile<T, DY>::at(i, d)])) * (HALF ? st * s_scale[c] : st);
           }
           v *= f;
@@ -565,13 +579,30 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
     }
     if (owner) {
       V uf[JT][NU];
+      floatx8 U[JT];
 #pragma unroll
       for (int t = 0; t < JT; ++t) {
-        floatx8 v = __builtin_convertvector(down_z.get(zs + 32 * t * DZ, 16 * ct_s), floatx8);
+        U[t] = __builtin_convertvector(down_z.get(zs + 32 * t * DZ, 16 * ct_s), floatx8);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= u[k % 4] * u_tile[2 * t + k / 4];
-        split<T, NU, HALF ? 11 : 0>(v, uf[t]);
+        for (int k = 0; k < 8; ++k) U[t][k] *= u[k % 4] * u_tile[2 * t + k / 4];
       }
+      float u_up = upd;
+      if constexpr (HALF) {
+        float m = 0.f;
+#pragma unroll
+        for (int t = 0; t < JT; ++t)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) m = fmaxf(m, fabsf(U[t][k]));
+        const int e = half_exponent(m);
+        const float down = ldexpf(1.f, -e);
+        u_up *= ldexpf(1.f, e);
+#pragma unroll
+        for (int t = 0; t < JT; ++t)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) U[t][k] *= down;
+      }
+#pragma unroll
+      for (int t = 0; t < JT; ++t) split<T, NU, SHIFT>(U[t], uf[t]);
       const Decay whole = shift || !e0 ? Decay(uniform(decay_power(g, n - 1 + e0))) : whole_full;
       // Products are added up apart and go to the state once a chunk: added to it one by one, each would round it, and a long memory takes many (fp32, 18 k rows a
       // scene, 8 heads of 48: 7.7e-7 of the outputs off, 2.9e-7 so).  A state of bf16 that nobody keeps, rounded to 16 bits a chunk later, takes that, and two pieces:
@@ -588,9 +619,9 @@ __global__ __launch_bounds__(256, (scan_waves<T, DY, DZ>())) void scan_chunks_ke
           for (int q = exact ? NU - 1 : 1; q >= 0; --q) {
 #pragma unroll
             for (int t = 0; t < JT; ++t) v = O::mma(yf[t], uf[t][q], v);
-            if (HALF && q) v *= 1.f / 2048.f;
+            if (HALF && q) v *= 1.f / (1 << SHIFT);
           }
-          if constexpr (HALF) v *= upd;
+          if constexpr (HALF) v *= u_up;
           S[dt] = exact ? whole.of(S[dt], v) : v;
         }
       };

@@ -505,3 +505,48 @@ def test_scenes_of_nearly_all_the_rows_there_can_be(backward):
         assert (ends.float() - want).abs().max() <= 2 * U[F16] * 2
         inner = t[:-64] if reverse else t[64:]
         assert inner.min() == 2 and inner.max() == 2
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("small,large", [(0.1, 100.0), (0.01, 1000.0)])
+@pytest.mark.parametrize("decay", [-1.0, -0.25, -1 / 256])
+@pytest.mark.parametrize("which", ["qkv", "k", "v", "kv"])
+def test_rows_of_unlike_scales(which, decay, small, large, dtype):
+    """Every sixteenth row far above the others, so that far rows count as much as near ones: each product is held against the sum of the magnitudes that it is made of."""
+    q, k, v, g, offsets, at, S0 = make([150, 70], 2, 1, 16, 24, dtype, 151, True, decay=decay)
+    by = torch.where(torch.arange(220) % 16 == 3, large, small).cuda()[:, None, None]
+    q, k, v = (t.float() * (by if name in which else 1.0) for name, t in zip("qkv", (q, k, v)))
+    scale = 30 / large ** len(which) if dtype == F16 else 0.3  # (outputs of fp16 below its largest number)
+    check_forward(q.to(dtype), k.to(dtype), v.to(dtype), g, offsets, at, S0, dtype, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_gradients_of_rows_of_unlike_scales(dtype):
+    q, k, v, g, offsets, at, S0 = make([150, 70], 4, 2, 16, 24, dtype, 152, True, decay=-0.5)
+    by = torch.where(torch.arange(220) % 16 == 3, 10.0, 0.02).cuda()[:, None, None]
+    check_backward(*((t.float() * by).to(dtype) for t in (q, k, v)), g, offsets, at, S0, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_channels_of_unlike_scales(dtype):
+    """One channel of the keys far above the others, which queries read as far below them."""
+    q, k, v, g, offsets, at, _ = make([200], 2, 2, 32, 32, dtype, 153, False, decay=-0.02)
+    by = torch.where(torch.arange(32) == 5, 1000.0, 0.01).cuda()
+    check_forward((q.float() / by / 10).to(dtype), (k.float() * by).to(dtype), v, g, offsets, at, None, dtype, scale=1.0)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("decay", [-1.0, -0.4])
+@pytest.mark.parametrize("rows", [64, 50])
+def test_values_before_rows_of_zeros(rows, decay, dtype):
+    """Values of a chunk's first rows and zeros behind them: the state is what the decay has left of the former."""
+    q, k, v, g, offsets, at, _ = make([rows], 2, 2, 16, 32, dtype, 154, False, decay=decay, layout="rows")
+    v[16:] = 0
+    check_forward(q, k, v, g, offsets, at, None, dtype)
+    do = torch.randn(rows, 2, 32, generator=torch.Generator().manual_seed(155)).to(dtype).cuda()
+    do[:-16] = 0  # (backward in time)
+    first = B.spc_linear_attention_backward(do, q, k, v, g, offsets, scale=0.3, want_dinitial=True)[3]
+    zero = torch.zeros(1, 2, 16, 32, dtype=torch.float64)
+    ref = reference_gradients(cpu(do), cpu(q), cpu(k), cpu(v), cpu(g), at, 0.3, zero, zero)[3]
+    mag = reference_gradients(cpu(do).abs(), cpu(q).abs(), cpu(k).abs(), cpu(v).abs(), cpu(g), at, 0.3, zero, zero)[3]
+    within32(first, ref, mag, dtype, "dinitial")
