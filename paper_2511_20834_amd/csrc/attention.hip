@@ -731,7 +731,8 @@ __global__ __launch_bounds__(256) void attention_step_kernel(Rows q, Rows k, Row
     vc[e] = c < dv ? static_cast<float>(static_cast<const T*>(v.p)[v.at(row, h) + c + e]) : 0.f;
     o[e] = 0.f;
   }
-  const float l = expf(log_decay[h]);
+  const float g = log_decay[h];
+  const Decay l(g, g * 1.44269504f, 1);  // (a stream takes it every row: one rounding of it drifts, 20 k rows at a decay of -1/4096 by 1e-4 of the state)
   __syncthreads();
   for (int r0 = t >> log_q; r0 < dk; r0 += AHEAD * step) {
     if (r0 >= AHEAD * step) load(r0);
@@ -742,7 +743,7 @@ __global__ __launch_bounds__(256) void attention_step_kernel(Rows q, Rows k, Row
         const float kr = ks[r], qr = qs[r];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          s[a][e] = fmaf(l, s[a][e], kr * vc[e]);
+          s[a][e] = l.of(s[a][e], kr * vc[e]);
           o[e] = fmaf(qr, s[a][e], o[e]);
         }
         *reinterpret_cast<Values*>(S + r * dv) = s[a];

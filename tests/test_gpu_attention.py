@@ -550,3 +550,26 @@ def test_values_before_rows_of_zeros(rows, decay, dtype):
     ref = reference_gradients(cpu(do), cpu(q), cpu(k), cpu(v), cpu(g), at, 0.3, zero, zero)[3]
     mag = reference_gradients(cpu(do).abs(), cpu(q).abs(), cpu(k).abs(), cpu(v).abs(), cpu(g), at, 0.3, zero, zero)[3]
     within32(first, ref, mag, dtype, "dinitial")
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("decay", [-1 / 4096, -1 / 3000, -1 / 256, -0.3])
+def test_long_streams_keep_their_bits(dtype, decay):
+    """20 000 steps of one stream (2-norms over a head).  A step rounds its state once, by up to half of 2^-23 of it, 2^-23 / sqrt(12) on average, and a memory of M = 1 / -decay
+    rows adds up M / 2 squares of that: sqrt(M / 2) 2^-24.8, twice that allowed.  (Short memories: no less than a step's own roundings, of its product and its decay.)  One
+    rounding of the decay would add up to M / 2 of 2^-24, 45 times as much at M = 4096.  And the scene call over the same rows, which has its own 2^-21."""
+    n, heads, d = 20_000, 4, 16
+    gen = torch.Generator().manual_seed(6)
+    q, k, v = (torch.randn(n, heads, d, generator=gen).to(dtype) for _ in range(3))
+    g = torch.full((heads,), decay)
+    S = torch.zeros(1, heads, d, d, device="cuda")
+    qg, kg, vg, gg, out = q.cuda(), k.cuda(), v.cuda(), g.cuda(), torch.empty(1, heads, d, dtype=dtype, device="cuda")
+    for t in range(n):
+        B.spc_linear_attention_step(qg[t:t + 1], kg[t:t + 1], vg[t:t + 1], gg, S, out=out)
+    _, last = B.spc_linear_attention_forward(qg, kg, vg, gg, want_state=True)
+    w = torch.exp(g[0].double() * torch.arange(n - 1, -1, -1))[:, None]
+    bound = 2 * max(0.5 / -decay, 4.0) ** 0.5 * 2.0 ** -24.8
+    for h in range(heads):
+        ref = (k[:, h].double() * w).T @ v[:, h].double()
+        assert (cpu(S[0, h]) - ref).norm() <= bound * ref.norm(), h
+        assert (cpu(S[0, h]) - cpu(last[0, h])).norm() <= (bound + 2.0 ** -21) * ref.norm(), h
