@@ -776,18 +776,18 @@ __global__ __launch_bounds__(256) void batch_offsets_kernel(const KeyT* __restri
 }
 
 // ---------------------------------------------------------------- host
-int check_desc(const spc_attn_desc* d) {
+int check_desc(const spc_attn_desc* d, bool scenes = true) {  // (without `scenes` their number is not read)
   if (!d) return set_error(SPC_ERR_ARG, "descriptor is NULL");
   if (d->dtype != SPC_DTYPE_F16 && d->dtype != SPC_DTYPE_BF16 && d->dtype != SPC_DTYPE_F32)
     return set_error(SPC_ERR_ARG, "unknown dtype %d", d->dtype);
-  if (d->n_rows < 0 || d->n_scenes < 1 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads || d->dk < 1 || d->dv < 1)
-    return set_error(SPC_ERR_ARG, "%lld rows, %d scenes, %d heads over %d, %d and %d channels", static_cast<long long>(d->n_rows), d->n_scenes,
+  if (d->n_rows < 0 || (scenes && d->n_scenes < 1) || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads || d->dk < 1 || d->dv < 1)
+    return set_error(SPC_ERR_ARG, "%lld rows, %d scenes, %d heads over %d, %d and %d channels", static_cast<long long>(d->n_rows), scenes ? d->n_scenes : 1,
                      d->heads, d->kv_heads, d->dk, d->dv);
   if (!(d->scale > -3.4e38f && d->scale < 3.4e38f)) return set_error(SPC_ERR_ARG, "scale is not finite");
   if (d->dk > ATTN_MAX_D || d->dv > ATTN_MAX_D) return set_error(SPC_ERR_UNSUPPORTED, "heads of %d and %d channels: at most %d", d->dk, d->dv, ATTN_MAX_D);
   // (a launch takes less than 2^32 threads, 64 workgroups of 256 of them to a scene and head; a segment's rows grow with all rows)
-  if (d->n_rows >= (int64_t(1) << 31) || int64_t(d->n_scenes) * d->heads > ATTN_MAX_SCENE_HEADS)
-    return set_error(SPC_ERR_UNSUPPORTED, "%lld rows of %d heads in %d scenes", static_cast<long long>(d->n_rows), d->heads, d->n_scenes);
+  if (d->n_rows >= (int64_t(1) << 31) || (scenes && int64_t(d->n_scenes) * d->heads > ATTN_MAX_SCENE_HEADS))
+    return set_error(SPC_ERR_UNSUPPORTED, "%lld rows of %d heads in %d scenes", static_cast<long long>(d->n_rows), d->heads, scenes ? d->n_scenes : 1);
   return SPC_OK;
 }
 // Pitches of an input may be zero (broadcast); places of an output are its own.
@@ -986,7 +986,7 @@ extern "C" int spc_linear_attention_backward(const spc_attn_desc* d, const spc_a
 extern "C" int spc_linear_attention_step(const spc_attn_desc* d, const spc_attn_rows* q, const spc_attn_rows* k, const spc_attn_rows* v,
                                          const float* log_decay, float* state, const spc_attn_rows* out, void* stream) {
   using namespace spc;
-  SPC_RETURN_IF(check_desc(d));
+  SPC_RETURN_IF(check_desc(d, false));
   if (d->n_rows * d->heads >= (int64_t(1) << 24)) return set_error(SPC_ERR_UNSUPPORTED, "%lld streams of %d heads", static_cast<long long>(d->n_rows), d->heads);
   if (!log_decay) return set_error(SPC_ERR_ARG, "log_decay is NULL");
   if (!d->n_rows) return SPC_OK;

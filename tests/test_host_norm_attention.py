@@ -75,3 +75,13 @@ def test_gradients_steps_and_offsets_refuse():
         assert L.spc_batch_offsets(keys, n, ctypes.byref(p), batch, out, None) == B.ERR_ARG
     assert L.spc_batch_offsets(P, 5, None, 2, P, None) == B.ERR_ARG
     assert "scenes" in B.lib().spc_last_error().decode() or "NULL" in B.lib().spc_last_error().decode()
+
+
+@pytest.mark.parametrize("scenes", [0, -7, 100_000, 2 ** 31 - 1])
+def test_steps_do_not_read_the_number_of_scenes(scenes):
+    L = B.lib()
+    assert L.spc_linear_attention_step(desc(rows=0, scenes=scenes), None, None, None, P, None, None, None) == B.OK
+    assert L.spc_linear_attention_step(desc(scenes=scenes), ROWS, ROWS, ROWS, P, None, ROWS, None) == B.ERR_ARG  # (no state)
+    assert L.spc_linear_attention_step(desc(scenes=scenes, heads=3), ROWS, ROWS, ROWS, P, P, ROWS, None) == B.ERR_ARG
+    assert L.spc_linear_attention_step(desc(rows=1 << 23, scenes=scenes), ROWS, ROWS, ROWS, P, P, ROWS, None) == B.ERR_UNSUPPORTED
+    assert L.spc_linear_attention_step(desc(rows=0, heads=300_000, kv=300_000), None, None, None, P, None, None, None) == B.OK
