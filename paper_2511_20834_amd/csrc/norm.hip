@@ -174,7 +174,7 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_backward_kernel(const NormA
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int k = 0; k < R::E; ++k) {
-      h[k] = me.has(k / R::VEC) ? (h[k] - mean) * rstd : 0.f;  // (behind the last channel dy is zero, but this may be infinite)
+      h[k] = (FIT == FEW ? me.counts(k) : me.has(k / R::VEC)) ? (h[k] - mean) * rstd : 0.f;  // (behind the last channel dy is zero, but this may be infinite)
       dgamma[k] = fmaf(dy[k], h[k], dgamma[k]);
       dbeta[k] += dy[k];
       dy[k] *= gamma[k];

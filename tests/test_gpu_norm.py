@@ -245,3 +245,26 @@ def test_refusals():
     assert L.spc_layer_norm_forward(None, 8, None, 0, None, None, 1e-5, p, 8, None, 0, None, None, 4, 8, 2, None) == B.ERR_ARG
     assert L.spc_layer_norm_forward(p, 8, None, 0, None, None, 1e-5, p, 8, None, 0, None, None, -1, 8, 2, None) == B.ERR_ARG
     assert L.spc_layer_norm_backward(p, 8, p, 8, None, p, None, None, 0, p, 8, None, None, 4, 8, 2, None) == B.ERR_ARG
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("c", [1, 2, 3, 4, 5, 7, 8, 9, 33, 90, 257, 513, 2051])
+def test_gradients_of_a_large_mean_with_a_tiny_deviation(c, dtype):
+    """mean * rstd leaves the range of 32 bits, (x - mean) * rstd of the row's channels does not: places behind the last channel must not come in.  Values are the
+    mean or the next one, so h has no rounding."""
+    gen = torch.Generator().manual_seed(c)
+    level, rstd = 2.0 ** 90, 2.0 ** 50
+    step = level * 2 * U[dtype]
+    x = (level + step * torch.randint(0, 2, (20, c), generator=gen)).to(dtype).cuda()
+    dy = torch.randn(20, c, generator=gen).to(dtype).cuda()
+    gamma = (1 + torch.randn(c, generator=gen)).cuda()
+    mean, s = torch.full((20,), level, device="cuda"), torch.full((20,), 1 / step, device="cuda")
+    x[10:], s[10:] = level, rstd  # (h of 0 and 1 above, of 0 here)
+    dx, dgamma, dbeta = B.spc_layer_norm_backward(dy, x, mean, s, gamma)
+    h = (x.double() - level) * s.double()[:, None]
+    w = dy.double() * gamma.double()
+    ref = s.double()[:, None] * (w - w.mean(1, keepdim=True) - h * (w * h).mean(1, keepdim=True))
+    wm, wh = w.abs().mean(1, keepdim=True), (w * h).abs().mean(1, keepdim=True)
+    within(dx, ref, U[dtype] * ref.abs() + 2.0 ** -126 + 2.0 ** -16 * s.double()[:, None] * (w.abs() + wm + h.abs() * wh), "dx")
+    within(dgamma, (dy.double() * h).sum(0), 2.0 ** -16 * (dy.double() * h).abs().sum(0), "dgamma")
+    within(dbeta, dy.double().sum(0), 2.0 ** -16 * dy.double().abs().sum(0), "dbeta")
