@@ -130,3 +130,75 @@ def test_recorded():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("heads,kv_heads", [(4, 4), (4, 2)])
+@pytest.mark.parametrize("rejected", [0, 1, 70])
+def test_rows_in_no_scene_stay_out(rejected, heads, kv_heads, dtype):
+    """Rejected rows lie behind the last scene.  They hold NaN in every input, and the memory that buffers are taken from is full of NaN: results of the other rows
+    and all gradients are those of the other rows alone."""
+    counts, c, d = [150, 0, 200], 64, 16
+    m = block(c, heads, kv_heads, d, dtype, 13)
+    gen = torch.Generator().manual_seed(14)
+    rows = []
+    for b, n in enumerate(counts):
+        lin = torch.randperm(40 ** 3, generator=gen)[:n]
+        rows.append(torch.stack([torch.full((n,), b), lin // 1600, lin // 40 % 40, lin % 40], 1))
+    rows = torch.cat([*rows, torch.full((rejected, 4), 1000)]).to(torch.int32).cuda()
+    n = 350 + rejected
+    desc = B.spc_pack_desc_fit([0, 0, 0], [39, 39, 39], 3, 1, 1)
+    keys, perm = B.spc_pack_coords(rows, desc)
+    kmap, offsets = m.scenes(keys, desc, 3)
+    assert offsets.tolist() == [0, 150, 150, 350]
+    x, dz, ds = (torch.randn(n, c, generator=gen).to(dtype).cuda() for _ in range(3))
+    for t in (x, dz, ds):
+        t[350:] = float("nan")
+    stale = [torch.full((n, w), float("nan"), dtype=t, device="cuda") for t in (dtype, torch.float32) for w in (1, c, heads * d, (heads + 2 * kv_heads) * d) for _ in range(8)]
+    del stale
+    z, s, saved = m.forward(x, kmap, offsets, save=True)
+    got = m.backward(dz, ds, saved)
+    p = params64(m)
+    x64 = x[:350].double().cpu().requires_grad_()
+    rz, rs = reference(m, x64, counts, p)
+    close(z[:350], rz, TOL[dtype], "z")
+    close(s[:350], rs, TOL[dtype], "s")
+    assert all(torch.equal(a[:350], b[:350]) for a, b in zip(m.forward(x, kmap, offsets), (z, s)))
+    grads = torch.autograd.grad((rz * dz[:350].double().cpu()).sum() + (rs * ds[:350].double().cpu()).sum(), [x64, *p])
+    ref = dict(zip(("x", "w_qkv", "w_out", "gamma1", "beta1", "gamma2", "beta2"), grads))
+    assert (got.x[350:] == 0).all()
+    for name in got._fields:
+        close(getattr(got, name)[:350] if name == "x" else getattr(got, name), ref[name], TOL[dtype], name)
+
+
+def test_scenes_in_the_middle_of_the_rows():
+    """Offsets of a part of the rows, in front and behind as well; without a second gradient."""
+    m = block(32, 2, 1, 16, F32, 15)
+    keys, _, desc = cloud([90, 60, 50], 16)
+    gen = torch.Generator().manual_seed(17)
+    x, dz = (torch.randn(200, 32, generator=gen).cuda() for _ in range(2))
+    kmap, offsets = m.scenes(keys, desc, 3)
+    x[:90], x[150:], dz[:90], dz[150:] = float("nan"), float("inf"), float("nan"), float("inf")
+    z, s, saved = m.forward(x, kmap, offsets[1:3].contiguous(), save=True)
+    got = m.backward(dz, None, saved)
+    p = params64(m)
+    x64 = x[90:150].double().cpu().requires_grad_()
+    rz, _ = reference(m, x64, [60], p)
+    close(z[90:150], rz, TOL[F32], "z")
+    grads = torch.autograd.grad((rz * dz[90:150].double().cpu()).sum(), [x64, *p])
+    ref = dict(zip(("x", "w_qkv", "w_out", "gamma1", "beta1", "gamma2", "beta2"), grads))
+    assert (got.x[:90] == 0).all() and (got.x[150:] == 0).all()
+    for name in got._fields:
+        close(getattr(got, name)[90:150] if name == "x" else getattr(got, name), ref[name], TOL[F32], name)
+
+
+def test_all_rows_said_to_lie_in_scenes():
+    """The same bits where that is so."""
+    m = block(64, 4, 2, 16, BF16, 18)
+    keys, _, desc = cloud([150, 0, 200], 19)
+    x, dz, ds = (torch.randn(350, 64, generator=torch.Generator().manual_seed(20 + i)).to(BF16).cuda() for i in range(3))
+    kmap, offsets = m.scenes(keys, desc, 3)
+    z, s, saved = m.forward(x, kmap, offsets, save=True)
+    z2, s2, saved2 = m.forward(x, kmap, offsets, save=True, all_rows=True)
+    assert torch.equal(z, z2) and torch.equal(s, s2)
+    assert all(torch.equal(a, b) for a, b in zip(m.backward(dz, ds, saved), m.backward(dz, ds, saved2)))
