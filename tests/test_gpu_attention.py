@@ -573,3 +573,74 @@ def test_long_streams_keep_their_bits(dtype, decay):
         ref = (k[:, h].double() * w).T @ v[:, h].double()
         assert (cpu(S[0, h]) - ref).norm() <= bound * ref.norm(), h
         assert (cpu(S[0, h]) - cpu(last[0, h])).norm() <= (bound + 2.0 ** -21) * ref.norm(), h
+
+
+def without_states(lengths, heads, kv, dk, dv, dtype, seed, decay=None, initial=False):
+    """The calls that return no state (bf16 keeps fewer bits of the states in between then), outputs and gradients within the same bounds."""
+    q, k, v, g, offsets, at, S0 = make(lengths, heads, kv, dk, dv, dtype, seed, initial, decay=decay)
+    do = torch.randn(q.shape[0], heads, dv, generator=torch.Generator().manual_seed(seed + 1)).to(dtype).cuda()
+    zero = torch.zeros(len(at) - 1, heads, dk, dv, dtype=torch.float64)
+    first = zero if S0 is None else cpu(S0)
+    o, last = B.spc_linear_attention_forward(q, k, v, g, offsets, scale=0.3, initial_state=S0)
+    assert last is None
+    within(o, recur(cpu(q), cpu(k), cpu(v), cpu(g), at, 0.3, first)[0], recur(cpu(q).abs(), cpu(k).abs(), cpu(v).abs(), cpu(g), at, 0.3, first.abs())[0], dtype, "out")
+    got = B.spc_linear_attention_backward(do, q, k, v, g, offsets, scale=0.3, initial_state=S0)
+    assert got[3] is None
+    refs = reference_gradients(cpu(do), cpu(q), cpu(k), cpu(v), cpu(g), at, 0.3, first, zero)
+    mags = reference_gradients(cpu(do).abs(), cpu(q).abs(), cpu(k).abs(), cpu(v).abs(), cpu(g), at, 0.3, first.abs(), zero)
+    for a, b, m, what in zip(got[:3], refs, mags, ("dq", "dk", "dv")):
+        within(a, b, m, dtype, what)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("lengths", [[2, 63, 64, 65], [129, 0, 1, 300], [700]], ids=str)
+@pytest.mark.parametrize("heads,kv,dk,dv", HEADS)
+def test_without_states(lengths, heads, kv, dk, dv, dtype):
+    without_states(lengths, heads, kv, dk, dv, dtype, 7 * dk + dv + 2)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("decay", [0.0, -1e-4, -0.05, -3.0, -200.0])
+def test_decays_without_states(decay, dtype):
+    without_states([150, 3, 400], 2, 2, 32, 32, dtype, 161, decay=decay, initial=True)
+
+
+def test_several_chunks_a_segment_without_states():
+    without_states([5000, 900], 16, 4, 16, 16, BF16, 162)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("decay", [0.0, -1 / 4096])
+def test_outputs_of_long_memories_without_states(dtype, decay):
+    """The last rows of one head of 20 000 (as in the test of their states; here what nobody keeps the state of)."""
+    n, heads, d = 20_000, 8, 32
+    gen = torch.Generator().manual_seed(7)
+    q, k, v = (torch.randn(n, heads, d, generator=gen).to(dtype) for _ in range(3))
+    g = torch.full((heads,), decay)
+    o, _ = B.spc_linear_attention_forward(q.cuda(), k.cuda(), v.cuda(), g.cuda(), scale=0.01)
+    for t in (n - 1, n - 70, 12_345):
+        w = torch.exp(g[0].double() * torch.arange(t, -1, -1))[:, None]
+        for h in range(0, heads, 3):
+            a, b, c = q[t, h].double(), k[:t + 1, h].double(), v[:t + 1, h].double()
+            within(o[t, h], 0.01 * ((b @ a)[:, None] * w * c).sum(0), 0.01 * ((b.abs() @ a.abs())[:, None] * w * c.abs()).sum(0), dtype, (t, h))
+
+
+@pytest.mark.parametrize("states", [False, True])
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_many_scenes_each_within_its_bounds(dtype, states):
+    """Scenes of three rows (and an empty one, and a long one), each held against the recurrence with the bounds of all other results."""
+    b, H, d = 3000, 4, 16
+    lengths = [3] * b + [0, 300]
+    q, k, v, g, offsets, _, S0 = make(lengths, H, 2, d, d, dtype, 163, True)
+    o, last = B.spc_linear_attention_forward(q, k, v, g, offsets, scale=0.3, initial_state=S0, want_state=states)
+    l = torch.exp(cpu(g))[:, None, None]
+    qs, ks, vs = (cpu(t[:3 * b]).reshape(b, 3, -1, d) for t in (q, k, v))
+    ks, vs = ks.repeat_interleave(2, 2), vs.repeat_interleave(2, 2)
+    S, M = cpu(S0[:b]), cpu(S0[:b]).abs()
+    for t in range(3):
+        S, M = l * S + ks[:, t, :, :, None] * vs[:, t, :, None, :], l * M + (ks[:, t, :, :, None] * vs[:, t, :, None, :]).abs()
+        ref, mag = (0.3 * (x[:, t, :, :, None] * y).sum(2) for x, y in ((qs, S), (qs.abs(), M)))
+        within(o[t:3 * b:3], ref, mag, dtype, t)
+    if states:
+        within32(last[:b], S, M, dtype, "states")
+        assert torch.equal(last[b], S0[b])
