@@ -394,6 +394,9 @@ int spc_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_
  * Linear attention with a decay for each head, along the rows of every scene in their (sorted) order:
  *   S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T,   out_t = scale S_t^T q_t,   S of dk x dv, in 32 bits.
  * heads query heads, of which heads / kv_heads consecutive ones share a head of keys and values.
+ * States are fp32, and every sum is accumulated in 32 bits.  fp32 rows take fp32 products.  For 16-bit rows the products q.k and the states enter 16-bit
+ * products as two pieces: bf16 16 bits of each value, fp16 22 (down to 2^-51 of the largest of a row or column).  What the states add up has 24 bits (fp16:
+ * 22); bf16 calls that return no state take 16 bits for it too, so their results may differ in the last bit from those of calls that do.
  * Heads have 1 to 128 channels, scenes times heads are at most 200 000 (a step's streams times heads below 2^24): SPC_ERR_UNSUPPORTED above.
  */
 typedef struct spc_attn_desc {
@@ -416,8 +419,8 @@ typedef struct spc_attn_rows {
  *               in no scene are neither read nor written, so padded buffers need no host count.  NULL: one scene of all rows.
  *   state_in    [device] [n_scenes][heads][dk][dv] floats, S before each scene's first row; NULL: zeros.
  *   state_out   [device] the same shape, S behind each scene's last row (state_in for an empty scene); may be NULL; not state_in itself.
- * An infinity or NaN in row t reaches rows from t on of its scene (and heads that read it) only.
- * Products and sums are accumulated in 32 bits; results are bit-reproducible.  Scratch comes from the library's block cache (as
+ * An infinity or NaN in row t reaches rows from t on of its scene (and heads that read it) only; in later rows and states it may arrive as NaN.
+ * Results are bit-reproducible.  Scratch comes from the library's block cache (as
  * for spc_conv_forward: a warmed-up call can be captured); nothing is waited for.
  */
 int spc_linear_attention_forward(const spc_attn_desc* d, const spc_attn_rows* q, const spc_attn_rows* k,
@@ -426,7 +429,7 @@ int spc_linear_attention_forward(const spc_attn_desc* d, const spc_attn_rows* q,
 /*
  * Its gradients (the decays are constants of the layer).  dout: gradient of out; state_in as in the forward pass; dstate_out: gradient of
  * state_out, may be NULL (zeros).  dq, dk, dv overlap no input; dk and dv are sums over the heads that share them.  dstate_in [device]:
- * gradient of state_in, may be NULL; not dstate_out itself.
+ * gradient of state_in, may be NULL; not dstate_out itself.  Rows in no scene are left alone in all three.
  */
 int spc_linear_attention_backward(const spc_attn_desc* d, const spc_attn_rows* dout, const spc_attn_rows* q,
                                   const spc_attn_rows* k, const spc_attn_rows* v, const float* log_decay,

@@ -12,10 +12,10 @@
 //
 // Bytes bound large calls: the sums read k and v (for gradients q and the output's gradient as well), which are read again by the third launch, so a forward
 // pass moves 6 tensors for the 4 it cannot do without, a backward pass 11 for 7.  Measured, us a pass among others (in brackets the latter at a copy's
-// 4.84 TB/s): 120 k rows, 8 heads of 64, fp16 207 (102), its gradients in bf16 414 (178); 240 k rows, 4 heads of 32, bf16, with states 110 (51).  A row at a time
-// through LDS, the first version, took 7033, 13 343 and 3575.  Of the 207: sums 65 (51 for their bytes), states 10, outputs 132 (102).  In the gradients' third launch (286,
-// with 4 tensors read once for its three jobs, 178) the vector unit is busy 46 %, the matrix cores 20 %, LDS 30 %: three waves to a SIMD wait for each other's
-// fragments and barriers.  Small calls are bound by three launches: 2118 rows, 4 heads of 16, fp32 18.6, of which the kernels take 5.7, 4.9 and 6.9 and an empty one 2.4.
+// 4.84 TB/s): 120 k rows, 8 heads of 64, fp16 209 (102), its gradients in bf16 406 (178); 240 k rows, 4 heads of 32, bf16, with states 109 (51).  A row at a time
+// through LDS, the first version, took 7033, 13 343 and 3575.  Of the 209 (launches traced alone, the fastest of 12): sums 64 (51 for their bytes), states
+// 10, outputs 131 (102).  In the gradients' third launch (285, with 4 tensors read once for its three jobs, 178) the vector unit issues in 55 % of the CUs' busy
+// cycles, the matrix cores work in 26 %, LDS in 36 %: three waves to a SIMD wait for each other's fragments and barriers.  Small calls are bound by three launches: 2118 rows, 4 heads of 16, fp32 18.7, of which the kernels take 5.0, 6.0 and 7.6 and an empty one 2.4.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
