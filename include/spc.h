@@ -452,6 +452,118 @@ int spc_batch_offsets(const void* keys, int64_t n, const spc_pack_desc* d, int32
                       void* stream);
 
 /*
+ * Root-mean-square norm of feature rows: z = x (+ residual), y = z / sqrt(mean(z^2) + eps) * gamma over the c channels of every row.  Arguments as
+ * spc_layer_norm_forward's: sum receives z where there is a residual, rstd [device] n floats (may be NULL) what the backward pass needs.  A row whose squares
+ * add up beyond 32 bits (values of 2^63 and more) comes out as zeros.
+ */
+int spc_rms_norm_forward(const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const float* gamma, float eps,
+                         void* y, int64_t ld_y, void* sum, int64_t ld_s, float* rstd, int64_t n, int32_t c, int32_t dtype,
+                         void* stream);
+/*
+ * The same with its output in 8 bits: row r of q holds e4m3 values (OCP: largest 448, no infinities), row pitch ld_q in bytes, and scale[r] (fp32)
+ * the largest |y| of the row over 448, so that y is q scale, rounded to nearest.  Rows of less than 2^-100 are scaled as if that were their largest value.  NaN
+ * stays NaN, and does not count as the largest.  q overlaps no input; sum may be x or residual.
+ */
+int spc_rms_norm_quantize(const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const float* gamma, float eps,
+                          void* q, int64_t ld_q, float* scale, void* sum, int64_t ld_s, float* rstd, int64_t n, int32_t c,
+                          int32_t dtype, void* stream);
+/* Rows in 8 bits as they are, by the same rule (weights of spc_linear_f8, for one: a row for each output channel).  A row with an infinity has an infinite scale. */
+int spc_quantize_rows(const void* x, int64_t ld_x, void* q, int64_t ld_q, float* scale, int64_t n, int32_t c, int32_t dtype,
+                      void* stream);
+/*
+ * Gradients of spc_rms_norm_forward: x the rows that were normalised (its x, or its sum), rstd as it was stored; dsum, dx, dgamma and scratch as in
+ * spc_layer_norm_backward.
+ */
+int spc_rms_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const float* rstd, const float* gamma,
+                          const void* dsum, int64_t ld_ds, void* dx, int64_t ld_dx, float* dgamma, int64_t n, int32_t c,
+                          int32_t dtype, void* stream);
+/*
+ * A 1x1x1 layer in 8 bits: out[r][j] = x_scale[r] * w_scale[j] * sum over k of x[r][k] w[j][k], e4m3 values added up in 32 bits.
+ *   x         [device] n rows of c bytes, pitch ld_x in bytes, any address; x_scale n floats (spc_rms_norm_quantize, spc_quantize_rows).
+ *   w         [device] cout rows of c bytes, pitch ld_w: the layer's weights with output channels as rows; w_scale cout floats.
+ *   out       [device] n rows of cout elements of dtype, pitch ld_out in elements; overlaps no input.
+ * c and cout are at most 65536, n at most 2^30 (SPC_ERR_UNSUPPORTED above).  Enqueues one kernel and waits for nothing.
+ */
+int spc_linear_f8(const void* x, int64_t ld_x, const float* x_scale, const void* w, int64_t ld_w, const float* w_scale, void* out,
+                  int64_t ld_out, int64_t n, int32_t c, int32_t cout, int32_t dtype, void* stream);
+
+/*
+ * Short causal convolution of every channel along the rows of its scene: p_t = bias + sum over k < width of weight[width-1-k] x_{t-k}, y_t = p_t / (1 + exp(-p_t))
+ * with silu, p_t without.  Sums are held in 32 bits.
+ *   x, y        [device] n rows of c elements, pitches ld_x, ld_y; y overlaps no input.
+ *   weight      [device] c x width floats, bias c floats (may be NULL), whatever the rows' type; width 1 to 4, c at most 65536 (SPC_ERR_UNSUPPORTED above).
+ *   offsets     [device] n_scenes + 1 ascending row numbers (spc_batch_offsets); NULL: one scene of all rows.  Rows in no scene are neither
+ *               used nor written.
+ *   rows_in     [device] [n_scenes][width - 1][c] of the rows' type: the rows in front of each scene, oldest first; NULL: zeros.
+ *   rows_out    [device] the same shape: the last width - 1 rows of each scene (rows_in's where it is shorter); may be NULL; not rows_in itself.
+ */
+int spc_causal_conv_forward(const void* x, int64_t ld_x, const float* weight, const float* bias, int32_t width, int32_t silu,
+                            const int32_t* offsets, int32_t n_scenes, const void* rows_in, void* y, int64_t ld_y,
+                            void* rows_out, int64_t n, int32_t c, int32_t dtype, void* stream);
+/*
+ * Its gradients.  drows_out: gradient of rows_out, may be NULL (zeros); dx overlaps no input; dweight, dbias [device] floats, overwritten, added up in a
+ * fixed order; drows_in: gradient of rows_in; not drows_out itself.  The last three may be NULL.  Scratch comes from the library's block cache (as for spc_conv_forward).
+ */
+int spc_causal_conv_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const float* weight, const float* bias,
+                             int32_t width, int32_t silu, const int32_t* offsets, int32_t n_scenes, const void* rows_in,
+                             const void* drows_out, void* dx, int64_t ld_dx, float* dweight, float* dbias, void* drows_in,
+                             int64_t n, int32_t c, int32_t dtype, void* stream);
+/* One more row of n independent streams: rows [device] [n][width - 1][c] (not read where width is 1) are the streams' last rows, updated in place. */
+int spc_causal_conv_step(const void* x, int64_t ld_x, const float* weight, const float* bias, int32_t width, int32_t silu,
+                         void* rows, void* y, int64_t ld_y, int64_t n, int32_t c, int32_t dtype, void* stream);
+
+/*
+ * Selective state space scan of every channel along the rows of its scene, with `states` states a channel:
+ *   d_t = dt_t + dt_bias, through ln(1 + exp(.)) with softplus;   h_t = exp(d_t A) h_{t-1} + d_t u_t B_t;
+ *   y_t = sum over states of C_t h_t + skip u_t;   out_t = y_t gate_t / (1 + exp(-gate_t)) with a gate, y_t without.
+ * channels / groups consecutive channels share a group's B and C.  States and sums are fp32 whatever the rows' type.  A decay near 1 is rounded to 24 bits a row: a
+ * state is off by at most 2^-25 for every row that it remembers, of those since its segment's start (at most 4096 rows; a step has no such rounding).
+ * At most 64 states, 65536 channels, 200000 scenes; scenes times channels times states below 2^31, those of a step's streams too (SPC_ERR_UNSUPPORTED above).
+ */
+typedef struct spc_scan_desc {
+  int32_t dtype;
+  int32_t n_scenes;
+  int64_t n_rows;
+  int32_t channels, groups, states;
+  int32_t softplus;
+} spc_scan_desc;
+/*
+ *   u, dt, gate, out  [device] rows of `channels` elements, row pitches in elements; gate may be NULL; out overlaps no input.
+ *   A           [device] channels x states floats, finite; usually below zero.
+ *   B, C        rows of `groups` heads of `states` elements (spc_attn_rows: row and group pitches, zero for a broadcast input).
+ *   skip, dt_bias  [device] `channels` floats, NULL: zeros.
+ *   offsets     as spc_linear_attention_forward's.  Rows in no scene are neither used nor written.
+ *   state_in    [device] [n_scenes][channels][states] floats, h before each scene's first row; NULL: zeros.
+ *   state_out   [device] the same shape, h behind each scene's last row (state_in for an empty scene); may be NULL; not state_in itself.
+ * An infinity or NaN in row t reaches rows from t on of its scene only, and of its channel (its group's channels from B and C); it may arrive as NaN.
+ * Results are bit-reproducible.  Scratch comes from the library's block cache (as for spc_conv_forward: a warmed-up call can be captured); nothing is waited for.
+ */
+int spc_selective_scan_forward(const spc_scan_desc* d, const void* u, int64_t ld_u, const void* dt, int64_t ld_dt, const float* A,
+                               const spc_attn_rows* B, const spc_attn_rows* C, const float* skip, const void* gate,
+                               int64_t ld_gate, const float* dt_bias, const int32_t* offsets, const float* state_in, void* out,
+                               int64_t ld_out, float* state_out, void* stream);
+/*
+ * Its gradients.  dout: gradient of out; the other inputs as in the forward pass; dstate_out: gradient of state_out, may be NULL (zeros).
+ *   du, ddt, dgate  [device] rows of `channels` elements (dgate only with a gate); dB, dC rows as B and C, summed over the channels that share them, every
+ *                   row and group at places of its own.  They overlap no input.  Rows in no scene are left alone.
+ *   dA, dskip, ddt_bias  [device] floats, any may be NULL; overwritten, added up in a fixed order (no atomics).
+ *   dstate_in       [device] gradient of state_in, may be NULL; not dstate_out itself.
+ */
+int spc_selective_scan_backward(const spc_scan_desc* d, const void* dout, int64_t ld_dout, const void* u, int64_t ld_u,
+                                const void* dt, int64_t ld_dt, const float* A, const spc_attn_rows* B, const spc_attn_rows* C,
+                                const float* skip, const void* gate, int64_t ld_gate, const float* dt_bias,
+                                const int32_t* offsets, const float* state_in, const float* dstate_out, void* du, int64_t ld_du,
+                                void* ddt, int64_t ld_ddt, float* dA, const spc_attn_rows* dB, const spc_attn_rows* dC,
+                                float* dskip, void* dgate, int64_t ld_dgate, float* ddt_bias, float* dstate_in, void* stream);
+/*
+ * One more row of n_rows independent streams (n_scenes is not read): row r belongs to stream r, whose state [n_rows][channels][states] floats [device] is
+ * updated in place.  out overlaps no input.
+ */
+int spc_selective_scan_step(const spc_scan_desc* d, const void* u, int64_t ld_u, const void* dt, int64_t ld_dt, const float* A,
+                            const spc_attn_rows* B, const spc_attn_rows* C, const float* skip, const void* gate, int64_t ld_gate,
+                            const float* dt_bias, float* state, void* out, int64_t ld_out, void* stream);
+
+/*
  * Measurement aids (Section 6 reports rates; these give the machine's own denominators next to the data-sheet
  * ones).  spc_probe_copy: a plain copy kernel, dst[0..bytes) = src[0..bytes) ([device], bytes a multiple of 16):
  * its rate is what a streaming kernel can reach on this GPU, and its known size calibrates the profiler's byte

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from collections import namedtuple
 
 import torch
 
@@ -46,6 +47,9 @@ EXPORTS = [
     "spc_conv_prepare_weights", "spc_permute_rows",
     "spc_layer_norm_forward", "spc_layer_norm_backward",
     "spc_linear_attention_forward", "spc_linear_attention_backward", "spc_linear_attention_step", "spc_batch_offsets",
+    "spc_rms_norm_forward", "spc_rms_norm_quantize", "spc_rms_norm_backward", "spc_quantize_rows", "spc_linear_f8",
+    "spc_causal_conv_forward", "spc_causal_conv_backward", "spc_causal_conv_step",
+    "spc_selective_scan_forward", "spc_selective_scan_backward", "spc_selective_scan_step",
     "spc_probe_copy", "spc_probe_mfma",
     "spc_release_cache", "spc_last_error", "spc_version",
 ]
@@ -80,6 +84,13 @@ class AttnDesc(ctypes.Structure):
 class AttnRows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("row_pitch", ctypes.c_int64), ("head_pitch", ctypes.c_int64)]
 
+
+class ScanDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_scenes", ctypes.c_int32), ("n_rows", ctypes.c_int64), ("channels", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("states", ctypes.c_int32), ("softplus", ctypes.c_int32)]
+
+
+ScanGradients = namedtuple("ScanGradients", "u dt A B C skip gate dt_bias initial")
 
 _lib = None
 
@@ -126,6 +137,19 @@ def lib():
         f32, ad, ar = ctypes.c_float, ctypes.POINTER(AttnDesc), ctypes.POINTER(AttnRows)
         L.spc_layer_norm_forward.argtypes = [vp, i64, vp, i64, vp, vp, f32, vp, i64, vp, i64, vp, vp, i64, i32, i32, vp]
         L.spc_layer_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, i64, i32, i32, vp]
+        L.spc_rms_norm_forward.argtypes = [vp, i64, vp, i64, vp, f32, vp, i64, vp, i64, vp, i64, i32, i32, vp]
+        L.spc_rms_norm_quantize.argtypes = [vp, i64, vp, i64, vp, f32, vp, i64, vp, vp, i64, vp, i64, i32, i32, vp]
+        L.spc_quantize_rows.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, vp]
+        L.spc_rms_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, i32, i32, vp]
+        L.spc_linear_f8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i64, i64, i32, i32, i32, vp]
+        L.spc_causal_conv_forward.argtypes = [vp, i64, vp, vp, i32, i32, vp, i32, vp, vp, i64, vp, i64, i32, i32, vp]
+        L.spc_causal_conv_backward.argtypes = [vp, i64, vp, i64, vp, vp, i32, i32, vp, i32, vp, vp, vp, i64, vp, vp, vp, i64, i32, i32, vp]
+        L.spc_causal_conv_step.argtypes = [vp, i64, vp, vp, i32, i32, vp, vp, i64, i64, i32, i32, vp]
+        sd = ctypes.POINTER(ScanDesc)
+        L.spc_selective_scan_forward.argtypes = [sd, vp, i64, vp, i64, vp, ar, ar, vp, vp, i64, vp, vp, vp, vp, i64, vp, vp]
+        L.spc_selective_scan_backward.argtypes = [sd, vp, i64, vp, i64, vp, i64, vp, ar, ar, vp, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp, ar, ar, vp, vp,
+                                                  i64, vp, vp, vp]
+        L.spc_selective_scan_step.argtypes = [sd, vp, i64, vp, i64, vp, ar, ar, vp, vp, i64, vp, vp, vp, i64, vp]
         L.spc_linear_attention_forward.argtypes = [ad, ar, ar, ar, vp, vp, vp, ar, vp, vp]
         L.spc_linear_attention_backward.argtypes = [ad, ar, ar, ar, ar, vp, vp, vp, vp, ar, ar, ar, vp, vp]
         L.spc_linear_attention_step.argtypes = [ad, ar, ar, ar, vp, vp, ar, vp]
@@ -578,6 +602,250 @@ def spc_linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     if rc:
         _check(rc)
     return out
+
+
+def _opt_rows(t: torch.Tensor | None, like: torch.Tensor):
+    """(address, row pitch) of an optional matrix of like's shape and type."""
+    return (None, 0) if t is None else (t.data_ptr(), _norm_rows(t, like))
+
+
+def _code(t: torch.Tensor) -> int:
+    code = _TORCH_DTYPE.get(t.dtype)
+    assert code is not None
+    return code
+
+
+def spc_rms_norm_forward(x: torch.Tensor, gamma: torch.Tensor | None = None, eps: float = 1e-5, residual: torch.Tensor | None = None,
+                         out: torch.Tensor | None = None, sum_out: torch.Tensor | None = None, want_stats: bool = False, stream=None):
+    """Root-mean-square norm of the rows of x [n, c] (+ residual); gamma [c] fp32.  Returns (y, sum, rstd): sum is None without a residual,
+    rstd [n] fp32 None without want_stats."""
+    (n, c), dev, code, ld = x.shape, x.device, _code(x), _norm_rows(x, x)
+    assert residual is not None or sum_out is None
+    r, ld_r = _opt_rows(residual, x)
+    y = torch.empty(n, c, dtype=x.dtype, device=dev) if out is None else out
+    total = torch.empty(n, c, dtype=x.dtype, device=dev) if residual is not None and sum_out is None else sum_out
+    rstd = torch.empty(n, dtype=torch.float32, device=dev) if want_stats else None
+    rc = lib().spc_rms_norm_forward(x.data_ptr(), ld, r, ld_r, _f32(gamma, (c,), dev), eps, y.data_ptr(), c if out is None else _norm_rows(out, x),
+                                    None if total is None else total.data_ptr(), c if sum_out is None else _norm_rows(sum_out, x),
+                                    rstd.data_ptr() if want_stats else None, n, c, code, current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return y, total, rstd
+
+
+def _bytes(q: torch.Tensor, n: int, c: int, dev) -> int:
+    """Row pitch of a matrix of e4m3 values."""
+    st = q.stride()
+    assert q.dtype == torch.float8_e4m3fn and q.shape == (n, c) and q.device == dev and q.is_cuda and (st[1] == 1 or c <= 1)
+    return st[0] if n > 1 else max(st[0], c)
+
+
+def spc_rms_norm_quantize(x: torch.Tensor, gamma: torch.Tensor | None = None, eps: float = 1e-5, residual: torch.Tensor | None = None,
+                          out: torch.Tensor | None = None, scale_out: torch.Tensor | None = None, sum_out: torch.Tensor | None = None,
+                          want_stats: bool = False, stream=None):
+    """The same norm with its output in 8 bits: returns (q [n, c] float8_e4m3fn, scale [n] fp32, sum, rstd), y being q times its row's scale."""
+    (n, c), dev, code, ld = x.shape, x.device, _code(x), _norm_rows(x, x)
+    assert residual is not None or sum_out is None
+    r, ld_r = _opt_rows(residual, x)
+    q = torch.empty(n, c, dtype=torch.float8_e4m3fn, device=dev) if out is None else out
+    scale = torch.empty(n, dtype=torch.float32, device=dev) if scale_out is None else scale_out
+    total = torch.empty(n, c, dtype=x.dtype, device=dev) if residual is not None and sum_out is None else sum_out
+    rstd = torch.empty(n, dtype=torch.float32, device=dev) if want_stats else None
+    rc = lib().spc_rms_norm_quantize(x.data_ptr(), ld, r, ld_r, _f32(gamma, (c,), dev), eps, q.data_ptr(), c if out is None else _bytes(out, n, c, dev),
+                                     _f32(scale, (n,), dev), None if total is None else total.data_ptr(),
+                                     c if sum_out is None else _norm_rows(sum_out, x), rstd.data_ptr() if want_stats else None, n, c, code,
+                                     current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return q, scale, total, rstd
+
+
+def spc_quantize_rows(x: torch.Tensor, out: torch.Tensor | None = None, scale_out: torch.Tensor | None = None, stream=None):
+    """Rows of x [n, c] in 8 bits: (q [n, c] float8_e4m3fn, scale [n] fp32).  Weights for spc_linear_f8 are quantised as [cout, cin]."""
+    (n, c), dev, code, ld = x.shape, x.device, _code(x), _norm_rows(x, x)
+    q = torch.empty(n, c, dtype=torch.float8_e4m3fn, device=dev) if out is None else out
+    scale = torch.empty(n, dtype=torch.float32, device=dev) if scale_out is None else scale_out
+    _check(lib().spc_quantize_rows(x.data_ptr(), ld, q.data_ptr(), _bytes(q, n, c, dev), _f32(scale, (n,), dev), n, c, code,
+                                   current_raw_stream() if stream is None else _stream(stream)))
+    return q, scale
+
+
+def spc_rms_norm_backward(dy: torch.Tensor, x: torch.Tensor, rstd: torch.Tensor, gamma: torch.Tensor | None = None, dsum: torch.Tensor | None = None,
+                          out: torch.Tensor | None = None, want_params: bool = True, stream=None):
+    """Gradients of spc_rms_norm_forward; x is its x, or its sum where there was a residual, dsum a gradient that reaches that sum past the
+    norm.  Returns (dx, dgamma), the latter [c] fp32, or None without want_params."""
+    (n, c), dev, code, ld = x.shape, x.device, _code(x), _norm_rows(x, x)
+    e, ld_e = _opt_rows(dsum, x)
+    dx = torch.empty(n, c, dtype=x.dtype, device=dev) if out is None else out
+    dgamma = torch.empty(c, dtype=torch.float32, device=dev) if want_params else None
+    rc = lib().spc_rms_norm_backward(dy.data_ptr(), _norm_rows(dy, x), x.data_ptr(), ld, _f32(rstd, (n,), dev), _f32(gamma, (c,), dev), e, ld_e,
+                                     dx.data_ptr(), c if out is None else _norm_rows(out, x), dgamma.data_ptr() if want_params else None, n, c, code,
+                                     current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return dx, dgamma
+
+
+def spc_linear_f8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
+                  out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """1x1x1 layer in 8 bits: x [n, cin] and w [cout, cin] float8_e4m3fn with a scale for each row (spc_rms_norm_quantize, spc_quantize_rows).
+    Returns [n, cout] of `dtype` (or of out's)."""
+    (n, c), (m, _), dev = x.shape, w.shape, x.device
+    if out is None:
+        out = torch.empty(n, m, dtype=dtype, device=dev)
+    assert out.shape == (n, m) and out.device == dev
+    rc = lib().spc_linear_f8(x.data_ptr(), _bytes(x, n, c, dev), _f32(x_scale, (n,), dev), w.data_ptr(), _bytes(w, m, c, dev), _f32(w_scale, (m,), dev),
+                             out.data_ptr(), _norm_rows(out, out), n, c, m, _code(out), current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return out
+
+
+def _scenes_of(offsets: torch.Tensor | None, dev):
+    """(number of scenes, address of their offsets)."""
+    if offsets is None:
+        return 1, None
+    assert offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.is_contiguous() and offsets.device == dev
+    return offsets.shape[0] - 1, offsets.data_ptr()
+
+
+def _past(t: torch.Tensor | None, shape, like: torch.Tensor) -> int | None:
+    """Address of optional contiguous rows in front of scenes or streams, of like's type."""
+    if t is None:
+        return None
+    assert t.shape == shape and t.dtype == like.dtype and t.device == like.device and t.is_contiguous()
+    return t.data_ptr()
+
+
+def spc_causal_conv_forward(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None, offsets: torch.Tensor | None = None,
+                            silu: bool = True, initial_rows: torch.Tensor | None = None, want_rows: bool = False, out: torch.Tensor | None = None,
+                            rows_out: torch.Tensor | None = None, stream=None):
+    """Short causal convolution of every channel of x [n, c] along the rows of its scene, through x / (1 + exp(-x)) with silu; weight [c, width] (the
+    row itself last) and bias [c] fp32; offsets [scenes + 1] int32 (spc_batch_offsets), None: one scene.  initial_rows [scenes, width - 1, c] of x's
+    type: the rows in front of each scene.  Returns (y [n, c], every scene's last width - 1 rows or None)."""
+    (n, c), dev, code, ld = x.shape, x.device, _code(x), _norm_rows(x, x)
+    width, (scenes, at) = weight.shape[1], _scenes_of(offsets, dev)
+    shape = (scenes, width - 1, c)
+    y = torch.empty(n, c, dtype=x.dtype, device=dev) if out is None else out
+    if rows_out is None and want_rows:
+        rows_out = torch.empty(shape, dtype=x.dtype, device=dev)
+    rc = lib().spc_causal_conv_forward(x.data_ptr(), ld, _f32(weight, (c, width), dev), _f32(bias, (c,), dev), width, bool(silu), at, scenes,
+                                       _past(initial_rows, shape, x), y.data_ptr(), c if out is None else _norm_rows(out, x),
+                                       _past(rows_out, shape, x), n, c, code, current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return y, rows_out
+
+
+def spc_causal_conv_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None, offsets: torch.Tensor | None = None,
+                             silu: bool = True, initial_rows: torch.Tensor | None = None, drows: torch.Tensor | None = None, want_params: bool = True,
+                             want_dinitial: bool = False, out: torch.Tensor | None = None, stream=None):
+    """Gradients of spc_causal_conv_forward; drows: gradient of the rows it returned.  Returns (dx, dweight, dbias, gradient of initial_rows), the
+    second and third None without want_params, the last without want_dinitial."""
+    (n, c), dev, code, ld = x.shape, x.device, _code(x), _norm_rows(x, x)
+    width, (scenes, at) = weight.shape[1], _scenes_of(offsets, dev)
+    shape = (scenes, width - 1, c)
+    dx = torch.empty(n, c, dtype=x.dtype, device=dev) if out is None else out
+    dweight = torch.empty(c, width, dtype=torch.float32, device=dev) if want_params else None
+    dbias = torch.empty(c, dtype=torch.float32, device=dev) if want_params else None
+    dinitial = torch.empty(shape, dtype=x.dtype, device=dev) if want_dinitial else None
+    rc = lib().spc_causal_conv_backward(dy.data_ptr(), _norm_rows(dy, x), x.data_ptr(), ld, _f32(weight, (c, width), dev), _f32(bias, (c,), dev), width,
+                                        bool(silu), at, scenes, _past(initial_rows, shape, x), _past(drows, shape, x), dx.data_ptr(),
+                                        c if out is None else _norm_rows(out, x), dweight.data_ptr() if want_params else None,
+                                        dbias.data_ptr() if want_params else None, dinitial.data_ptr() if want_dinitial else None, n, c, code,
+                                        current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return dx, dweight, dbias, dinitial
+
+
+def spc_causal_conv_step(x: torch.Tensor, weight: torch.Tensor, rows: torch.Tensor, bias: torch.Tensor | None = None, silu: bool = True,
+                         out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """One more row x [streams, c] of every stream; rows [streams, width - 1, c], the streams' last ones, are updated in place."""
+    (n, c), dev, code, ld = x.shape, x.device, _code(x), _norm_rows(x, x)
+    width = weight.shape[1]
+    y = torch.empty(n, c, dtype=x.dtype, device=dev) if out is None else out
+    rc = lib().spc_causal_conv_step(x.data_ptr(), ld, _f32(weight, (c, width), dev), _f32(bias, (c,), dev), width, bool(silu),
+                                    _past(rows, (n, width - 1, c), x), y.data_ptr(), c if out is None else _norm_rows(out, x), n, c, code,
+                                    current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return y
+
+
+def _scan(u, dt, A, b, c, skip, gate, dt_bias, offsets, softplus):
+    """What the scan's calls share: (descriptor, arguments from u to dt_bias in C form, offsets' address)."""
+    n, channels = u.shape
+    groups, states = b.shape[1], A.shape[1]
+    dev = u.device
+    scenes, at = _scenes_of(offsets, dev)
+    d = ScanDesc(_code(u), scenes, n, channels, groups, states, bool(softplus))
+    z, ld_z = _opt_rows(gate, u)
+    return d, (u.data_ptr(), _norm_rows(u, u), dt.data_ptr(), _norm_rows(dt, u), _f32(A, (channels, states), dev), _heads(b, n, groups, states, u.dtype, dev),
+               _heads(c, n, groups, states, u.dtype, dev), _f32(skip, (channels,), dev), z, ld_z, _f32(dt_bias, (channels,), dev)), at
+
+
+def spc_selective_scan_forward(u: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor, skip: torch.Tensor | None = None,
+                               gate: torch.Tensor | None = None, dt_bias: torch.Tensor | None = None, offsets: torch.Tensor | None = None,
+                               softplus: bool = True, initial_state: torch.Tensor | None = None, want_state: bool = False,
+                               out: torch.Tensor | None = None, state_out: torch.Tensor | None = None, stream=None):
+    """Selective scan along every scene's rows: u, dt, gate [n, channels], B, C [n, groups, states] (any row and group pitch, e.g. column ranges of one
+    projection's output); A [channels, states], skip and dt_bias [channels] fp32; step sizes dt + dt_bias, through ln(1 + exp) with softplus; offsets
+    [scenes + 1] int32 (spc_batch_offsets), None: one scene; states [scenes, channels, states] fp32.  Returns (out [n, channels], state behind
+    every scene's last row, or None)."""
+    d, args, at = _scan(u, dt, A, B, C, skip, gate, dt_bias, offsets, softplus)
+    dev = u.device
+    shape = (d.n_scenes, d.channels, d.states)
+    y = torch.empty(d.n_rows, d.channels, dtype=u.dtype, device=dev) if out is None else out
+    if state_out is None and want_state:
+        state_out = torch.empty(shape, dtype=torch.float32, device=dev)
+    rc = lib().spc_selective_scan_forward(d, *args, at, _f32(initial_state, shape, dev), y.data_ptr(), d.channels if out is None else _norm_rows(out, u),
+                                          _f32(state_out, shape, dev), current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return y, state_out
+
+
+def spc_selective_scan_backward(dout: torch.Tensor, u: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor,
+                                skip: torch.Tensor | None = None, gate: torch.Tensor | None = None, dt_bias: torch.Tensor | None = None,
+                                offsets: torch.Tensor | None = None, softplus: bool = True, initial_state: torch.Tensor | None = None,
+                                dstate: torch.Tensor | None = None, want_dinitial: bool = False, out=None, stream=None) -> ScanGradients:
+    """Gradients of spc_selective_scan_forward; dstate: gradient of the state it returned.  out: (du, ddt, dB, dC, dgate or None) to write to.  Returns
+    ScanGradients; skip, gate and dt_bias have none where they were None, initial without want_dinitial."""
+    d, args, at = _scan(u, dt, A, B, C, skip, gate, dt_bias, offsets, softplus)
+    dev, n, ch = u.device, d.n_rows, d.channels
+    shape = (d.n_scenes, ch, d.states)
+    if out is None:
+        rows = lambda: torch.empty(n, ch, dtype=u.dtype, device=dev)  # noqa: E731
+        low = lambda: torch.empty(n, d.groups, d.states, dtype=u.dtype, device=dev)  # noqa: E731
+        out = (rows(), rows(), low(), low(), None if gate is None else rows())
+    du, ddt, dB, dC, dgate = out
+    assert (dgate is None) == (gate is None)
+    z, ld_z = _opt_rows(dgate, u)
+    f32 = lambda t, *s: torch.empty(s, dtype=torch.float32, device=dev) if t else None  # noqa: E731
+    dA, dskip, dbias, dinitial = f32(True, ch, d.states), f32(skip is not None, ch), f32(dt_bias is not None, ch), f32(want_dinitial, *shape)
+    address = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    rc = lib().spc_selective_scan_backward(d, dout.data_ptr(), _norm_rows(dout, u), *args, at, _f32(initial_state, shape, dev), _f32(dstate, shape, dev),
+                                           du.data_ptr(), _norm_rows(du, u), ddt.data_ptr(), _norm_rows(ddt, u), dA.data_ptr(),
+                                           _heads(dB, n, d.groups, d.states, u.dtype, dev), _heads(dC, n, d.groups, d.states, u.dtype, dev), address(dskip), z, ld_z,
+                                           address(dbias), address(dinitial), current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return ScanGradients(du, ddt, dA, dB, dC, dskip, dgate, dbias, dinitial)
+
+
+def spc_selective_scan_step(u: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor, state: torch.Tensor,
+                            skip: torch.Tensor | None = None, gate: torch.Tensor | None = None, dt_bias: torch.Tensor | None = None,
+                            softplus: bool = True, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """One more row for every stream: u [streams, channels] and so on; state [streams, channels, states] fp32 is updated in place."""
+    d, args, _ = _scan(u, dt, A, B, C, skip, gate, dt_bias, None, softplus)
+    y = torch.empty(d.n_rows, d.channels, dtype=u.dtype, device=u.device) if out is None else out
+    assert state is not None
+    rc = lib().spc_selective_scan_step(d, *args, _f32(state, (d.n_rows, d.channels, d.states), u.device), y.data_ptr(),
+                                       d.channels if out is None else _norm_rows(out, u), current_raw_stream() if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return y
 
 
 def spc_batch_offsets(keys: torch.Tensor, desc: PackDesc, n_batch: int, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:

@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspc.so")
-SOURCES = ["runtime.hip", "pack_sort.hip", "bucket_sort.hip", "kmap.hip", "conv.hip", "norm.hip", "attention.hip", "probe.hip"]
+SOURCES = ["runtime.hip", "pack_sort.hip", "bucket_sort.hip", "kmap.hip", "conv.hip", "norm.hip", "attention.hip", "linear8.hip", "causal_conv.hip",
+           "selective_scan.hip", "probe.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -22,7 +23,8 @@ def build(force: bool = True, verbose: bool = False) -> str:
     os.makedirs(objdir, exist_ok=True)
     hdrs = [os.path.join(CSRC, "spc_internal.h"), os.path.join(ROOT, "include", "spc.h")]
     newest_hdr = max(os.path.getmtime(h) for h in hdrs)
-    own_hdrs = {"conv.hip": ["conv_common.h", "conv_resident.h"], "norm.hip": ["rows.h"], "attention.hip": ["rows.h"]}  # read by some sources only
+    own_hdrs = {"conv.hip": ["conv_common.h", "conv_resident.h"], "norm.hip": ["rows.h"], "attention.hip": ["rows.h"], "linear8.hip": ["rows.h"],
+                "causal_conv.hip": ["rows.h", "scenes.h"], "selective_scan.hip": ["rows.h", "scenes.h"]}  # read by some sources only
     objs, procs = [], []
     for src in SOURCES:
         s = os.path.join(CSRC, src)

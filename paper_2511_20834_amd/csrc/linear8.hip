@@ -1,0 +1,196 @@
+// 1x1x1 layers in 8 bits: rows and weights of e4m3 values with a scale each.
+//
+//   out[r, j] = sx[r] sw[j] sum_k x[r, k] w[j, k]
+//
+// The values become fp16 on their way to the matrix cores, which holds each of them exactly, as do 32 bits each product; sums are held in 32 bits, the scales come behind, one
+// rounding to the output's type.  (The matrix cores' products of 8-bit operands line up their terms in fewer bits: 2^-13.5 of the sum of magnitudes off at 128 places
+// of values from all binades, 2^-22.8 so.  They would be twice as fast, which bytes leave no use for: 120 k x 256 -> 1024 moves 277 MB for 63 GFLOP.)
+// A workgroup holds 128 rows in its waves' registers where their channels fit, so x is read once, and walks over the columns in tiles of 64, whose weights
+// all four waves read from LDS.  The weights are the product's left operand and a tile's lines are dealt to its four 16 x 16 products so that a lane ends up with 16
+// consecutive columns of one output row: whole lines are stored, 128 bytes a row and wave in 16 bits.
+#include <algorithm>
+#include <type_traits>
+
+#include "rows.h"
+
+namespace spc {
+namespace {
+
+constexpr int LIN_COLS = 64, LIN_K = 64;  // a tile of weights: columns, places of each
+constexpr int LIN_THREADS = 256, LIN_GROUPS = 2;  // groups of 16 rows a wave
+constexpr int LIN_MAX_C = 65536;
+
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+struct LinearArgs {
+  const uint8_t *x, *w;
+  const float *sx, *sw;
+  void* out;
+  int64_t ld_x, ld_w, ld_out, n;
+  int c, cout, tiles;  // tiles: column tiles of a workgroup
+};
+
+// 16 bytes of a row of c from place k on, zeros behind its end.  WHOLE: c is a multiple of 16.
+template <bool WHOLE>
+__device__ inline Words4 piece16(const uint8_t* row, int k, int c) {
+  typedef int Any __attribute__((ext_vector_type(4), aligned(1), may_alias));
+  Words4 v = {0, 0, 0, 0};
+  const int left = c - k;
+  if (left >= 16) {
+    v = *reinterpret_cast<const Any*>(row + k);
+  } else if (!WHOLE && left > 0) {
+#pragma unroll
+    for (int i = 0; i < 15; ++i)
+      if (i < left) v[i / 4] |= int(row[k + i]) << (i % 4 * 8);
+  }
+  return v;
+}
+__device__ inline void to_halves(Words4 v, half8 (&f)[2]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const half2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[q], 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[q], 1.f, true);
+    f[q / 2][q % 2 * 4] = a[0], f[q / 2][q % 2 * 4 + 1] = a[1], f[q / 2][q % 2 * 4 + 2] = b[0], f[q / 2][q % 2 * 4 + 3] = b[1];
+  }
+}
+
+// KT: tiles of 64 places that a wave's rows are held in (0: they are read again for every tile of columns).  Lane l has row (column) l % 16 of every operand and 16 places of a
+// tile's 64 from 16 (l / 16) on, in two products of 32; of a result column l % 16 and rows 4 (l / 16) + r.
+template <typename T, int KT, bool WHOLE>
+__global__ __launch_bounds__(LIN_THREADS) void linear8_kernel(const LinearArgs a) {
+  constexpr int RT = LIN_GROUPS;
+  __shared__ half8 tile[2][LIN_COLS * LIN_K / 8];
+  const int t = threadIdx.x, lane = t % 64, wave = t / 64, i = lane % 16, g = lane / 16;
+  const int all = (a.cout + LIN_COLS - 1) / LIN_COLS, splits = (all + a.tiles - 1) / a.tiles, n_kt = (a.c + LIN_K - 1) / LIN_K;
+  const int64_t block = blockIdx.x / splits;
+  const int first_tile = blockIdx.x % splits * a.tiles, last_tile = min(first_tile + a.tiles, all);
+  const int64_t row0 = (block * 4 + wave) * (16 * RT) + i;  // of group 0; the lane's row of group q is 16 q further
+  // this thread's part of a tile of weights, 16 places of a line; line 16 q + m of the tile in LDS is column 16 (m / 4) + 4 q + m % 4, its pieces of 8 are turned by its number
+  const int line = t / 4, line_col = line % 16 / 4 * 16 + line / 16 * 4 + line % 4;
+  auto stage = [&](int ct, int kt) {
+    const int col = ct * LIN_COLS + line_col;
+    return col < a.cout ? piece16<WHOLE>(a.w + int64_t(col) * a.ld_w, kt * LIN_K + t % 4 * 16, a.c) : Words4{0, 0, 0, 0};
+  };
+  auto rows = [&](int kt, half8 (&f)[RT][2]) {
+#pragma unroll
+    for (int q = 0; q < RT; ++q) {
+      Words4 v = {0, 0, 0, 0};
+      if (row0 + 16 * q < a.n) v = piece16<WHOLE>(a.x + (row0 + 16 * q) * a.ld_x, kt * LIN_K + 16 * g, a.c);
+      to_halves(v, f[q]);
+    }
+  };
+  half8 held[KT ? KT : 1][RT][2];
+  if constexpr (KT > 0)
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) rows(kt, held[kt]);
+  float sx[RT];
+#pragma unroll
+  for (int q = 0; q < RT; ++q) sx[q] = row0 + 16 * q < a.n ? a.sx[row0 + 16 * q] : 0.f;
+  Words4 next = stage(first_tile, 0);
+  int buf = 0;
+  for (int ct = first_tile; ct < last_tile; ++ct) {
+    floatx4 acc[RT][4];
+#pragma unroll
+    for (int q = 0; q < RT; ++q)
+#pragma unroll
+      for (int m = 0; m < 4; ++m) acc[q][m] = floatx4{0.f, 0.f, 0.f, 0.f};
+    auto step = [&](int kt, const half8 (&f)[RT][2]) {
+      half8 w[2];
+      to_halves(next, w);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) tile[buf][line * 8 + ((t % 4 * 2 + p) ^ line % 8)] = w[p];
+      // (one barrier a tile: whoever stores to a buffer again has passed the barrier behind its last reads, since there are two)
+      __syncthreads();
+      if (kt + 1 < n_kt) next = stage(ct, kt + 1);
+      else if (ct + 1 < last_tile) next = stage(ct + 1, 0);
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const int from = 16 * m + i;
+          const half8 v = tile[buf][from * 8 + ((2 * g + p) ^ from % 8)];
+#pragma unroll
+          for (int q = 0; q < RT; ++q) acc[q][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, f[q][p], acc[q][m], 0, 0, 0);
+        }
+      buf ^= 1;
+    };
+    if constexpr (KT > 0) {
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+        if (kt < n_kt) step(kt, held[kt]);
+    } else {
+      for (int kt = 0; kt < n_kt; ++kt) {
+        half8 f[RT][2];
+        rows(kt, f);
+        step(kt, f);
+      }
+    }
+    const int col = ct * LIN_COLS + 16 * g, left = a.cout - col;
+    float sw[16];
+#pragma unroll
+    for (int m = 0; m < 16; ++m) sw[m] = m < left ? a.sw[col + m] : 0.f;
+#pragma unroll
+    for (int q = 0; q < RT; ++q) {
+      if (row0 + 16 * q >= a.n) continue;
+      T* to = static_cast<T*>(a.out) + (row0 + 16 * q) * a.ld_out + col;
+      constexpr int VEC = 16 / sizeof(T);
+      typedef T Values __attribute__((ext_vector_type(VEC)));
+#pragma unroll
+      for (int p = 0; p < 16 / VEC; ++p) {
+        Values v;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) v[k] = static_cast<T>(acc[q][(p * VEC + k) / 4][k % 4] * sx[q] * sw[p * VEC + k]);
+        if ((p + 1) * VEC <= left) {
+          *reinterpret_cast<AnyWords4*>(to + p * VEC) = __builtin_bit_cast(Words4, v);
+        } else {
+#pragma unroll
+          for (int k = 0; k < VEC; ++k)
+            if (p * VEC + k < left) to[p * VEC + k] = v[k];
+        }
+      }
+    }
+  }
+}
+
+}  // namespace
+}  // namespace spc
+
+extern "C" int spc_linear_f8(const void* x, int64_t ld_x, const float* x_scale, const void* w, int64_t ld_w, const float* w_scale, void* out, int64_t ld_out,
+                             int64_t n, int32_t c, int32_t cout, int32_t dtype, void* stream) {
+  using namespace spc;
+  if (dtype != SPC_DTYPE_F16 && dtype != SPC_DTYPE_BF16 && dtype != SPC_DTYPE_F32) return set_error(SPC_ERR_ARG, "unknown dtype %d", dtype);
+  if (n < 0 || c < 1 || cout < 1) return set_error(SPC_ERR_ARG, "n = %lld, c = %d, cout = %d", static_cast<long long>(n), c, cout);
+  if (c > LIN_MAX_C || cout > LIN_MAX_C || n > (int64_t(1) << 30))  // (a launch takes less than 2^32 threads, 256 of them to 128 rows)
+    return set_error(SPC_ERR_UNSUPPORTED, "%lld rows of %d channels to %d: at most 2^30 and %d", static_cast<long long>(n), c, cout, LIN_MAX_C);
+  if (!n) return SPC_OK;
+  if (!x || !w || !out || !x_scale || !w_scale) return set_error(SPC_ERR_ARG, "NULL argument");
+  if (ld_x < c || ld_w < c || ld_out < cout)
+    return set_error(SPC_ERR_ARG, "row pitches %lld, %lld, %lld are below %d, %d, %d", static_cast<long long>(ld_x), static_cast<long long>(ld_w), static_cast<long long>(ld_out),
+                     c, c, cout);
+  if (reinterpret_cast<uintptr_t>(out) % (dtype == SPC_DTYPE_F32 ? 4 : 2)) return set_error(SPC_ERR_ARG, "out is not aligned to its type");
+  LinearArgs a{static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(w), x_scale, w_scale, out, ld_x, ld_w, ld_out, n, c, cout, 1};
+  const int all = (cout + LIN_COLS - 1) / LIN_COLS;
+  constexpr int ROWS = 64 * LIN_GROUPS;
+  const int64_t blocks = (n + ROWS - 1) / ROWS;
+  // columns are split between workgroups until there are some 1024 of them
+  const int splits = static_cast<int>(std::min<int64_t>(all, std::max<int64_t>(1, 1024 / blocks)));
+  a.tiles = (all + splits - 1) / splits;
+  by_dtype(dtype, [&](auto type) {
+    auto go = [&](auto kt, auto whole) {
+      hipLaunchKernelGGL((linear8_kernel<decltype(type), decltype(kt)::value, decltype(whole)::value>), dim3(blocks * ((all + a.tiles - 1) / a.tiles)), dim3(LIN_THREADS), 0,
+                         static_cast<hipStream_t>(stream), a);
+    };
+    auto with = [&](auto kt) {
+      if (c % 16 == 0) go(kt, std::true_type{});
+      else go(kt, std::false_type{});
+    };
+    using std::integral_constant;
+    if (c <= 64) with(integral_constant<int, 1>{});
+    else if (c <= 128) with(integral_constant<int, 2>{});
+    else if (c <= 256) with(integral_constant<int, 4>{});
+    else with(integral_constant<int, 0>{});
+  });
+  SPC_HIP_CHECK(hipGetLastError());
+  return SPC_OK;
+}

@@ -1,4 +1,4 @@
-// Layer norm of feature rows, forward and backward.
+// Layer norm and root-mean-square norm of feature rows, forward and backward, the latter's rows also in 8 bits.
 //
 //   z = x + r,  mu = mean(z),  s = 1/sqrt(mean((z - mu)^2) + eps),  h = (z - mu) s,  y = h gamma + beta
 //   w = gamma dy,  dz = s (w - mean(w) - h mean(w h)) + e,  dgamma = sum over rows of dy h,  dbeta = sum over rows of dy
@@ -36,6 +36,20 @@ __device__ inline float row_sum(float v, float* lds) {
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
     __syncthreads();
     v = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+  }
+  return v;
+}
+
+// The largest over them (values are no less than zero, NaN aside, which is passed over).
+template <int G>
+__device__ inline float row_max(float v, float* lds) {
+#pragma unroll
+  for (int d = (G < 64 ? G : 64) / 2; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
+  if constexpr (G > 64) {
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
   }
   return v;
 }
@@ -98,6 +112,27 @@ struct Row {
           if (first + k < c) at[first + k] = q[k];
       } else if (has(i)) {
         *reinterpret_cast<AnyWords4*>(at + place(i)) = __builtin_bit_cast(Words4, q);
+      }
+    }
+  }
+  // (rounded to nearest, ties to even)
+  __device__ void store_bytes(const float (&f)[E], void* p, int64_t row, int64_t ld) const {
+    uint8_t* at = static_cast<uint8_t*>(p) + row * ld;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      int q[VEC / 4];
+#pragma unroll
+      for (int k = 0; k < VEC / 4; ++k) {
+        const float* v = f + i * VEC + 4 * k;
+        q[k] = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), true);
+      }
+      if (FIT == FEW) {
+#pragma unroll
+        for (int k = 0; k < VEC - 1; ++k)
+          if (first + k < c) at[first + k] = static_cast<uint8_t>(q[k / 4] >> (k % 4 * 8));
+      } else if (has(i)) {
+        if constexpr (VEC == 8) *reinterpret_cast<AnyBytes8*>(at + place(i)) = Words2{q[0], q[1]};
+        else *reinterpret_cast<AnyBytes4*>(at + place(i)) = q[0];
       }
     }
   }
@@ -249,6 +284,127 @@ __global__ __launch_bounds__(1024) void norm_params_kernel(const float* __restri
   if (to) to[col < c ? col : col - c] = s;
 }
 
+// Root-mean-square norm: z = x + r, s = 1/sqrt(mean(z^2) + eps), y = z s gamma; or y in 8 bits: a = the row's largest |y|, q = e4m3(y 448 / a), scale = a / 448,
+// so that q scale is y.  BARE: the rows themselves in 8 bits.
+enum Form { SAME, BYTES, BARE_BYTES };
+constexpr float F8_MOST = 448.f;              // e4m3's largest value
+constexpr float F8_LEAST = 0x1p-100f;         // rows below this are scaled as if it were their largest value: 448 / a stays finite, zeros stay zeros
+
+struct RmsArgs {
+  const void *x, *r, *dy, *e;
+  const float *gamma, *rstd_in;
+  void *y, *z;
+  float *scale, *rstd, *partial;
+  int64_t ld_x, ld_r, ld_dy, ld_e, ld_y, ld_z, n;
+  int c;
+  float eps;
+};
+
+template <typename T, int NV, int G, Fit FIT, Form FORM>
+__global__ __launch_bounds__(NORM_THREADS) void rms_forward_kernel(const RmsArgs a) {
+  using R = Row<T, NV, G, FIT>;
+  constexpr int ROWS = NORM_THREADS / G;
+  __shared__ float lds[4];
+  const R me(a.c);
+  float gamma[R::E];
+  if (FORM != BARE_BYTES) me.load_param(gamma, a.gamma, 1.f);
+  const float c = a.c;
+  for (int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / G; row < a.n; row += int64_t(gridDim.x) * ROWS) {
+    float z[R::E];
+    me.load(z, a.x, row, a.ld_x);
+    if (FORM != BARE_BYTES) {
+      if (a.r) {
+        float r[R::E];
+        me.load(r, a.r, row, a.ld_r);
+#pragma unroll
+        for (int k = 0; k < R::E; ++k) z[k] += r[k];
+        if (G > 64 && FIT == MOVED) __syncthreads();  // (z may lie over x or r: another wave's piece is read here too)
+        me.store(z, a.z, row, a.ld_z);  // (the norm goes on with the sum as it was before this rounding)
+      }
+      float s = 0.f;
+#pragma unroll
+      for (int k = 0; k < R::E; ++k) s += FIT != MOVED || me.counts(k) ? z[k] * z[k] : 0.f;  // (places behind the last channel hold zeros)
+      const float rstd = 1.f / sqrtf(row_sum<G>(s, lds) / c + a.eps);
+#pragma unroll
+      for (int k = 0; k < R::E; ++k) z[k] = z[k] * rstd * gamma[k];
+      if (threadIdx.x % G == 0 && a.rstd) a.rstd[row] = rstd;
+    }
+    if (FORM == SAME) {
+      me.store(z, a.y, row, a.ld_y);
+    } else {
+      float top = F8_LEAST;
+#pragma unroll
+      for (int k = 0; k < R::E; ++k) top = fmaxf(top, fabsf(z[k]));
+      top = row_max<G>(top, lds);
+      const float up = F8_MOST / top;
+#pragma unroll
+      for (int k = 0; k < R::E; ++k) z[k] *= up;
+      me.store_bytes(z, a.y, row, a.ld_y);
+      if (threadIdx.x % G == 0) a.scale[row] = top / F8_MOST;
+    }
+  }
+}
+
+// h = z s, w = gamma dy:  dz = s (w - h mean(w h)) + e,  dgamma = sum over rows of dy h
+template <typename T, int NV, int G, Fit FIT>
+__global__ __launch_bounds__(NORM_THREADS) void rms_backward_kernel(const RmsArgs a) {
+  using R = Row<T, NV, G, FIT>;
+  constexpr int ROWS = NORM_THREADS / G;
+  __shared__ float lds[4];
+  extern __shared__ float sums[];  // G <= 64: c floats
+  const R me(a.c);
+  float gamma[R::E], dgamma[R::E] = {};
+  me.load_param(gamma, a.gamma, 1.f);
+  const float c = a.c;
+  for (int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / G; row < a.n; row += int64_t(gridDim.x) * ROWS) {
+    float h[R::E], dy[R::E];
+    me.load(h, a.x, row, a.ld_x);
+    me.load(dy, a.dy, row, a.ld_dy);
+    const float rstd = a.rstd_in[row];
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < R::E; ++k) {
+      h[k] = (FIT == FEW ? me.counts(k) : me.has(k / R::VEC)) ? h[k] * rstd : 0.f;  // (rstd may be infinite where there is no channel)
+      dgamma[k] = fmaf(dy[k], h[k], dgamma[k]);
+      dy[k] *= gamma[k];
+      s += FIT != MOVED || me.counts(k) ? dy[k] * h[k] : 0.f;
+    }
+    s = row_sum<G>(s, lds) / c;
+    if (a.e) {
+      float e[R::E];
+      me.load(e, a.e, row, a.ld_e);
+#pragma unroll
+      for (int k = 0; k < R::E; ++k) dy[k] = fmaf(rstd, dy[k] - h[k] * s, e[k]);
+      if (G > 64 && FIT == MOVED) __syncthreads();  // (dx may lie over e)
+    } else {
+#pragma unroll
+      for (int k = 0; k < R::E; ++k) dy[k] = rstd * (dy[k] - h[k] * s);
+    }
+    me.store(dy, a.y, row, a.ld_y);
+  }
+  if (!a.partial) return;
+  float* out = a.partial + int64_t(blockIdx.x) * a.c;
+  if constexpr (G <= 64) {
+    // the rows of a wave, then the waves one after the other
+#pragma unroll
+    for (int k = 0; k < R::E; ++k)
+#pragma unroll
+      for (int d = G; d < 64; d <<= 1) dgamma[k] += __shfl_xor(dgamma[k], d, 64);
+    for (int w = 0; w < NORM_THREADS / 64; ++w) {
+      if (int(threadIdx.x) / 64 == w && threadIdx.x % 64 < G)
+#pragma unroll
+        for (int k = 0; k < R::E; ++k)
+          if (me.counts(k)) sums[me.channel(k)] = w ? sums[me.channel(k)] + dgamma[k] : dgamma[k];
+      __syncthreads();
+    }
+    for (int i = threadIdx.x; i < a.c; i += NORM_THREADS) out[i] = sums[i];
+  } else {
+#pragma unroll
+    for (int k = 0; k < R::E; ++k)
+      if (me.counts(k)) out[me.channel(k)] = dgamma[k];
+  }
+}
+
 int norm_check(int64_t n, int32_t c, int32_t dtype) {
   if (dtype != SPC_DTYPE_F16 && dtype != SPC_DTYPE_BF16 && dtype != SPC_DTYPE_F32) return set_error(SPC_ERR_ARG, "unknown dtype %d", dtype);
   if (n < 0 || c < 1) return set_error(SPC_ERR_ARG, "n = %lld, c = %d", static_cast<long long>(n), c);
@@ -318,8 +474,96 @@ void norm_backward(const NormArgs& a, int wgs, hipStream_t s) {
   });
 }
 
+template <Form FORM>
+void rms_forward(const RmsArgs& a, int32_t dtype, hipStream_t s) {
+  const int wgs = norm_grid(dtype, a.c, a.n, false);
+  by_dtype(dtype, [&](auto t) {
+    norm_shape<decltype(t)>(a.c, [&](auto nv, auto g, auto fit) {
+      hipLaunchKernelGGL((rms_forward_kernel<decltype(t), decltype(nv)::value, decltype(g)::value, decltype(fit)::value, FORM>), dim3(wgs), dim3(NORM_THREADS), 0, s, a);
+    });
+  });
+}
+
+// What the two root-mean-square forward passes share.
+int rms_call(const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const float* gamma, float eps, void* y, int64_t ld_y, bool bytes, float* scale, void* sum,
+             int64_t ld_s, float* rstd, int64_t n, int32_t c, int32_t dtype, void* stream) {
+  SPC_RETURN_IF(norm_check(n, c, dtype));
+  const int es = dtype == SPC_DTYPE_F32 ? 4 : 2;
+  SPC_RETURN_IF(norm_check_rows("x", x, ld_x, c, es, n == 0));
+  SPC_RETURN_IF(norm_check_rows("y", y, ld_y, c, bytes ? 1 : es, n == 0));
+  SPC_RETURN_IF(norm_check_rows("residual", residual, ld_r, c, es, true));
+  SPC_RETURN_IF(norm_check_rows("sum", sum, ld_s, c, es, true));
+  if (!(eps > 0.f && eps < 3.4e38f)) return set_error(SPC_ERR_ARG, "eps must be positive and finite");
+  if (n && !residual != !sum) return set_error(SPC_ERR_ARG, "residual and sum come together");
+  if (n && bytes && !scale) return set_error(SPC_ERR_ARG, "scale is NULL");
+  if (!n) return SPC_OK;
+  RmsArgs a{};
+  a.x = x, a.ld_x = ld_x, a.r = residual, a.ld_r = ld_r, a.gamma = gamma, a.eps = eps, a.y = y, a.ld_y = ld_y, a.z = sum, a.ld_z = ld_s;
+  a.scale = scale, a.rstd = rstd, a.n = n, a.c = c;
+  if (bytes) rms_forward<BYTES>(a, dtype, static_cast<hipStream_t>(stream));
+  else rms_forward<SAME>(a, dtype, static_cast<hipStream_t>(stream));
+  SPC_HIP_CHECK(hipGetLastError());
+  return SPC_OK;
+}
+
 }  // namespace
 }  // namespace spc
+
+extern "C" int spc_rms_norm_forward(const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const float* gamma, float eps, void* y, int64_t ld_y, void* sum,
+                                    int64_t ld_s, float* rstd, int64_t n, int32_t c, int32_t dtype, void* stream) {
+  return spc::rms_call(x, ld_x, residual, ld_r, gamma, eps, y, ld_y, false, nullptr, sum, ld_s, rstd, n, c, dtype, stream);
+}
+
+extern "C" int spc_rms_norm_quantize(const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const float* gamma, float eps, void* q, int64_t ld_q, float* scale,
+                                     void* sum, int64_t ld_s, float* rstd, int64_t n, int32_t c, int32_t dtype, void* stream) {
+  return spc::rms_call(x, ld_x, residual, ld_r, gamma, eps, q, ld_q, true, scale, sum, ld_s, rstd, n, c, dtype, stream);
+}
+
+extern "C" int spc_quantize_rows(const void* x, int64_t ld_x, void* q, int64_t ld_q, float* scale, int64_t n, int32_t c, int32_t dtype, void* stream) {
+  using namespace spc;
+  SPC_RETURN_IF(norm_check(n, c, dtype));
+  SPC_RETURN_IF(norm_check_rows("x", x, ld_x, c, dtype == SPC_DTYPE_F32 ? 4 : 2, n == 0));
+  SPC_RETURN_IF(norm_check_rows("q", q, ld_q, c, 1, n == 0));
+  if (n && !scale) return set_error(SPC_ERR_ARG, "scale is NULL");
+  if (!n) return SPC_OK;
+  RmsArgs a{};
+  a.x = x, a.ld_x = ld_x, a.y = q, a.ld_y = ld_q, a.scale = scale, a.n = n, a.c = c;
+  rms_forward<BARE_BYTES>(a, dtype, static_cast<hipStream_t>(stream));
+  SPC_HIP_CHECK(hipGetLastError());
+  return SPC_OK;
+}
+
+extern "C" int spc_rms_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const float* rstd, const float* gamma, const void* dsum, int64_t ld_ds,
+                                     void* dx, int64_t ld_dx, float* dgamma, int64_t n, int32_t c, int32_t dtype, void* stream) {
+  using namespace spc;
+  SPC_RETURN_IF(norm_check(n, c, dtype));
+  const int es = dtype == SPC_DTYPE_F32 ? 4 : 2;
+  SPC_RETURN_IF(norm_check_rows("dy", dy, ld_dy, c, es, n == 0));
+  SPC_RETURN_IF(norm_check_rows("x", x, ld_x, c, es, n == 0));
+  SPC_RETURN_IF(norm_check_rows("dx", dx, ld_dx, c, es, n == 0));
+  SPC_RETURN_IF(norm_check_rows("dsum", dsum, ld_ds, c, es, true));
+  if (n && !rstd) return set_error(SPC_ERR_ARG, "rstd is NULL");
+  const StreamId s(static_cast<hipStream_t>(stream));
+  const StreamWorkNote note{s};
+  RmsArgs a{};
+  a.dy = dy, a.ld_dy = ld_dy, a.x = x, a.ld_x = ld_x, a.rstd_in = rstd, a.gamma = gamma, a.e = dsum, a.ld_e = ld_ds, a.y = dx, a.ld_y = ld_dx, a.n = n, a.c = c;
+  const int wgs = norm_grid(dtype, c, n, true);
+  if (dgamma && n) {
+    a.partial = static_cast<float*>(pool_alloc(scratch_bytes(size_t(wgs) * c * sizeof(float)), s));
+    if (!a.partial) return SPC_ERR_NOMEM;
+  }
+  if (n)
+    by_dtype(dtype, [&](auto t) {
+      norm_shape<decltype(t)>(c, [&](auto nv, auto g, auto fit) {
+        constexpr int G = decltype(g)::value;
+        hipLaunchKernelGGL((rms_backward_kernel<decltype(t), decltype(nv)::value, G, decltype(fit)::value>), dim3(wgs), dim3(NORM_THREADS), G <= 64 ? 4 * c : 0, s, a);
+      });
+    });
+  if (dgamma) column_sums({{dgamma}, {c}}, a.partial, n ? wgs : 0, s);
+  pool_free(a.partial, s);
+  SPC_HIP_CHECK(hipGetLastError());
+  return SPC_OK;
+}
 
 extern "C" int spc_layer_norm_forward(const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const float* gamma, const float* beta,
                                       float eps, void* y, int64_t ld_y, void* sum, int64_t ld_s, float* mean, float* rstd, int64_t n, int32_t c,

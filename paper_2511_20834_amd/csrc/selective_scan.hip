@@ -1,0 +1,809 @@
+// Selective state space scan of every channel along the rows of its scene, forward and backward, and one row of many streams.
+//
+//   d_t = softplus(dt_t + bias),  h_t = exp(d_t A) h_{t-1} + d_t u_t B_t  (N states a channel),  y_t = C_t . h_t + D u_t,  out_t = y_t silu(gate_t)
+//
+// Backward, with dy = dout silu(gate), q the gradient of a state and a_t = exp(d_t A):
+//
+//   q_t = C_t dy_t + a_{t+1} q_{t+1},  dC_t = sum over channels of h_t dy_t,  dB_t = sum over channels of q_t d_t u_t,  x_t = sum over states of q_t B_t,
+//   du_t = d_t x_t + D dy_t,  p_t = q_t a_t h_{t-1},  dd_t = u_t x_t + sum over states of A p_t,  dA = sum over rows of d_t p_t
+//
+// A lane has a channel and keeps its states in registers, so that a row is one wide load for 64 channels; B and C are the same for all lanes: a first launch
+// writes them as floats, which arrive through scalar loads.  A scene is cut into segments: one launch makes every segment's own state (from zeros) and its sum of d, a
+// second chains them (a segment's decay is exp(A sum d)), the last scans the segments from the states in front of them.  Scenes of one segment need the last alone.
+// The vector unit bounds it: an exponential and three products or sums a state and row in the sums, four in the outputs.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "scenes.h"
+
+namespace spc {
+namespace {
+
+constexpr int SCAN_MAX_N = 64;
+constexpr int SCAN_MAX_C = 65536;
+constexpr float LOG2E = 1.44269504f;
+
+struct LowRows {  // B or C: channel j of group g in row r is r * row + g * group + j
+  void* p;
+  int64_t row, group;
+};
+
+struct ScanArgs {
+  Scenes scenes;
+  const void *u, *dt, *gate, *dout;
+  void *out, *ddt, *dgate;  // out: backward du
+  int64_t ld_u, ld_dt, ld_gate, ld_dout, ld_out, ld_ddt, ld_dgate;
+  LowRows b, c, db, dc;
+  const float *A, *skip, *bias;
+  const float *state_in, *dstate_out;
+  float *state_out, *dstate_in;
+  float* low;      // [row][group][B, C][NP], a row of zeros behind the last one
+  float* between;  // [segment][NP][channels]: its state from zeros, then the state behind it
+  float* behind;   // the same for the gradient: what reaches the rows in front of a segment, from zeros, then what arrives from behind it
+  float* steps;    // [segment][channels]: sum of d
+  float* parts;    // [segment][NP + 2][channels]: dA, dD, dbias
+  float* low_parts;  // [block of channels][row][B, C][NP], where several blocks share a group
+  int channels, groups, share, N, blocks, ids;  // share: channels of a group; blocks: of 64 channels, of all groups
+  bool softplus;
+};
+
+typedef const __attribute__((address_space(4))) float* Scalars;  // (read through the scalar cache: nothing writes there while the kernel runs)
+
+// ln(1 + e), 0 <= e <= 1: 2 artanh(e / (2 + e)) by its series, what is left out is below 2^-27.
+__device__ inline float log1p_of(float e) {
+  const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;
+  float p = 1.f / 15;
+#pragma unroll
+  for (int k = 13; k > 0; k -= 2) p = fmaf(p, q, 1.f / k);
+  return 2.f * s * p;
+}
+
+// Step sizes.
+template <typename T>
+struct Step {
+  float d, slope;  // d and its derivative
+  __device__ Step(float raw, bool softplus) : d(raw), slope(1.f) {
+    if (!softplus) return;
+    const float e = exp_of<sizeof(T) == 4>(-fabsf(raw)), r = __builtin_amdgcn_rcpf(1.f + e);
+    d = fmaxf(raw, 0.f) + log1p_of(e);
+    if (raw != raw) d = raw;  // (the maximum passes over NaN)
+    slope = raw >= 0.f ? r : e * r;
+  }
+};
+
+// A lane's channel in block `block` of all channels.
+struct Lane {
+  int channel, group;
+  bool some;
+  __device__ Lane(const ScanArgs& a, int block, int lane) {
+    const int per = a.blocks / a.groups;
+    group = block / per;
+    const int i = (block - group * per) * 64 + lane;
+    some = i < a.share;
+    channel = group * a.share + min(i, a.share - 1);
+  }
+};
+
+__device__ inline Scalars low_row(const ScanArgs& a, int64_t row, int group, int np) {
+  return (Scalars)(uintptr_t)(a.low + (row * a.groups + group) * (2 * np));
+}
+
+// B and C as floats, N of them filled up to NP with zeros.
+template <typename T>
+__global__ __launch_bounds__(256) void scan_low_kernel(LowRows b, LowRows c, float* low, int n_rows, int groups, int N, int log_np) {
+  const int64_t n = (int64_t(n_rows) + 1) * groups << (log_np + 1);
+  for (int64_t i = blockIdx.x * int64_t(256) + threadIdx.x; i < n; i += gridDim.x * int64_t(256)) {
+    const int j = static_cast<int>(i & ((1 << log_np) - 1));
+    const int64_t rg = i >> (log_np + 1), row = rg / groups, g = rg - row * groups;
+    const LowRows& from = i >> log_np & 1 ? c : b;
+    low[i] = row < n_rows && j < N ? static_cast<float>(static_cast<const T*>(from.p)[row * from.row + g * from.group + j]) : 0.f;
+  }
+}
+
+// Rates of a lane's states first .. first + n of NP, times log2(e).
+template <int NP>
+__device__ inline void rates(float (&A2)[NP], const ScanArgs& a, int channel, int first) {
+#pragma unroll
+  for (int n = 0; n < NP; ++n) A2[n] = first + n < a.N ? a.A[int64_t(channel) * a.N + first + n] * LOG2E : 0.f;
+}
+template <int NP>
+__device__ inline void load_state(float (&h)[NP], const float* p, const ScanArgs& a, int scene, const Lane& me, int first) {
+#pragma unroll
+  for (int n = 0; n < NP; ++n) h[n] = p && me.some && first + n < a.N ? p[(int64_t(scene) * a.channels + me.channel) * a.N + first + n] : 0.f;
+}
+template <int NP>
+__device__ inline void store_state(const float (&h)[NP], float* p, const ScanArgs& a, int scene, const Lane& me, int first) {
+  if (!p || !me.some) return;
+#pragma unroll
+  for (int n = 0; n < NP; ++n)
+    if (first + n < a.N) p[(int64_t(scene) * a.channels + me.channel) * a.N + first + n] = h[n];
+}
+template <int NP, int ALL>
+__device__ inline void load_between(float (&h)[NP], const float* p, const ScanArgs& a, int id, const Lane& me, int first) {
+#pragma unroll
+  for (int n = 0; n < NP; ++n) h[n] = me.some ? p[(int64_t(id) * ALL + first + n) * a.channels + me.channel] : 0.f;
+}
+
+// What a lane reads of `U` rows.
+template <typename T, int U, bool GATE, bool GRAD>
+struct Inputs {
+  T u[U], dt[U], gate[GATE ? U : 1], dout[GRAD ? U : 1];
+  __device__ void load(const ScanArgs& a, const Lane& me, int64_t first, int t, int rows) {
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      const int64_t row = first + min(t + q, rows - 1);
+      u[q] = static_cast<const T*>(a.u)[row * a.ld_u + me.channel];
+      dt[q] = static_cast<const T*>(a.dt)[row * a.ld_dt + me.channel];
+      if (GATE) gate[q] = static_cast<const T*>(a.gate)[row * a.ld_gate + me.channel];
+      if (GRAD) dout[q] = static_cast<const T*>(a.dout)[row * a.ld_dout + me.channel];
+    }
+  }
+};
+
+// SUMS: a segment's own state, its sum of d, and (GRAD) what its rows send to those in front of it.  Else: outputs.
+template <typename T, int NP, bool GATE, bool SUMS, bool GRAD>
+__global__ __launch_bounds__(64) void scan_kernel(const ScanArgs a) {
+  constexpr int U = 8;
+  constexpr bool EXACT = sizeof(T) == 4, GATED = GATE && (GRAD || !SUMS);
+  const int id = blockIdx.x / a.blocks, block = blockIdx.x - id * a.blocks;
+  SceneSegment s;
+  if (!s.find(a.scenes, id) || (SUMS && (s.n == 1 || (!GRAD && s.m == s.n - 1)))) return;
+  s.uniform();
+  const Lane me(a, block, threadIdx.x);
+  const float bias = a.bias ? a.bias[me.channel] : 0.f, skip = a.skip ? a.skip[me.channel] : 0.f;
+  float A2[NP], h[NP], sent[GRAD ? NP : 1] = {}, through[GRAD ? NP : 1], steps = 0.f;
+  rates<NP>(A2, a, me.channel, 0);
+  if (SUMS) {
+#pragma unroll
+    for (int n = 0; n < NP; ++n) h[n] = 0.f;
+    if (GRAD)
+#pragma unroll
+      for (int n = 0; n < NP; ++n) through[n] = 1.f;
+  } else if (s.m == 0) {
+    load_state<NP>(h, a.state_in, a, s.scene, me, 0);
+  } else {
+    load_between<NP, NP>(h, a.between, a, id - 1, me, 0);
+  }
+  Inputs<T, U, GATED, GRAD> now, next;
+  if (s.rows > 0) now.load(a, me, s.first, 0, s.rows);
+  for (int t = 0; t < s.rows; t += U) {
+    if (t + U < s.rows) next.load(a, me, s.first, t + U, s.rows);
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      if (t + q >= s.rows) break;
+      const int64_t row = int64_t(s.first) + t + q;
+      const Scalars low = low_row(a, row, me.group, NP);
+      const float u = static_cast<float>(now.u[q]), d = Step<T>(static_cast<float>(now.dt[q]) + bias, a.softplus).d, x = d * u;
+      float dy = 0.f, y = 0.f;
+      if constexpr (GRAD) {
+        dy = static_cast<float>(now.dout[q]);
+        if constexpr (GATED) {
+          const float z = static_cast<float>(now.gate[q]);
+          dy *= z * sigmoid_of<EXACT>(z);
+        }
+      }
+      if (SUMS) steps += d;
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        const float e = __builtin_amdgcn_exp2f(d * A2[n]);
+        h[n] = fmaf(e, h[n], x * low[n]);
+        if (!SUMS) y = fmaf(low[NP + n], h[n], y);
+        if constexpr (GRAD) {
+          through[n] *= e;
+          sent[n] = fmaf(through[n], dy * low[NP + n], sent[n]);
+        }
+      }
+      if (!SUMS) {
+        y = fmaf(skip, u, y);
+        if constexpr (GATED) {
+          const float z = static_cast<float>(now.gate[q]);
+          y *= z * sigmoid_of<EXACT>(z);
+        }
+        if (me.some) static_cast<T*>(a.out)[row * a.ld_out + me.channel] = static_cast<T>(y);
+      }
+    }
+    now = next;
+  }
+  if (!SUMS) {
+    if (s.m == s.n - 1) store_state<NP>(h, a.state_out, a, s.scene, me, 0);
+    return;
+  }
+  if (!me.some) return;
+  a.steps[int64_t(id) * a.channels + me.channel] = steps;
+#pragma unroll
+  for (int n = 0; n < NP; ++n) {
+    const int64_t at = (int64_t(id) * NP + n) * a.channels + me.channel;
+    a.between[at] = h[n];
+    if (GRAD) a.behind[at] = sent[n];
+  }
+}
+
+// A scene's segments one after the other: their own states -> the states behind them; with time running backward, what they send forward -> what arrives behind them.
+__global__ __launch_bounds__(256) void scan_chain_kernel(const ScanArgs a, int np) {
+  constexpr int AHEAD = 16;
+  const bool back = blockIdx.y;
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, each = int64_t(np) * a.channels;
+  const int scene = static_cast<int>(i / each), at = static_cast<int>(i - scene * each), n = at / a.channels, channel = at - n * a.channels;
+  if (scene >= a.scenes.n_scenes) return;
+  const int lo = a.scenes.offsets ? min(max(a.scenes.offsets[scene], 0), a.scenes.n_rows) : 0;
+  const int id = lo / a.scenes.seg_rows + scene;
+  SceneSegment s;
+  if (!s.find(a.scenes, id) || s.scene != scene || s.n == 1) return;
+  const bool is = n < a.N;
+  const float A2 = is ? a.A[int64_t(channel) * a.N + n] * LOG2E : 0.f;
+  const float* start = back ? a.dstate_out : a.state_in;
+  float h = start && is ? start[(int64_t(scene) * a.channels + channel) * a.N + n] : 0.f;
+  float* p = (back ? a.behind : a.between) + int64_t(id) * each + at;
+  const float* steps = a.steps + int64_t(id) * a.channels + channel;
+  const int links = back ? s.n : s.n - 1;  // (nothing is behind a scene's last segment)
+  for (int m0 = 0; m0 < links; m0 += AHEAD) {
+    float v[AHEAD], d[AHEAD];
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) {
+      const int m = back ? s.n - 1 - min(m0 + q, links - 1) : min(m0 + q, links - 1);
+      v[q] = p[m * each];
+      d[q] = steps[int64_t(m) * a.channels];
+    }
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) {
+      if (m0 + q >= links) break;
+      const float after = fmaf(__builtin_amdgcn_exp2f(A2 * d[q]), h, v[q]);
+      if (back) p[(s.n - 1 - (m0 + q)) * each] = h;  // (what arrives behind the segment)
+      else p[(m0 + q) * each] = after;
+      h = after;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- gradients
+template <int CTRL>
+__device__ inline float from_lane(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+constexpr int XOR_1 = 0xb1, XOR_2 = 0x4e, XOR_7 = 0x141, XOR_8 = 0x128;  // (of a row's 16 lanes: two orders of four, the half turned round, turned by 8)
+template <int CTRL>
+__device__ inline float halves(float a, float b, bool upper) {  // a of this lane and its partner where `upper` is false, b where it is true
+  return (upper ? b : a) + from_lane<CTRL>(upper ? a : b);
+}
+// Sums of V values over the 64 lanes: lane l ends with value l / (64 / V).  Half of the values go with every step.
+template <int V>
+__device__ inline float sums_over_lanes(float (&v)[V], int lane) {
+  static_assert(V == 16 || V == 32, "two rows of four or eight states");
+#pragma unroll
+  for (int k = 0; k < V / 2; ++k) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v[k]), __builtin_bit_cast(unsigned, v[k + V / 2]), false, false);
+    const unsigned a = r[0], b = r[1];  // (a cast of r[1] itself is one of r[0] to the compiler)
+    v[k] = __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+  }
+#pragma unroll
+  for (int k = 0; k < V / 4; ++k) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v[k]), __builtin_bit_cast(unsigned, v[k + V / 4]), false, false);
+    const unsigned a = r[0], b = r[1];  // (a cast of r[1] itself is one of r[0] to the compiler)
+    v[k] = __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+  }
+#pragma unroll
+  for (int k = 0; k < V / 8; ++k) v[k] = halves<XOR_8>(v[k], v[k + V / 8], lane & 8);
+#pragma unroll
+  for (int k = 0; k < V / 16; ++k) v[k] = halves<XOR_7>(v[k], v[k + V / 16], lane & 4);
+  if constexpr (V == 32) v[0] = halves<XOR_2>(v[0], v[1], lane & 2);
+  else v[0] += from_lane<XOR_2>(v[0]);
+  return v[0] + from_lane<XOR_1>(v[0]);
+}
+
+// A workgroup has a segment of 64 channels, each of its LP waves NG of their states.  The states at the start of every chunk of L rows go to LDS in a first sweep; then chunk by
+// chunk from the last one the states are made again, kept in registers, and the gradient runs back over them.  What rows share (d, d u, dy) is made by
+// one wave a row and read by all; the sums over states (x, sum of A p, C . h) are parts of the waves, which the row's wave adds up.
+constexpr int PART_ROWS = 8;
+template <int NG, int L, int LP, bool GATE>
+struct GradLds {
+  static constexpr int VALUES = GATE ? 3 : 2;
+  float stage[3][L][64];
+  float part[LP][PART_ROWS][VALUES][64];
+  // behind it: starts [LP][chunks][NG][64], of 128 rows of 16 states, or as many fewer as there are more states: 68 KB of LDS, 94, 118
+  static size_t bytes(int chunks) { return sizeof(GradLds) + size_t(LP) * chunks * NG * 64 * sizeof(float); }
+};
+
+template <typename T, int NG, int L, int LP, bool GATE>
+__global__ __launch_bounds__(64 * LP) void scan_grad_kernel(const ScanArgs a) {
+  using Lds = GradLds<NG, L, LP, GATE>;
+  constexpr int NP = NG * LP, RW = L / LP, V = 4 * NG;
+  constexpr bool EXACT = sizeof(T) == 4;
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  Lds& lds = *reinterpret_cast<Lds*>(raw);
+  float* starts = reinterpret_cast<float*>(raw + sizeof(Lds));
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), first_n = wave * NG;
+  const int id = blockIdx.x / a.blocks, block = blockIdx.x - id * a.blocks;
+  const Lane me(a, block, lane);
+  float* parts = a.parts + int64_t(id) * (NP + 2) * a.channels + me.channel;
+  SceneSegment s;
+  if (!s.find(a.scenes, id)) {
+    if (me.some) {
+#pragma unroll
+      for (int n = 0; n < NG; ++n) parts[int64_t(first_n + n) * a.channels] = 0.f;
+      if (wave == 0) parts[int64_t(NP) * a.channels] = parts[int64_t(NP + 1) * a.channels] = 0.f;
+    }
+    return;
+  }
+  s.uniform();
+  const float bias = a.bias ? a.bias[me.channel] : 0.f, skip = a.skip ? a.skip[me.channel] : 0.f;
+  float A2[NG], h[NG], r[NG], dA[NG] = {};
+  rates<NG>(A2, a, me.channel, first_n);
+  if (s.m == 0) load_state<NG>(h, a.state_in, a, s.scene, me, first_n);
+  else load_between<NG, NP>(h, a.between, a, id - 1, me, first_n);
+  if (s.m == s.n - 1) load_state<NG>(r, a.dstate_out, a, s.scene, me, first_n);
+  else load_between<NG, NP>(r, a.behind, a, id, me, first_n);
+  const int chunks = (s.rows + L - 1) / L, room = a.scenes.seg_rows / L;
+  auto at_start = [&](int chunk, int n) -> float& { return starts[((wave * room + chunk) * NG + n) * 64 + lane]; };
+  auto low_of = [&](int t) { return low_row(a, t < s.rows ? int64_t(s.first) + t : int64_t(a.scenes.n_rows), me.group, NP); };
+  // this wave's rows of a chunk: t = chunk L + j LP + wave
+  float u[RW], d[RW], slope[RW], dout[RW], gate[GATE ? RW : 1], dy[RW];
+  auto stage = [&](int chunk, bool grad) {
+    T in_u[RW], in_dt[RW], in_g[RW], in_o[RW];
+#pragma unroll
+    for (int j = 0; j < RW; ++j) {
+      const int64_t row = int64_t(s.first) + min(chunk * L + j * LP + wave, s.rows - 1);
+      in_u[j] = static_cast<const T*>(a.u)[row * a.ld_u + me.channel];
+      in_dt[j] = static_cast<const T*>(a.dt)[row * a.ld_dt + me.channel];
+      if (grad) in_o[j] = static_cast<const T*>(a.dout)[row * a.ld_dout + me.channel];
+      if (GATE && grad) in_g[j] = static_cast<const T*>(a.gate)[row * a.ld_gate + me.channel];
+    }
+#pragma unroll
+    for (int j = 0; j < RW; ++j) {
+      const int i = j * LP + wave;
+      const bool there = me.some && chunk * L + i < s.rows;  // (rows that are not there leave states and gradients as they are)
+      const Step<T> step(static_cast<float>(in_dt[j]) + bias, a.softplus);
+      u[j] = there ? static_cast<float>(in_u[j]) : 0.f;
+      d[j] = there ? step.d : 0.f;
+      lds.stage[0][i][lane] = d[j];
+      lds.stage[1][i][lane] = d[j] * u[j];
+      if (!grad) continue;
+      slope[j] = step.slope;
+      dout[j] = there ? static_cast<float>(in_o[j]) : 0.f;
+      dy[j] = dout[j];
+      if constexpr (GATE) {
+        gate[j] = there ? static_cast<float>(in_g[j]) : 0.f;
+        dy[j] *= gate[j] * sigmoid_of<EXACT>(gate[j]);
+      }
+      lds.stage[2][i][lane] = dy[j];
+    }
+  };
+  for (int chunk = 0; chunk + 1 < chunks; ++chunk) {
+#pragma unroll
+    for (int n = 0; n < NG; ++n) at_start(chunk, n) = h[n];
+    __syncthreads();  // (the rows before have been read)
+    stage(chunk, false);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const Scalars low = low_of(chunk * L + i);
+      const float di = lds.stage[0][i][lane], xi = lds.stage[1][i][lane];
+#pragma unroll
+      for (int n = 0; n < NG; ++n) h[n] = fmaf(__builtin_amdgcn_exp2f(di * A2[n]), h[n], xi * low[first_n + n]);
+    }
+  }
+  float dskip = 0.f, dbias = 0.f;
+  for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+    if (chunk < chunks - 1)
+#pragma unroll
+      for (int n = 0; n < NG; ++n) h[n] = at_start(chunk, n);
+    __syncthreads();
+    stage(chunk, true);
+    __syncthreads();
+    float hs[L][NG];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const Scalars low = low_of(chunk * L + i);
+      const float di = lds.stage[0][i][lane], xi = lds.stage[1][i][lane];
+#pragma unroll
+      for (int n = 0; n < NG; ++n) hs[i][n] = fmaf(__builtin_amdgcn_exp2f(di * A2[n]), i ? hs[i ? i - 1 : 0][n] : h[n], xi * low[first_n + n]);
+    }
+#pragma unroll
+    for (int half = L / PART_ROWS - 1; half >= 0; --half) {
+#pragma unroll
+      for (int pair = PART_ROWS / 2 - 1; pair >= 0; --pair) {
+        float v[V];
+#pragma unroll
+        for (int e = 1; e >= 0; --e) {
+          const int i = half * PART_ROWS + pair * 2 + e;
+          const Scalars low = low_of(chunk * L + i);
+          const float di = lds.stage[0][i][lane], xi = lds.stage[1][i][lane], dyi = lds.stage[2][i][lane];
+          float sx = 0.f, sp = 0.f, sy = 0.f;
+#pragma unroll
+          for (int n = 0; n < NG; ++n) {
+            const float B = low[first_n + n], C = low[NP + first_n + n];
+            const float q = fmaf(C, dyi, r[n]);
+            v[e * 2 * NG + n] = q * xi;
+            v[e * 2 * NG + NG + n] = hs[i][n] * dyi;
+            if (GATE) sy = fmaf(C, hs[i][n], sy);
+            sx = fmaf(q, B, sx);
+            r[n] = q * __builtin_amdgcn_exp2f(di * A2[n]);
+            const float p = r[n] * (i ? hs[i ? i - 1 : 0][n] : h[n]);
+            sp = fmaf(A2[n], p, sp);
+            dA[n] = fmaf(di, p, dA[n]);
+          }
+          float(*to)[64] = lds.part[wave][pair * 2 + e];
+          to[0][lane] = sx;
+          to[1][lane] = sp;
+          if (GATE) to[2][lane] = sy;
+        }
+        const float sum = sums_over_lanes<V>(v, lane);
+        constexpr int EACH = 64 / V;
+        const int k = lane / EACH, t = chunk * L + half * PART_ROWS + pair * 2 + k / (2 * NG), n = first_n + k % NG;
+        const bool is_c = k / NG % 2;
+        if (lane % EACH == 0 && t < s.rows) {
+          const int64_t row = int64_t(s.first) + t;
+          if (a.low_parts) {
+            a.low_parts[((int64_t(block) * a.scenes.n_rows + row) * 2 + is_c) * NP + n] = sum;
+          } else if (n < a.N) {
+            const LowRows& to = is_c ? a.dc : a.db;
+            static_cast<T*>(to.p)[row * to.row + me.group * to.group + n] = static_cast<T>(sum);
+          }
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = half * PART_ROWS / LP; j < (half + 1) * PART_ROWS / LP; ++j) {
+        const int i = j * LP + wave, t = chunk * L + i;
+        float sx = 0.f, sp = 0.f, sy = 0.f;
+#pragma unroll
+        for (int w = 0; w < LP; ++w) {
+          sx += lds.part[w][i % PART_ROWS][0][lane];
+          sp += lds.part[w][i % PART_ROWS][1][lane];
+          if (GATE) sy += lds.part[w][i % PART_ROWS][GATE ? 2 : 0][lane];
+        }
+        if (!me.some || t >= s.rows) continue;
+        const int64_t row = int64_t(s.first) + t;
+        const float ddt = fmaf(u[j], sx, sp * (1.f / LOG2E)) * slope[j];
+        static_cast<T*>(a.out)[row * a.ld_out + me.channel] = static_cast<T>(fmaf(d[j], sx, skip * dy[j]));
+        static_cast<T*>(a.ddt)[row * a.ld_ddt + me.channel] = static_cast<T>(ddt);
+        if constexpr (GATE) {
+          const float g = sigmoid_of<EXACT>(gate[j]);
+          static_cast<T*>(a.dgate)[row * a.ld_dgate + me.channel] = static_cast<T>(dout[j] * fmaf(skip, u[j], sy) * fmaf(gate[j] * g, 1.f - g, g));
+        }
+        dskip = fmaf(dy[j], u[j], dskip);
+        dbias += ddt;
+      }
+      if (half) __syncthreads();  // (the parts have been read)
+    }
+  }
+  if (s.m == 0) store_state<NG>(r, a.dstate_in, a, s.scene, me, first_n);
+  __syncthreads();
+  lds.part[wave][0][0][lane] = dskip;
+  lds.part[wave][0][1][lane] = dbias;
+  __syncthreads();
+  if (!me.some) return;
+#pragma unroll
+  for (int n = 0; n < NG; ++n) parts[int64_t(first_n + n) * a.channels] = dA[n];
+  if (wave < 2) {
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < LP; ++w) sum += lds.part[w][0][wave][lane];
+    parts[int64_t(NP + wave) * a.channels] = sum;
+    if (LP == 1) {
+      sum = lds.part[0][0][1][lane];
+      parts[int64_t(NP + 1) * a.channels] = sum;
+    }
+  }
+}
+
+// Sums of the segments' parts: 32 columns a workgroup, 32 shares of the segments added up in LDS, in a fixed order.
+__global__ __launch_bounds__(1024) void scan_params_kernel(const float* __restrict__ parts, int n, int np, int channels, int N, float* dA, float* dskip, float* dbias) {
+  __shared__ float lds[32][33];
+  const int cols = (np + 2) * channels, col = blockIdx.x * 32 + threadIdx.x % 32, share = threadIdx.x / 32;
+  float s = 0.f;
+  if (col < cols) {
+    const float* p = parts + col;
+#pragma unroll 8
+    for (int q = share; q < n; q += 32) s += p[int64_t(q) * cols];
+  }
+  lds[share][threadIdx.x % 32] = s;
+  __syncthreads();
+  if (share || col >= cols) return;
+  s = 0.f;
+#pragma unroll
+  for (int q = 0; q < 32; ++q) s += lds[q][threadIdx.x];
+  const int j = col / channels, channel = col - j * channels;
+  if (j < N && dA) dA[int64_t(channel) * N + j] = s;
+  if (j == np && dskip) dskip[channel] = s;
+  if (j == np + 1 && dbias) dbias[channel] = s;
+}
+
+// dB and dC of groups of several blocks of channels.
+template <typename T>
+__global__ __launch_bounds__(256) void scan_low_grad_kernel(const ScanArgs a, int log_np) {
+  const int n_rows = a.scenes.n_rows, per = a.blocks / a.groups;
+  const int lo = a.scenes.offsets ? min(max(a.scenes.offsets[0], 0), n_rows) : 0;
+  const int hi = a.scenes.offsets ? min(max(a.scenes.offsets[a.scenes.n_scenes], lo), n_rows) : n_rows;
+  const int64_t each = int64_t(n_rows) << (log_np + 1), n = int64_t(hi - lo) * a.groups << (log_np + 1);
+  for (int64_t i = blockIdx.x * int64_t(256) + threadIdx.x; i < n; i += gridDim.x * int64_t(256)) {
+    const int j = static_cast<int>(i & ((1 << log_np) - 1));
+    if (j >= a.N) continue;
+    const int is_c = i >> log_np & 1;
+    const int64_t rg = i >> (log_np + 1), row = lo + rg / a.groups, g = rg % a.groups;
+    const float* p = a.low_parts + g * per * each + (row << (log_np + 1)) + (is_c << log_np) + j;
+    float s = 0.f;
+#pragma unroll 4
+    for (int q = 0; q < per; ++q) s += p[q * each];
+    const LowRows& to = is_c ? a.dc : a.db;
+    static_cast<T*>(to.p)[row * to.row + g * to.group + j] = static_cast<T>(s);
+  }
+}
+
+// ---------------------------------------------------------------- one row of many streams
+// A lane has VEC states of a channel, 2^log_q neighbouring lanes have a channel's; states are read and written once, which bounds it.  The decay is taken as
+// 1 + (e^w - 1) where it is near 1: rounded to 24 bits every row, a stream's long memory would drift.
+template <typename T, int VEC, bool GATE>
+__global__ __launch_bounds__(256) void scan_step_kernel(const ScanArgs a, float* state, int64_t n, int log_q) {
+  typedef float Values __attribute__((ext_vector_type(VEC), aligned(4), may_alias));
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) >> log_q, row = i / a.channels;
+  const int channel = static_cast<int>(i - row * a.channels), first = (threadIdx.x & ((1 << log_q) - 1)) * VEC;
+  const bool is = row < n && first < a.N;
+  float y = 0.f, u = 0.f;
+  if (row < n) u = static_cast<float>(static_cast<const T*>(a.u)[row * a.ld_u + channel]);
+  if (is) {
+    Values* S = reinterpret_cast<Values*>(state + i * a.N + first);
+    Values h = *S;
+    const float d = Step<T>(static_cast<float>(static_cast<const T*>(a.dt)[row * a.ld_dt + channel]) + (a.bias ? a.bias[channel] : 0.f), a.softplus).d;
+    const int group = channel / a.share;
+    const T* B = static_cast<const T*>(a.b.p) + row * a.b.row + group * a.b.group + first;
+    const T* C = static_cast<const T*>(a.c.p) + row * a.c.row + group * a.c.group + first;
+    const Values A = *reinterpret_cast<const Values*>(a.A + int64_t(channel) * a.N + first);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      const float w = d * A[k], x = d * u * static_cast<float>(B[k]);
+      float e = 1.f;
+#pragma unroll
+      for (int j = 7; j > 1; --j) e = fmaf(e, w * (1.f / j), 1.f);  // (what the series leaves out is below 2^-28 of it for |w| < 1/4)
+      h[k] = fabsf(w) < .25f ? h[k] + fmaf(h[k], e * w, x) : fmaf(__builtin_amdgcn_exp2f(w * LOG2E), h[k], x);
+      y = fmaf(static_cast<float>(C[k]), h[k], y);
+    }
+    *S = h;
+  }
+  for (int o = 1; o < (1 << log_q); o <<= 1) y += __shfl_xor(y, o, 64);
+  if (!is || first) return;
+  y = fmaf(a.skip ? a.skip[channel] : 0.f, u, y);
+  if constexpr (GATE) {
+    const float z = static_cast<float>(static_cast<const T*>(a.gate)[row * a.ld_gate + channel]);
+    y *= z * sigmoid_of<sizeof(T) == 4>(z);
+  }
+  static_cast<T*>(a.out)[row * a.ld_out + channel] = static_cast<T>(y);
+}
+
+// ---------------------------------------------------------------- host
+int check_scan(const spc_scan_desc* d, const float* A, bool scenes, const int32_t* offsets) {
+  if (!d) return set_error(SPC_ERR_ARG, "descriptor is NULL");
+  if (d->dtype != SPC_DTYPE_F16 && d->dtype != SPC_DTYPE_BF16 && d->dtype != SPC_DTYPE_F32) return set_error(SPC_ERR_ARG, "unknown dtype %d", d->dtype);
+  if (d->n_rows < 0 || d->channels < 1 || d->groups < 1 || d->channels % d->groups || d->states < 1)
+    return set_error(SPC_ERR_ARG, "%lld rows, %d channels in %d groups, %d states", static_cast<long long>(d->n_rows), d->channels, d->groups, d->states);
+  if (!A) return set_error(SPC_ERR_ARG, "A is NULL");
+  if (d->channels > SCAN_MAX_C || d->states > SCAN_MAX_N)
+    return set_error(SPC_ERR_UNSUPPORTED, "%d channels of %d states: at most %d and %d", d->channels, d->states, SCAN_MAX_C, SCAN_MAX_N);
+  if (scenes) SPC_RETURN_IF(check_scenes(offsets, d->n_rows, d->n_scenes));
+  return SPC_OK;
+}
+int check_matrix(const char* what, const void* p, int64_t ld, const spc_scan_desc* d) {
+  if (!p) return set_error(SPC_ERR_ARG, "%s is NULL", what);
+  if (ld < d->channels) return set_error(SPC_ERR_ARG, "row pitch %lld of %s is below %d channels", static_cast<long long>(ld), what, d->channels);
+  if (reinterpret_cast<uintptr_t>(p) % (d->dtype == SPC_DTYPE_F32 ? 4 : 2)) return set_error(SPC_ERR_ARG, "%s is not aligned to its type", what);
+  return SPC_OK;
+}
+// Pitches of an input may be zero (broadcast); places of an output are its own.
+int check_low(const char* what, const spc_attn_rows* t, const spc_scan_desc* d, bool output) {
+  if (!t || !t->data) return set_error(SPC_ERR_ARG, "%s is NULL", what);
+  if (reinterpret_cast<uintptr_t>(t->data) % (d->dtype == SPC_DTYPE_F32 ? 4 : 2)) return set_error(SPC_ERR_ARG, "%s is not aligned to its type", what);
+  const int64_t row = t->row_pitch, group = t->head_pitch, far = int64_t(1) << 40;
+  bool ok = row >= 0 && group >= 0 && row < far && group < far;
+  if (output && ok) {
+    const bool one_row = d->n_rows <= 1, one_group = d->groups == 1;
+    ok = (one_row || row >= d->states) && (one_group || group >= d->states) &&
+         (one_row || one_group || row >= (d->groups - 1) * group + d->states || group >= (d->n_rows - 1) * row + d->states);
+  }
+  return ok ? SPC_OK : set_error(SPC_ERR_ARG, "pitches %lld and %lld of %s do not fit %d groups of %d states", static_cast<long long>(row), static_cast<long long>(group), what,
+                                 d->groups, d->states);
+}
+LowRows low_rows(const spc_attn_rows* t) { return {t->data, t->row_pitch, t->head_pitch}; }
+
+int log_padded(int N) { return N <= 4 ? 2 : N <= 8 ? 3 : N <= 16 ? 4 : N <= 32 ? 5 : 6; }
+
+// Calls f(type, NP, GATE).
+template <typename F>
+void scan_variant(const spc_scan_desc* d, bool gate, F&& f) {
+  using std::integral_constant;
+  by_dtype(d->dtype, [&](auto t) {
+    auto with = [&](auto np) {
+      if (gate) f(t, np, std::true_type{});
+      else f(t, np, std::false_type{});
+    };
+    switch (log_padded(d->states)) {
+      case 2: return with(integral_constant<int, 4>{});
+      case 3: return with(integral_constant<int, 8>{});
+      case 4: return with(integral_constant<int, 16>{});
+      case 5: return with(integral_constant<int, 32>{});
+      default: return with(integral_constant<int, 64>{});
+    }
+  });
+}
+
+void scan_shape(ScanArgs& a, const spc_scan_desc* d) {
+  a.channels = d->channels, a.groups = d->groups, a.share = d->channels / d->groups, a.N = d->states;
+  a.blocks = (a.share + 63) / 64 * a.groups;
+  a.softplus = d->softplus != 0;
+}
+// Rows of a segment, a multiple of `unit`: as few as give some `waves` waves, but not so few that the chain of a scene's segments takes longer than a segment.
+int segment_rows(const spc_scan_desc* d, int blocks, int waves, int unit, int most) {
+  const int64_t fill = d->n_rows * blocks / waves;
+  const double chain = std::sqrt(double(d->n_rows) / d->n_scenes / 4);
+  const int64_t rows = std::max<int64_t>(fill, std::llround(chain));
+  return static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(unit, (rows + unit - 1) / unit * unit)));
+}
+int check_grid(const ScanArgs& a, int threads) {  // (a launch takes less than 2^32 threads)
+  if (int64_t(a.ids) * a.blocks * threads < (int64_t(1) << 32) && (int64_t(a.scenes.n_scenes) * a.channels << log_padded(a.N)) < (int64_t(1) << 31)) return SPC_OK;
+  return set_error(SPC_ERR_UNSUPPORTED, "%d rows of %d channels and %d states in %d scenes", a.scenes.n_rows, a.channels, a.N, a.scenes.n_scenes);
+}
+template <typename T>
+void launch_low(const ScanArgs& a, int log_np, hipStream_t s) {
+  const int64_t n = (int64_t(a.scenes.n_rows) + 1) * a.groups << (log_np + 1);
+  hipLaunchKernelGGL(scan_low_kernel<T>, dim3(std::min<int64_t>((n + 255) / 256, 8192)), dim3(256), 0, s, a.b, a.c, a.low, a.scenes.n_rows, a.groups, a.N, log_np);
+}
+void launch_chain(const ScanArgs& a, int np, bool grad, hipStream_t s) {
+  const int64_t n = int64_t(a.scenes.n_scenes) * np * a.channels;
+  hipLaunchKernelGGL(scan_chain_kernel, dim3((n + 255) / 256, grad ? 2 : 1), dim3(256), 0, s, a, np);
+}
+
+}  // namespace
+}  // namespace spc
+
+extern "C" int spc_selective_scan_forward(const spc_scan_desc* d, const void* u, int64_t ld_u, const void* dt, int64_t ld_dt, const float* A, const spc_attn_rows* B,
+                                          const spc_attn_rows* C, const float* skip, const void* gate, int64_t ld_gate, const float* dt_bias, const int32_t* offsets,
+                                          const float* state_in, void* out, int64_t ld_out, float* state_out, void* stream) {
+  using namespace spc;
+  SPC_RETURN_IF(check_scan(d, A, true, offsets));
+  if (d->n_rows) {
+    SPC_RETURN_IF(check_matrix("u", u, ld_u, d));
+    SPC_RETURN_IF(check_matrix("dt", dt, ld_dt, d));
+    if (gate) SPC_RETURN_IF(check_matrix("gate", gate, ld_gate, d));
+    SPC_RETURN_IF(check_matrix("out", out, ld_out, d));
+    SPC_RETURN_IF(check_low("B", B, d, false));
+    SPC_RETURN_IF(check_low("C", C, d, false));
+  }
+  if (state_out && state_out == state_in) return set_error(SPC_ERR_ARG, "state_out is state_in");
+  if (!d->n_rows && !state_out) return SPC_OK;
+  const StreamId s(static_cast<hipStream_t>(stream));
+  const StreamWorkNote note{s};
+  const int log_np = log_padded(d->states), np = 1 << log_np;
+  ScanArgs a{};
+  scan_shape(a, d);
+  a.u = u, a.ld_u = ld_u, a.dt = dt, a.ld_dt = ld_dt, a.gate = gate, a.ld_gate = ld_gate, a.out = out, a.ld_out = ld_out;
+  if (d->n_rows) a.b = low_rows(B), a.c = low_rows(C);
+  a.A = A, a.skip = skip, a.bias = dt_bias, a.state_in = state_in, a.state_out = state_out;
+  a.scenes = {offsets, static_cast<int>(d->n_rows), d->n_scenes, segment_rows(d, a.blocks, 4096, 16, 4096)};
+  a.ids = a.scenes.ids();
+  SPC_RETURN_IF(check_grid(a, 64));
+  const bool cut = d->n_rows > a.scenes.seg_rows;
+  const size_t low = ((size_t(d->n_rows) + 1) * a.groups * 2) << log_np, states = cut ? size_t(a.ids) * np * a.channels : 0, steps = cut ? size_t(a.ids) * a.channels : 0;
+  float* ws = static_cast<float*>(pool_alloc(scratch_bytes((low + states + steps) * sizeof(float)), s));
+  if (!ws) return SPC_ERR_NOMEM;
+  a.low = ws, a.between = ws + low, a.steps = a.between + states;
+  scan_variant(d, gate != nullptr, [&](auto t, auto n, auto g) {
+    using T = decltype(t);
+    constexpr int NP = decltype(n)::value;
+    constexpr bool GATE = decltype(g)::value;
+    if (d->n_rows) launch_low<T>(a, log_np, s);
+    if (cut) {
+      hipLaunchKernelGGL((scan_kernel<T, NP, false, true, false>), dim3(a.ids * a.blocks), dim3(64), 0, s, a);
+      launch_chain(a, np, false, s);
+    }
+    hipLaunchKernelGGL((scan_kernel<T, NP, GATE, false, false>), dim3(a.ids * a.blocks), dim3(64), 0, s, a);
+  });
+  pool_free(ws, s);
+  SPC_HIP_CHECK(hipGetLastError());
+  return SPC_OK;
+}
+
+extern "C" int spc_selective_scan_backward(const spc_scan_desc* d, const void* dout, int64_t ld_dout, const void* u, int64_t ld_u, const void* dt, int64_t ld_dt, const float* A,
+                                           const spc_attn_rows* B, const spc_attn_rows* C, const float* skip, const void* gate, int64_t ld_gate, const float* dt_bias,
+                                           const int32_t* offsets, const float* state_in, const float* dstate_out, void* du, int64_t ld_du, void* ddt, int64_t ld_ddt, float* dA,
+                                           const spc_attn_rows* dB, const spc_attn_rows* dC, float* dskip, void* dgate, int64_t ld_dgate, float* ddt_bias, float* dstate_in,
+                                           void* stream) {
+  using namespace spc;
+  SPC_RETURN_IF(check_scan(d, A, true, offsets));
+  if (d->n_rows) {
+    SPC_RETURN_IF(check_matrix("dout", dout, ld_dout, d));
+    SPC_RETURN_IF(check_matrix("u", u, ld_u, d));
+    SPC_RETURN_IF(check_matrix("dt", dt, ld_dt, d));
+    SPC_RETURN_IF(check_matrix("du", du, ld_du, d));
+    SPC_RETURN_IF(check_matrix("ddt", ddt, ld_ddt, d));
+    if (gate) {
+      SPC_RETURN_IF(check_matrix("gate", gate, ld_gate, d));
+      SPC_RETURN_IF(check_matrix("dgate", dgate, ld_dgate, d));
+    }
+    SPC_RETURN_IF(check_low("B", B, d, false));
+    SPC_RETURN_IF(check_low("C", C, d, false));
+    SPC_RETURN_IF(check_low("dB", dB, d, true));
+    SPC_RETURN_IF(check_low("dC", dC, d, true));
+  }
+  if (dstate_in && dstate_in == dstate_out) return set_error(SPC_ERR_ARG, "dstate_in is dstate_out");
+  const StreamId s(static_cast<hipStream_t>(stream));
+  const StreamWorkNote note{s};
+  const int log_np = log_padded(d->states), np = 1 << log_np, waves = np <= 16 ? np / 4 : np / 8;
+  ScanArgs a{};
+  scan_shape(a, d);
+  a.u = u, a.ld_u = ld_u, a.dt = dt, a.ld_dt = ld_dt, a.gate = gate, a.ld_gate = ld_gate, a.dout = dout, a.ld_dout = ld_dout;
+  a.out = du, a.ld_out = ld_du, a.ddt = ddt, a.ld_ddt = ld_ddt, a.dgate = dgate, a.ld_dgate = ld_dgate;
+  if (d->n_rows) a.b = low_rows(B), a.c = low_rows(C), a.db = low_rows(dB), a.dc = low_rows(dC);
+  a.A = A, a.skip = skip, a.bias = dt_bias, a.state_in = state_in, a.dstate_out = dstate_out, a.dstate_in = dstate_in;
+  a.scenes = {offsets, static_cast<int>(d->n_rows), d->n_scenes, segment_rows(d, a.blocks, 4096, 16, 128 >> std::max(0, log_np - 4))};
+  a.ids = a.scenes.ids();
+  SPC_RETURN_IF(check_grid(a, 64 * waves));
+  const bool cut = d->n_rows > a.scenes.seg_rows, shared = a.blocks > a.groups;
+  const size_t low = ((size_t(d->n_rows) + 1) * a.groups * 2) << log_np, states = cut ? size_t(a.ids) * np * a.channels : 0, steps = cut ? size_t(a.ids) * a.channels : 0;
+  const size_t parts = size_t(a.ids) * (np + 2) * a.channels, low_parts = shared ? (size_t(a.blocks) * d->n_rows * 2) << log_np : 0;
+  float* ws = static_cast<float*>(pool_alloc(scratch_bytes((low + 2 * states + steps + parts + low_parts) * sizeof(float)), s));
+  if (!ws) return SPC_ERR_NOMEM;
+  a.low = ws, a.between = ws + low, a.behind = a.between + states, a.steps = a.behind + states, a.parts = a.steps + steps;
+  a.low_parts = shared ? a.parts + parts : nullptr;
+  int rc = SPC_OK;
+  scan_variant(d, gate != nullptr, [&](auto t, auto n, auto g) {
+    using T = decltype(t);
+    constexpr int NP = decltype(n)::value, NG = NP <= 16 ? 4 : 8, L = NP <= 16 ? 16 : 8, LP = NP / NG;
+    constexpr bool GATE = decltype(g)::value;
+    const size_t lds = GradLds<NG, L, LP, GATE>::bytes(a.scenes.seg_rows / L);
+    constexpr auto kernel = scan_grad_kernel<T, NG, L, LP, GATE>;
+    if (lds > 64 * 1024) {
+      static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+      if (attr != hipSuccess) {
+        rc = set_error(SPC_ERR_HIP, "hipFuncSetAttribute failed: %s", hipGetErrorString(attr));
+        return;
+      }
+    }
+    if (d->n_rows) launch_low<T>(a, log_np, s);
+    if (cut) {
+      hipLaunchKernelGGL((scan_kernel<T, NP, GATE, true, true>), dim3(a.ids * a.blocks), dim3(64), 0, s, a);
+      launch_chain(a, np, true, s);
+    }
+    hipLaunchKernelGGL(kernel, dim3(a.ids * a.blocks), dim3(64 * LP), lds, s, a);
+    if (shared && d->n_rows) {
+      const int64_t m = d->n_rows * a.groups << (log_np + 1);
+      hipLaunchKernelGGL(scan_low_grad_kernel<T>, dim3(std::min<int64_t>((m + 255) / 256, 8192)), dim3(256), 0, s, a, log_np);
+    }
+  });
+  if (rc == SPC_OK && (dA || dskip || ddt_bias))
+    hipLaunchKernelGGL(scan_params_kernel, dim3(((np + 2) * a.channels + 31) / 32), dim3(1024), 0, s, a.parts, a.ids, np, a.channels, a.N, dA, dskip, ddt_bias);
+  pool_free(ws, s);
+  SPC_RETURN_IF(rc);
+  SPC_HIP_CHECK(hipGetLastError());
+  return SPC_OK;
+}
+
+extern "C" int spc_selective_scan_step(const spc_scan_desc* d, const void* u, int64_t ld_u, const void* dt, int64_t ld_dt, const float* A, const spc_attn_rows* B,
+                                       const spc_attn_rows* C, const float* skip, const void* gate, int64_t ld_gate, const float* dt_bias, float* state, void* out, int64_t ld_out,
+                                       void* stream) {
+  using namespace spc;
+  SPC_RETURN_IF(check_scan(d, A, false, nullptr));
+  if (!d->n_rows) return SPC_OK;
+  SPC_RETURN_IF(check_matrix("u", u, ld_u, d));
+  SPC_RETURN_IF(check_matrix("dt", dt, ld_dt, d));
+  if (gate) SPC_RETURN_IF(check_matrix("gate", gate, ld_gate, d));
+  SPC_RETURN_IF(check_matrix("out", out, ld_out, d));
+  SPC_RETURN_IF(check_low("B", B, d, false));
+  SPC_RETURN_IF(check_low("C", C, d, false));
+  if (!state) return set_error(SPC_ERR_ARG, "state is NULL");
+  const int vec = d->states % 4 ? 1 : 4;
+  int log_q = 0;
+  while ((vec << log_q) < d->states) ++log_q;
+  if (d->n_rows >= (int64_t(1) << 31) / d->channels >> log_q) return set_error(SPC_ERR_UNSUPPORTED, "%lld streams of %d channels and %d states", static_cast<long long>(d->n_rows), d->channels, d->states);
+  ScanArgs a{};
+  scan_shape(a, d);
+  a.u = u, a.ld_u = ld_u, a.dt = dt, a.ld_dt = ld_dt, a.gate = gate, a.ld_gate = ld_gate, a.out = out, a.ld_out = ld_out, a.b = low_rows(B), a.c = low_rows(C);
+  a.A = A, a.skip = skip, a.bias = dt_bias;
+  by_dtype(d->dtype, [&](auto t) {
+    using T = decltype(t);
+    const int64_t threads = d->n_rows * d->channels << log_q;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((threads + 255) / 256), dim3(256), 0, static_cast<hipStream_t>(stream), a, state, d->n_rows, log_q); };
+    if (vec == 4) gate ? go(scan_step_kernel<T, 4, true>) : go(scan_step_kernel<T, 4, false>);
+    else gate ? go(scan_step_kernel<T, 1, true>) : go(scan_step_kernel<T, 1, false>);
+  });
+  SPC_HIP_CHECK(hipGetLastError());
+  return SPC_OK;
+}

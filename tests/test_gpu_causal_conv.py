@@ -1,0 +1,233 @@
+"""Short causal convolution along scenes, forward, backward and by single rows, against the formula in 64 bits.
+
+Tolerances.  u: half a unit in the last place of the rows' type, the one rounding of an output.  p is a chain of width + 1 fp32 additions: ep = 6 x 2^-24 of its sum of
+magnitudes.  The sigmoid's exponent is off by up to 2^-23 |p| (16-bit rows), the rest of it by a few 2^-24: es = (|p| + 8) 2^-22 of it.  y: 1.1 ep + es |y| (a slope
+of SiLU is at most 1.1); its slope: ep / 2 + 2 es (1 + |p|).  Column sums are chains of at most some 400 additions for the sizes here: 2^-15 of the sum of magnitudes."""
+import pytest
+import torch
+
+from paper_2511_20834_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+U = {F16: 2.0 ** -11, BF16: 2.0 ** -8, F32: 2.0 ** -24}
+TINY = {F16: 2.0 ** -24, BF16: 0.0, F32: 0.0}
+
+
+def within(got, ref, tol, what):
+    got, ref, tol = got.double().cpu(), ref.cpu(), tol.cpu()
+    assert got.shape == ref.shape, what
+    if not got.numel():
+        return
+    over = (got - ref).abs() - tol
+    assert torch.isfinite(got).all() and over.max() <= 0, (what, float(over.max()), int(over.argmax()))
+
+
+def matrix(n, c, dtype, gen, pitch=0, first=0):
+    t = torch.randn(n, c, generator=gen).to(dtype).cuda()
+    if not pitch:
+        return t
+    wide = torch.full((n, c + pitch), float("nan"), dtype=dtype, device="cuda")
+    wide[:, first:first + c] = t
+    return wide[:, first:first + c]
+
+
+def offsets_of(lengths, before=0):
+    return torch.tensor([0, *lengths]).cumsum(0).add(before).to(torch.int32).cuda()
+
+
+def windows(x, past, w, at):
+    """Per scene the rows x_{t-k}: [k][t][c]; rows in front from `past`."""
+    out = []
+    for b, (lo, hi) in enumerate(zip(at, at[1:])):
+        front = past[b].double() if past is not None else torch.zeros(w - 1, x.shape[1], dtype=torch.float64, device=x.device)
+        seq = torch.cat([front, x[lo:hi].double()])
+        out.append((seq, torch.stack([seq[w - 1 - k:w - 1 - k + hi - lo] for k in range(w)])))
+    return out
+
+
+def reference(x, weight, bias, past, at, silu, dy=None, dpast=None):
+    """Forward results and, with dy, gradients; each with its tolerance before the last rounding, scenes one after the other."""
+    w, c = weight.shape[1], x.shape[1]
+    wt = torch.flip(weight.double(), [1]).t()[:, None]
+    b0 = torch.zeros(c, dtype=torch.float64, device=x.device) if bias is None else bias.double()
+    res = {k: [] for k in ("y", "past", "dx", "dpast")}
+    tol = {k: [] for k in ("y", "dx", "dpast")}
+    dw, dw_tol, db, db_tol = 0, 0, 0, 0
+    for b, (seq, win) in enumerate(windows(x, past, w, at)):
+        n = win.shape[1]
+        p, ep = b0 + (win * wt).sum(0), 6 * 2.0 ** -24 * (b0.abs() + (win * wt).abs().sum(0))
+        sig = torch.sigmoid(p)
+        es = (p.abs() + 8) * 2.0 ** -22
+        y = p * sig if silu else p
+        res["y"].append(y)
+        tol["y"].append(1.1 * ep + es * y.abs() if silu else ep)
+        res["past"].append(seq[n:])
+        if dy is None:
+            continue
+        g = dy[at[b]:at[b + 1]].double()
+        slope = sig * (1 + p * (1 - sig)) if silu else torch.ones_like(p)
+        d, ed = g * slope, g.abs() * (ep / 2 + 2 * es * (1 + p.abs()) if silu else 0 * ep)
+        dseq, eseq, mag = (torch.zeros_like(seq) for _ in range(3))
+        for k in range(w):
+            dseq[w - 1 - k:w - 1 - k + n] += wt[k] * d
+            eseq[w - 1 - k:w - 1 - k + n] += wt[k].abs() * ed
+            mag[w - 1 - k:w - 1 - k + n] += (wt[k] * d).abs()
+        if dpast is not None:
+            dseq[n:] += dpast[b].double()
+            mag[n:] += dpast[b].double().abs()
+        eseq += 6 * 2.0 ** -24 * mag
+        res["dx"].append(dseq[w - 1:])
+        tol["dx"].append(eseq[w - 1:])
+        res["dpast"].append(dseq[:w - 1])
+        tol["dpast"].append(eseq[:w - 1])
+        part = torch.flip(win * d, [0])
+        dw = dw + part.sum(1).t()
+        dw_tol = dw_tol + (2.0 ** -15 * part.abs() + torch.flip(win.abs() * ed, [0])).sum(1).t()
+        db = db + d.sum(0)
+        db_tol = db_tol + (2.0 ** -15 * d.abs() + ed).sum(0)
+    cat = lambda v: torch.cat(v) if v else None  # noqa: E731
+    out = {k: (cat(res[k]), cat(tol[k])) for k in ("y", "dx")}
+    out["past"] = torch.stack(res["past"])
+    if dy is not None:
+        out["dpast"] = torch.stack(res["dpast"]), torch.stack(tol["dpast"])
+        out |= {"dw": (dw, dw_tol), "db": (db, db_tol)}
+    return out
+
+
+def close(got, pair, dtype, what):
+    ref, tol = pair
+    within(got, ref, tol + U[dtype] * ref.abs() + TINY[dtype], what)
+
+
+SCENES = [[1], [2], [37], [0, 5, 1, 0, 700, 3], [2000], [130, 260, 1, 2, 3]]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("width", [1, 2, 3, 4])
+@pytest.mark.parametrize("lengths", SCENES, ids=str)
+@pytest.mark.parametrize("c,pitch,first,silu,states,bias", [(64, 0, 0, True, False, True), (90, 7, 3, True, True, True), (3, 0, 0, False, True, False), (600, 0, 0, True, True, True), (9, 5, 1, True, False, False)])
+def test_forward_and_backward(lengths, c, pitch, first, silu, states, bias, width, dtype):
+    gen = torch.Generator().manual_seed(sum(lengths) * 31 + c + width)
+    n, b = sum(lengths), len(lengths)
+    at = offsets_of(lengths)
+    x, dy = matrix(n, c, dtype, gen, pitch, first), matrix(n, c, dtype, gen, pitch, first)
+    weight, bv = (torch.randn(c, width, generator=gen) * width ** -0.5).cuda(), torch.randn(c, generator=gen).cuda() if bias else None
+    past, dpast = ((torch.randn(b, width - 1, c, generator=gen).to(dtype).cuda() for _ in range(2)) if states else (None, None))
+    ref = reference(x, weight, bv, past, at.tolist(), silu, dy, dpast)
+    out = torch.full((n, c + pitch + 2), 7.0, dtype=dtype, device="cuda")
+    y, last = B.spc_causal_conv_forward(x, weight, bv, at, silu=silu, initial_rows=past, want_rows=True, out=out[:, first:first + c])
+    close(y, ref["y"], dtype, "y")
+    assert torch.equal(last.double(), ref["past"])
+    assert (out[:, :first] == 7).all() and (out[:, first + c:] == 7).all()
+    dx, dw, db, dinitial = B.spc_causal_conv_backward(dy, x, weight, bv, at, silu=silu, initial_rows=past, drows=dpast, want_dinitial=True)
+    close(dx, ref["dx"], dtype, "dx")
+    close(dinitial, ref["dpast"], dtype, "dinitial")
+    within(dw, *ref["dw"], "dweight")
+    within(db, *ref["db"], "dbias")
+    if b == 1:
+        assert torch.equal(B.spc_causal_conv_forward(x, weight, bv, silu=silu, initial_rows=past)[0], y)
+    again = B.spc_causal_conv_backward(dy, x, weight, bv, at, silu=silu, initial_rows=past, drows=dpast)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dw) and torch.equal(again[2], db) and again[3] is None
+    assert torch.equal(B.spc_causal_conv_backward(dy, x, weight, bv, at, silu=silu, initial_rows=past, drows=dpast, want_params=False)[0], dx)
+
+
+@pytest.mark.parametrize("lengths,c", [([70_001], 24), ([40_000, 30_000], 40)])
+def test_long_scenes(lengths, c):
+    """Several segments a workgroup in the gradients: chains four times as long."""
+    gen = torch.Generator().manual_seed(12)
+    at, n = offsets_of(lengths), sum(lengths)
+    x, dy = matrix(n, c, BF16, gen), matrix(n, c, BF16, gen)
+    weight, bias = torch.randn(c, 4, generator=gen).cuda(), torch.randn(c, generator=gen).cuda()
+    ref = reference(x, weight, bias, None, at.tolist(), True, dy)
+    close(B.spc_causal_conv_forward(x, weight, bias, at)[0], ref["y"], BF16, "y")
+    dx, dw, db, _ = B.spc_causal_conv_backward(dy, x, weight, bias, at)
+    close(dx, ref["dx"], BF16, "dx")
+    within(dw, ref["dw"][0], 4 * ref["dw"][1], "dweight")
+    within(db, ref["db"][0], 4 * ref["db"][1], "dbias")
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("width", [1, 2, 3, 4])
+@pytest.mark.parametrize("c", [5, 64, 90])
+def test_rows_one_by_one(c, width, dtype):
+    """The same bits as the scenes at once, and the same rows kept."""
+    gen = torch.Generator().manual_seed(c + width)
+    lengths = [20, 20, 20]
+    x = matrix(60, c, dtype, gen)
+    weight, bias = torch.randn(c, width, generator=gen).cuda(), torch.randn(c, generator=gen).cuda()
+    past = torch.randn(3, width - 1, c, generator=gen).to(dtype).cuda()
+    y, last = B.spc_causal_conv_forward(x, weight, bias, offsets_of(lengths), initial_rows=past, want_rows=True)
+    for t in range(20):
+        assert torch.equal(B.spc_causal_conv_step(x[t::20], weight, past, bias), y[t::20]), t
+    assert torch.equal(past, last)
+
+
+def test_gradients_against_differences():
+    gen = torch.Generator().manual_seed(3)
+    lengths, c, w = [9, 0, 1, 30], 11, 4
+    at, n = offsets_of(lengths), sum(lengths)
+    x, dy = matrix(n, c, F32, gen), matrix(n, c, F32, gen)
+    weight, bias = torch.randn(c, w, generator=gen).cuda(), torch.randn(c, generator=gen).cuda()
+    past, dpast = (torch.randn(4, w - 1, c, generator=gen).cuda() for _ in range(2))
+    dx, dw, db, dpast_in = B.spc_causal_conv_backward(dy, x, weight, bias, at, initial_rows=past, drows=dpast, want_dinitial=True)
+
+    def loss(*a):
+        r = reference(a[0], a[1], a[2], a[3], at.tolist(), True)
+        return float((r["y"][0] * dy.double()).sum() + (r["past"] * dpast.double()).sum())
+
+    for i, grad in enumerate((dx, dw, db, dpast_in)):
+        base = [t.double() for t in (x, weight, bias, past)]
+        d = torch.randn(base[i].shape, generator=gen, dtype=torch.float64).cuda()
+        hi, lo, step = list(base), list(base), 1e-4
+        hi[i], lo[i] = base[i] + step * d, base[i] - step * d
+        num, ana = (loss(*hi) - loss(*lo)) / (2 * step), float((grad.double() * d).sum())
+        # (central differences: third derivatives times step^2; fp32 sums of some 440 terms)
+        assert abs(num - ana) <= 1e-5 * float((grad.double() * d).abs().sum()), i
+
+
+@pytest.mark.parametrize("c", [24, 5])
+def test_rows_in_no_scene_are_left_alone(c):
+    gen = torch.Generator().manual_seed(5)
+    x, dy = matrix(200, c, F16, gen), matrix(200, c, F16, gen)
+    weight = torch.randn(c, 4, generator=gen).cuda()
+    at = offsets_of([50, 0, 60], before=30)
+    y, _ = B.spc_causal_conv_forward(x[30:140], weight, offsets=offsets_of([50, 0, 60]))
+    grads = B.spc_causal_conv_backward(dy[30:140], x[30:140], weight, offsets=offsets_of([50, 0, 60]))
+    for t in (x, dy):
+        t[:30], t[140:] = float("nan"), float("inf")
+    out, dout = torch.full_like(x, 7), torch.full_like(x, 7)
+    B.spc_causal_conv_forward(x, weight, offsets=at, out=out)
+    dx, dw, db, _ = B.spc_causal_conv_backward(dy, x, weight, offsets=at, out=dout)
+    assert torch.equal(out[30:140], y) and torch.equal(dout[30:140], grads[0])
+    for t in (out, dout):
+        assert (t[:30] == 7).all() and (t[140:] == 7).all()
+    tol = 2.0 ** -14 * 110 * 8
+    assert (dw - grads[1]).abs().max() <= tol and (db - grads[2]).abs().max() <= tol and torch.isfinite(dw).all()
+
+
+def test_no_rows():
+    weight = torch.randn(16, 4, device="cuda")
+    x = torch.empty(0, 16, dtype=BF16, device="cuda")
+    past = torch.randn(2, 3, 16, device="cuda").to(BF16)
+    at = torch.zeros(3, dtype=torch.int32, device="cuda")
+    y, last = B.spc_causal_conv_forward(x, weight, offsets=at, initial_rows=past, want_rows=True)
+    assert y.shape == (0, 16) and torch.equal(last, past)
+    dx, dw, db, dpast = B.spc_causal_conv_backward(x, x, weight, offsets=at, initial_rows=past, drows=past, want_dinitial=True)
+    assert dx.shape == (0, 16) and (dw == 0).all() and (db == 0).all() and torch.equal(dpast, past)
+    assert B.spc_causal_conv_step(x, weight, past[:0]).shape == (0, 16)
+
+
+def test_infinities_and_nan_reach_later_rows_of_their_channel_only():
+    gen = torch.Generator().manual_seed(6)
+    x, weight = matrix(100, 24, F32, gen), torch.randn(24, 4, generator=gen).cuda()
+    at = offsets_of([40, 60])
+    y, _ = B.spc_causal_conv_forward(x, weight, offsets=at)
+    x2 = x.clone()
+    x2[38, 3], x2[70, 20] = float("nan"), float("inf")
+    y2, _ = B.spc_causal_conv_forward(x2, weight, offsets=at)
+    touched = torch.zeros_like(x, dtype=torch.bool)
+    touched[38:40, 3] = True
+    touched[70:74, 20] = True
+    assert torch.equal(y2[~touched], y[~touched]) and not torch.isfinite(y2[38, 3])
