@@ -22,6 +22,10 @@ namespace {
 
 constexpr int SCAN_MAX_N = 64;
 constexpr int SCAN_MAX_C = 65536;
+constexpr int SCAN_THREADS = 256;  // four waves of segments and blocks of their own (a CU takes no more than 16 workgroups of one wave: four to a SIMD do not fill it)
+// Rows whose states are held in registers while the gradient runs back over them, and states of a lane meanwhile.
+constexpr int grad_rows(int np) { return np <= 32 ? 16 : 8; }
+constexpr int grad_states(int np) { return np <= 16 ? np / 4 : np <= 32 ? 4 : 8; }
 constexpr float LOG2E = 1.44269504f;
 
 struct LowRows {  // B or C: channel j of group g in row r is r * row + g * group + j
@@ -38,10 +42,11 @@ struct ScanArgs {
   const float *A, *skip, *bias;
   const float *state_in, *dstate_out;
   float *state_out, *dstate_in;
-  float* low;      // [row][group][B, C][NP], a row of zeros behind the last one
+  float* low;      // [row][group][16 states at a time][B, C], NP states in all, a row of zeros behind the last one
   float* between;  // [segment][NP][channels]: its state from zeros, then the state behind it
   float* behind;   // the same for the gradient: what reaches the rows in front of a segment, from zeros, then what arrives from behind it
   float* steps;    // [segment][channels]: sum of d
+  float* starts;   // [segment][chunk][NP][channels]: its state from zeros in front of every grad_rows rows but the first, and their sums of d as state NP
   float* parts;    // [segment][NP + 2][channels]: dA, dD, dbias
   float* low_parts;  // [block of channels][row][B, C][NP], where several blocks share a group
   int channels, groups, share, N, blocks, ids;  // share: channels of a group; blocks: of 64 channels, of all groups
@@ -64,11 +69,10 @@ template <typename T>
 struct Step {
   float d, slope;  // d and its derivative
   __device__ Step(float raw, bool softplus) : d(raw), slope(1.f) {
-    if (!softplus) return;
     const float e = exp_of<sizeof(T) == 4>(-fabsf(raw)), r = __builtin_amdgcn_rcpf(1.f + e);
-    d = fmaxf(raw, 0.f) + log1p_of(e);
-    if (raw != raw) d = raw;  // (the maximum passes over NaN)
-    slope = raw >= 0.f ? r : e * r;
+    const float soft = fmaxf(raw, 0.f) + log1p_of(e);  // (NaN where raw is: e is)
+    d = softplus ? soft : raw;  // (no branch, which would part the rows of an unrolled loop)
+    slope = softplus ? (raw >= 0.f ? r : e * r) : 1.f;
   }
 };
 
@@ -85,6 +89,10 @@ struct Lane {
   }
 };
 
+// States are taken NB at a time: as many values of B and C as fit the scalar registers twice.
+template <int NP>
+constexpr int NB = NP < 8 ? NP : 8;
+
 __device__ inline Scalars low_row(const ScanArgs& a, int64_t row, int group, int np) {
   return (Scalars)(uintptr_t)(a.low + (row * a.groups + group) * (2 * np));
 }
@@ -92,11 +100,12 @@ __device__ inline Scalars low_row(const ScanArgs& a, int64_t row, int group, int
 // B and C as floats, N of them filled up to NP with zeros.
 template <typename T>
 __global__ __launch_bounds__(256) void scan_low_kernel(LowRows b, LowRows c, float* low, int n_rows, int groups, int N, int log_np) {
+  const int log_nb = min(log_np, 3);
   const int64_t n = (int64_t(n_rows) + 1) * groups << (log_np + 1);
   for (int64_t i = blockIdx.x * int64_t(256) + threadIdx.x; i < n; i += gridDim.x * int64_t(256)) {
-    const int j = static_cast<int>(i & ((1 << log_np) - 1));
+    const int at = static_cast<int>(i & ((2 << log_np) - 1)), j = (at >> (log_nb + 1) << log_nb) + (at & ((1 << log_nb) - 1));
     const int64_t rg = i >> (log_np + 1), row = rg / groups, g = rg - row * groups;
-    const LowRows& from = i >> log_np & 1 ? c : b;
+    const LowRows& from = at >> log_nb & 1 ? c : b;
     low[i] = row < n_rows && j < N ? static_cast<float>(static_cast<const T*>(from.p)[row * from.row + g * from.group + j]) : 0.f;
   }
 }
@@ -105,12 +114,19 @@ __global__ __launch_bounds__(256) void scan_low_kernel(LowRows b, LowRows c, flo
 template <int NP>
 __device__ inline void rates(float (&A2)[NP], const ScanArgs& a, int channel, int first) {
 #pragma unroll
-  for (int n = 0; n < NP; ++n) A2[n] = first + n < a.N ? a.A[int64_t(channel) * a.N + first + n] * LOG2E : 0.f;
+  for (int n = 0; n < NP; ++n) A2[n] = a.A[int64_t(channel) * a.N + min(first + n, a.N - 1)];  // (all loads under way at once: none hangs on a branch)
+#pragma unroll
+  for (int n = 0; n < NP; ++n) A2[n] = first + n < a.N ? A2[n] * LOG2E : 0.f;
 }
 template <int NP>
 __device__ inline void load_state(float (&h)[NP], const float* p, const ScanArgs& a, int scene, const Lane& me, int first) {
 #pragma unroll
-  for (int n = 0; n < NP; ++n) h[n] = p && me.some && first + n < a.N ? p[(int64_t(scene) * a.channels + me.channel) * a.N + first + n] : 0.f;
+  for (int n = 0; n < NP; ++n) h[n] = 0.f;
+  if (!p) return;
+#pragma unroll
+  for (int n = 0; n < NP; ++n) h[n] = p[(int64_t(scene) * a.channels + me.channel) * a.N + min(first + n, a.N - 1)];
+#pragma unroll
+  for (int n = 0; n < NP; ++n) h[n] = me.some && first + n < a.N ? h[n] : 0.f;
 }
 template <int NP>
 __device__ inline void store_state(const float (&h)[NP], float* p, const ScanArgs& a, int scene, const Lane& me, int first) {
@@ -125,32 +141,39 @@ __device__ inline void load_between(float (&h)[NP], const float* p, const ScanAr
   for (int n = 0; n < NP; ++n) h[n] = me.some ? p[(int64_t(id) * ALL + first + n) * a.channels + me.channel] : 0.f;
 }
 
-// What a lane reads of `U` rows.
-template <typename T, int U, bool GATE, bool GRAD>
-struct Inputs {
-  T u[U], dt[U], gate[GATE ? U : 1], dout[GRAD ? U : 1];
-  __device__ void load(const ScanArgs& a, const Lane& me, int64_t first, int t, int rows) {
-#pragma unroll
-    for (int q = 0; q < U; ++q) {
-      const int64_t row = first + min(t + q, rows - 1);
-      u[q] = static_cast<const T*>(a.u)[row * a.ld_u + me.channel];
-      dt[q] = static_cast<const T*>(a.dt)[row * a.ld_dt + me.channel];
-      if (GATE) gate[q] = static_cast<const T*>(a.gate)[row * a.ld_gate + me.channel];
-      if (GRAD) dout[q] = static_cast<const T*>(a.dout)[row * a.ld_dout + me.channel];
-    }
+// The rows of a matrix from `first` on, one after the other: a scalar address that moves on by the pitch, and the lane's place in a row.
+template <typename T>
+struct Walk {
+  const char* row;
+  int64_t pitch;
+  __device__ Walk(const void* p, int64_t ld, int64_t first) : row(static_cast<const char*>(p) + first * ld * int64_t(sizeof(T))), pitch(ld * int64_t(sizeof(T))) {}
+  __device__ T next(unsigned at) {
+    const T v = *reinterpret_cast<const T*>(row + at);
+    on();
+    return v;
+  }
+  __device__ void on() {
+    row += pitch;
+    asm("" : "+s"(row));  // (else every row of an unrolled loop has an offset of its own in scalar registers, which then do not suffice)
+  }
+  __device__ void put(unsigned at, T v) {
+    *reinterpret_cast<T*>(const_cast<char*>(row) + at) = v;
+    on();
   }
 };
 
-// SUMS: a segment's own state, its sum of d, and (GRAD) what its rows send to those in front of it.  Else: outputs.
+// SUMS: a segment's own state, its sum of d, and (GRAD) what its rows send to those in front of it.  Else: outputs.  Rows are taken U at a time while
+// the next ones are on their way, and B and C of the next NB states while those at hand are used.
 template <typename T, int NP, bool GATE, bool SUMS, bool GRAD>
-__global__ __launch_bounds__(64) void scan_kernel(const ScanArgs a) {
-  constexpr int U = 8;
-  constexpr bool EXACT = sizeof(T) == 4, GATED = GATE && (GRAD || !SUMS);
-  const int id = blockIdx.x / a.blocks, block = blockIdx.x - id * a.blocks;
+__global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const ScanArgs a) {
+  constexpr int U = 4, N1 = NB<NP>, BLOCKS = NP / N1;
+  constexpr bool EXACT = sizeof(T) == 4, GATED = GATE && (GRAD || !SUMS), NEEDS_C = GRAD || !SUMS;
+  const int unit = blockIdx.x * (SCAN_THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64), id = unit / a.blocks, block = unit - id * a.blocks;
   SceneSegment s;
-  if (!s.find(a.scenes, id) || (SUMS && (s.n == 1 || (!GRAD && s.m == s.n - 1)))) return;
+  if (!s.find(a.scenes, id) || (SUMS && !GRAD && s.m == s.n - 1)) return;
   s.uniform();
-  const Lane me(a, block, threadIdx.x);
+  const Lane me(a, block, threadIdx.x % 64);
+  if (!me.some) return;
   const float bias = a.bias ? a.bias[me.channel] : 0.f, skip = a.skip ? a.skip[me.channel] : 0.f;
   float A2[NP], h[NP], sent[GRAD ? NP : 1] = {}, through[GRAD ? NP : 1], steps = 0.f;
   rates<NP>(A2, a, me.channel, 0);
@@ -165,57 +188,109 @@ __global__ __launch_bounds__(64) void scan_kernel(const ScanArgs a) {
   } else {
     load_between<NP, NP>(h, a.between, a, id - 1, me, 0);
   }
-  Inputs<T, U, GATED, GRAD> now, next;
-  if (s.rows > 0) now.load(a, me, s.first, 0, s.rows);
-  for (int t = 0; t < s.rows; t += U) {
-    if (t + U < s.rows) next.load(a, me, s.first, t + U, s.rows);
+  const unsigned at = unsigned(me.channel) * unsigned(sizeof(T));
+  Walk<T> in_u(a.u, a.ld_u, s.first), in_dt(a.dt, a.ld_dt, s.first), in_gate(a.gate, a.ld_gate, s.first), in_dout(a.dout, a.ld_dout, s.first), out(a.out, a.ld_out, s.first);
+  struct Row {
+    T u, dt, gate, dout;
+  };
+  auto load = [&](Row& r) {
+    r.u = in_u.next(at);
+    r.dt = in_dt.next(at);
+    if (GATED) r.gate = in_gate.next(at);
+    if (GRAD) r.dout = in_dout.next(at);
+  };
+  Scalars low = low_row(a, s.first, me.group, NP);
+  const int64_t low_pitch = int64_t(a.groups) * (2 * NP);
+  float bc[2 * N1];
+  auto fetch = [&](float (&to)[2 * N1], Scalars from) {
 #pragma unroll
-    for (int q = 0; q < U; ++q) {
-      if (t + q >= s.rows) break;
-      const int64_t row = int64_t(s.first) + t + q;
-      const Scalars low = low_row(a, row, me.group, NP);
-      const float u = static_cast<float>(now.u[q]), d = Step<T>(static_cast<float>(now.dt[q]) + bias, a.softplus).d, x = d * u;
-      float dy = 0.f, y = 0.f;
-      if constexpr (GRAD) {
-        dy = static_cast<float>(now.dout[q]);
-        if constexpr (GATED) {
-          const float z = static_cast<float>(now.gate[q]);
-          dy *= z * sigmoid_of<EXACT>(z);
-        }
-      }
-      if (SUMS) steps += d;
-#pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        const float e = __builtin_amdgcn_exp2f(d * A2[n]);
-        h[n] = fmaf(e, h[n], x * low[n]);
-        if (!SUMS) y = fmaf(low[NP + n], h[n], y);
-        if constexpr (GRAD) {
-          through[n] *= e;
-          sent[n] = fmaf(through[n], dy * low[NP + n], sent[n]);
-        }
-      }
-      if (!SUMS) {
-        y = fmaf(skip, u, y);
-        if constexpr (GATED) {
-          const float z = static_cast<float>(now.gate[q]);
-          y *= z * sigmoid_of<EXACT>(z);
-        }
-        if (me.some) static_cast<T*>(a.out)[row * a.ld_out + me.channel] = static_cast<T>(y);
+    for (int n = 0; n < (NEEDS_C ? 2 : 1) * N1; ++n) to[n] = from[n];
+  };
+  fetch(bc, low);
+  auto compute = [&](const Row& r) {
+    const float u = static_cast<float>(r.u), d = Step<T>(static_cast<float>(r.dt) + bias, a.softplus).d, x = d * u;
+    float dy = 0.f, y = 0.f;
+    if constexpr (GRAD) {
+      dy = static_cast<float>(r.dout);
+      if constexpr (GATED) {
+        const float z = static_cast<float>(r.gate);
+        dy *= z * sigmoid_of<EXACT>(z);
       }
     }
-    now = next;
+    if (SUMS) steps += d;
+#pragma unroll
+    for (int k = 0; k < BLOCKS; ++k) {
+      float ahead[2 * N1];
+      const Scalars behind = k + 1 < BLOCKS ? low + 2 * N1 * (k + 1) : low + low_pitch;
+      fetch(ahead, behind);  // (behind the last row of all there is one of zeros)
+      if (k + 1 == BLOCKS) low = behind;
+      __builtin_amdgcn_sched_barrier(0);  // (else the loads are put where their values are used)
+#pragma unroll
+      for (int n = 0; n < N1; ++n) {
+        const int j = k * N1 + n;
+        const float e = __builtin_amdgcn_exp2f(d * A2[j]);
+        h[j] = fmaf(e, h[j], x * bc[n]);
+        if (!SUMS) y = fmaf(bc[N1 + n], h[j], y);
+        if constexpr (GRAD) {
+          through[j] *= e;
+          sent[j] = fmaf(through[j], dy * bc[N1 + n], sent[j]);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < (NEEDS_C ? 2 : 1) * N1; ++n) bc[n] = ahead[n];
+    }
+    if (!SUMS) {
+      y = fmaf(skip, u, y);
+      if constexpr (GATED) {
+        const float z = static_cast<float>(r.gate);
+        y *= z * sigmoid_of<EXACT>(z);
+      }
+      out.put(at, static_cast<T>(y));
+    }
+  };
+  auto start = [&](int t) {  // in front of row t
+    constexpr int L = grad_rows(NP);
+    if (!(SUMS && GRAD) || t % L || !t) return;
+    float* to = a.starts + (int64_t(id) * (a.scenes.seg_rows / L) + t / L) * (NP + 1) * a.channels + me.channel;
+#pragma unroll
+    for (int n = 0; n < NP; ++n) to[int64_t(n) * a.channels] = h[n];
+    to[int64_t(NP) * a.channels] = steps;
+  };
+  int t = 0;
+  if (s.rows >= U) {
+    Row now[U], next[U];
+#pragma unroll
+    for (int q = 0; q < U; ++q) load(now[q]);
+    for (; t + 2 * U <= s.rows; t += U) {
+      start(t);
+#pragma unroll
+      for (int q = 0; q < U; ++q) load(next[q]);
+#pragma unroll
+      for (int q = 0; q < U; ++q) compute(now[q]);
+#pragma unroll
+      for (int q = 0; q < U; ++q) now[q] = next[q];
+    }
+    start(t);
+#pragma unroll
+    for (int q = 0; q < U; ++q) compute(now[q]);
+    t += U;
+  }
+  for (; t < s.rows; ++t) {
+    start(t);
+    Row r;
+    load(r);
+    compute(r);
   }
   if (!SUMS) {
     if (s.m == s.n - 1) store_state<NP>(h, a.state_out, a, s.scene, me, 0);
     return;
   }
-  if (!me.some) return;
   a.steps[int64_t(id) * a.channels + me.channel] = steps;
 #pragma unroll
   for (int n = 0; n < NP; ++n) {
-    const int64_t at = (int64_t(id) * NP + n) * a.channels + me.channel;
-    a.between[at] = h[n];
-    if (GRAD) a.behind[at] = sent[n];
+    const int64_t to = (int64_t(id) * NP + n) * a.channels + me.channel;
+    a.between[to] = h[n];
+    if (GRAD) a.behind[to] = sent[n];
   }
 }
 
@@ -266,52 +341,56 @@ template <int CTRL>
 __device__ inline float halves(float a, float b, bool upper) {  // a of this lane and its partner where `upper` is false, b where it is true
   return (upper ? b : a) + from_lane<CTRL>(upper ? a : b);
 }
-// Sums of V values over the 64 lanes: lane l ends with value l / (64 / V).  Half of the values go with every step.
+template <bool WIDE>
+__device__ inline float swapped(float a, float b) {  // the same for lanes 32 (16) apart: a in the lower ones, b in the upper
+  const unsigned x = __builtin_bit_cast(unsigned, a), y = __builtin_bit_cast(unsigned, b);
+  const auto r = [&] {
+    if constexpr (WIDE) return __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    else return __builtin_amdgcn_permlane16_swap(x, y, false, false);
+  }();
+  const unsigned p = r[0], q = r[1];  // (a cast of r[1] itself is one of r[0] to the compiler)
+  return __builtin_bit_cast(float, p) + __builtin_bit_cast(float, q);
+}
+// Sums of V values over the 64 lanes: lane l ends with value l / (64 / V).  Half of the values go with every step, while there are several.
 template <int V>
 __device__ inline float sums_over_lanes(float (&v)[V], int lane) {
-  static_assert(V == 16 || V == 32, "two rows of four or eight states");
+  static_assert(V >= 4 && V <= 32, "two rows of one to eight states");
 #pragma unroll
-  for (int k = 0; k < V / 2; ++k) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v[k]), __builtin_bit_cast(unsigned, v[k + V / 2]), false, false);
-    const unsigned a = r[0], b = r[1];  // (a cast of r[1] itself is one of r[0] to the compiler)
-    v[k] = __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
-  }
+  for (int k = 0; k < V / 2; ++k) v[k] = swapped<true>(v[k], v[k + V / 2]);
 #pragma unroll
-  for (int k = 0; k < V / 4; ++k) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v[k]), __builtin_bit_cast(unsigned, v[k + V / 4]), false, false);
-    const unsigned a = r[0], b = r[1];  // (a cast of r[1] itself is one of r[0] to the compiler)
-    v[k] = __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
-  }
+  for (int k = 0; k < V / 4; ++k) v[k] = swapped<false>(v[k], v[k + V / 4]);
+  if constexpr (V >= 8) {
 #pragma unroll
-  for (int k = 0; k < V / 8; ++k) v[k] = halves<XOR_8>(v[k], v[k + V / 8], lane & 8);
+    for (int k = 0; k < V / 8; ++k) v[k] = halves<XOR_8>(v[k], v[k + V / 8], lane & 8);
+  } else v[0] += from_lane<XOR_8>(v[0]);
+  if constexpr (V >= 16) {
 #pragma unroll
-  for (int k = 0; k < V / 16; ++k) v[k] = halves<XOR_7>(v[k], v[k + V / 16], lane & 4);
-  if constexpr (V == 32) v[0] = halves<XOR_2>(v[0], v[1], lane & 2);
+    for (int k = 0; k < V / 16; ++k) v[k] = halves<XOR_7>(v[k], v[k + V / 16], lane & 4);
+  } else v[0] += from_lane<XOR_7>(v[0]);
+  if constexpr (V >= 32) v[0] = halves<XOR_2>(v[0], v[1], lane & 2);
   else v[0] += from_lane<XOR_2>(v[0]);
   return v[0] + from_lane<XOR_1>(v[0]);
 }
 
-// A workgroup has a segment of 64 channels, each of its LP waves NG of their states.  The states at the start of every chunk of L rows go to LDS in a first sweep; then chunk by
-// chunk from the last one the states are made again, kept in registers, and the gradient runs back over them.  What rows share (d, d u, dy) is made by
-// one wave a row and read by all; the sums over states (x, sum of A p, C . h) are parts of the waves, which the row's wave adds up.
+// A workgroup has a segment of 64 channels, each of its LP waves NG of their states.  Chunk by chunk from the segment's last one, the states are made again from that in
+// front of the chunk (what the first launch has left, and the decayed state in front of the segment), kept in registers with their decays, and the gradient runs back over
+// them.  What rows share (d, d u, dy) is made by one wave a row and read by all from LDS, as are B and C; the sums over states (x, sum of A p, C . h) are parts of the waves,
+// which the row's wave adds up.  The next chunk's rows are on their way meanwhile.
 constexpr int PART_ROWS = 8;
-template <int NG, int L, int LP, bool GATE>
+template <int NP, bool GATE>
 struct GradLds {
-  static constexpr int VALUES = GATE ? 3 : 2;
+  static constexpr int VALUES = GATE ? 3 : 2, L = grad_rows(NP), LP = NP / grad_states(NP);
   float stage[3][L][64];
+  float low[L][2][NP];
   float part[LP][PART_ROWS][VALUES][64];
-  // behind it: starts [LP][chunks][NG][64], of 128 rows of 16 states, or as many fewer as there are more states: 68 KB of LDS, 94, 118
-  static size_t bytes(int chunks) { return sizeof(GradLds) + size_t(LP) * chunks * NG * 64 * sizeof(float); }
 };
 
-template <typename T, int NG, int L, int LP, bool GATE>
-__global__ __launch_bounds__(64 * LP) void scan_grad_kernel(const ScanArgs a) {
-  using Lds = GradLds<NG, L, LP, GATE>;
-  constexpr int NP = NG * LP, RW = L / LP, V = 4 * NG;
-  constexpr bool EXACT = sizeof(T) == 4;
+template <typename T, int NP, bool GATE>
+__global__ __launch_bounds__(64 * NP / grad_states(NP), 2) void scan_grad_kernel(const ScanArgs a) {
+  constexpr int NG = grad_states(NP), L = grad_rows(NP), LP = NP / NG, RW = L / LP, V = 4 * NG, LOWS = L * 2 * NP, LOW = (LOWS + 64 * LP - 1) / (64 * LP);
+  constexpr bool EXACT = sizeof(T) == 4, KEEP = NG <= 4;  // KEEP: decays are kept beside the states (of eight states a lane, there is no room for them)
   extern __shared__ __attribute__((aligned(16))) char raw[];
-  Lds& lds = *reinterpret_cast<Lds*>(raw);
-  float* starts = reinterpret_cast<float*>(raw + sizeof(Lds));
+  auto& lds = *reinterpret_cast<GradLds<NP, GATE>*>(raw);
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), first_n = wave * NG;
   const int id = blockIdx.x / a.blocks, block = blockIdx.x - id * a.blocks;
   const Lane me(a, block, lane);
@@ -327,76 +406,84 @@ __global__ __launch_bounds__(64 * LP) void scan_grad_kernel(const ScanArgs a) {
   }
   s.uniform();
   const float bias = a.bias ? a.bias[me.channel] : 0.f, skip = a.skip ? a.skip[me.channel] : 0.f;
-  float A2[NG], h[NG], r[NG], dA[NG] = {};
+  float A2[NG], first_h[NG], r[NG], dA[NG] = {};
   rates<NG>(A2, a, me.channel, first_n);
-  if (s.m == 0) load_state<NG>(h, a.state_in, a, s.scene, me, first_n);
-  else load_between<NG, NP>(h, a.between, a, id - 1, me, first_n);
+  if (s.m == 0) load_state<NG>(first_h, a.state_in, a, s.scene, me, first_n);
+  else load_between<NG, NP>(first_h, a.between, a, id - 1, me, first_n);
   if (s.m == s.n - 1) load_state<NG>(r, a.dstate_out, a, s.scene, me, first_n);
   else load_between<NG, NP>(r, a.behind, a, id, me, first_n);
   const int chunks = (s.rows + L - 1) / L, room = a.scenes.seg_rows / L;
-  auto at_start = [&](int chunk, int n) -> float& { return starts[((wave * room + chunk) * NG + n) * 64 + lane]; };
-  auto low_of = [&](int t) { return low_row(a, t < s.rows ? int64_t(s.first) + t : int64_t(a.scenes.n_rows), me.group, NP); };
-  // this wave's rows of a chunk: t = chunk L + j LP + wave
-  float u[RW], d[RW], slope[RW], dout[RW], gate[GATE ? RW : 1], dy[RW];
-  auto stage = [&](int chunk, bool grad) {
-    T in_u[RW], in_dt[RW], in_g[RW], in_o[RW];
+  // what comes of a chunk: this wave's rows of it, t = chunk L + j LP + wave; this thread's values of B and C; the state in front of it
+  struct {
+    T u[RW], dt[RW], gate[GATE ? RW : 1], dout[RW], low[LOW];
+    float h[NG], steps;
+  } in;
+  auto load = [&](int chunk) {
 #pragma unroll
     for (int j = 0; j < RW; ++j) {
       const int64_t row = int64_t(s.first) + min(chunk * L + j * LP + wave, s.rows - 1);
-      in_u[j] = static_cast<const T*>(a.u)[row * a.ld_u + me.channel];
-      in_dt[j] = static_cast<const T*>(a.dt)[row * a.ld_dt + me.channel];
-      if (grad) in_o[j] = static_cast<const T*>(a.dout)[row * a.ld_dout + me.channel];
-      if (GATE && grad) in_g[j] = static_cast<const T*>(a.gate)[row * a.ld_gate + me.channel];
+      in.u[j] = static_cast<const T*>(a.u)[row * a.ld_u + me.channel];
+      in.dt[j] = static_cast<const T*>(a.dt)[row * a.ld_dt + me.channel];
+      in.dout[j] = static_cast<const T*>(a.dout)[row * a.ld_dout + me.channel];
+      if (GATE) in.gate[j] = static_cast<const T*>(a.gate)[row * a.ld_gate + me.channel];
     }
+#pragma unroll
+    for (int j = 0; j < LOW; ++j) {
+      const int i = min(j * (64 * LP) + int(threadIdx.x), LOWS - 1), n = min(i % NP, a.N - 1);
+      const int64_t row = int64_t(s.first) + min(chunk * L + i / (2 * NP), s.rows - 1);
+      const LowRows& from = i / NP % 2 ? a.c : a.b;
+      in.low[j] = static_cast<const T*>(from.p)[row * from.row + me.group * from.group + n];
+    }
+    if (!chunk) return;
+    const float* p = a.starts + (int64_t(id) * room + chunk) * (NP + 1) * a.channels + me.channel;
+#pragma unroll
+    for (int n = 0; n < NG; ++n) in.h[n] = p[int64_t(first_n + n) * a.channels];
+    in.steps = p[int64_t(NP) * a.channels];
+  };
+  float u[RW], slope[RW], through_gate[GATE ? RW : 1];  // the last: dout silu'(gate)
+  float dskip = 0.f, dbias = 0.f;
+  if (chunks) load(chunks - 1);
+  for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+    // (every wave has passed the barrier behind its last reads of what is written here, its own rows aside, which it reads to the end)
 #pragma unroll
     for (int j = 0; j < RW; ++j) {
       const int i = j * LP + wave;
       const bool there = me.some && chunk * L + i < s.rows;  // (rows that are not there leave states and gradients as they are)
-      const Step<T> step(static_cast<float>(in_dt[j]) + bias, a.softplus);
-      u[j] = there ? static_cast<float>(in_u[j]) : 0.f;
-      d[j] = there ? step.d : 0.f;
-      lds.stage[0][i][lane] = d[j];
-      lds.stage[1][i][lane] = d[j] * u[j];
-      if (!grad) continue;
+      const Step<T> step(static_cast<float>(in.dt[j]) + bias, a.softplus);
+      const float d = there ? step.d : 0.f;
+      float dy = there ? static_cast<float>(in.dout[j]) : 0.f;
+      u[j] = there ? static_cast<float>(in.u[j]) : 0.f;
       slope[j] = step.slope;
-      dout[j] = there ? static_cast<float>(in_o[j]) : 0.f;
-      dy[j] = dout[j];
       if constexpr (GATE) {
-        gate[j] = there ? static_cast<float>(in_g[j]) : 0.f;
-        dy[j] *= gate[j] * sigmoid_of<EXACT>(gate[j]);
+        const float z = there ? static_cast<float>(in.gate[j]) : 0.f, g = sigmoid_of<EXACT>(z);
+        through_gate[j] = dy * fmaf(z * g, 1.f - g, g);
+        dy *= z * g;
       }
-      lds.stage[2][i][lane] = dy[j];
+      lds.stage[0][i][lane] = d;
+      lds.stage[1][i][lane] = d * u[j];
+      lds.stage[2][i][lane] = dy;
     }
-  };
-  for (int chunk = 0; chunk + 1 < chunks; ++chunk) {
 #pragma unroll
-    for (int n = 0; n < NG; ++n) at_start(chunk, n) = h[n];
-    __syncthreads();  // (the rows before have been read)
-    stage(chunk, false);
+    for (int j = 0; j < LOW; ++j) {
+      const int i = j * (64 * LP) + threadIdx.x;
+      if (LOWS % (64 * LP) == 0 || i < LOWS) (&lds.low[0][0][0])[i] = i % NP < a.N && chunk * L + i / (2 * NP) < s.rows ? static_cast<float>(in.low[j]) : 0.f;
+    }
+    float h[NG];
+#pragma unroll
+    for (int n = 0; n < NG; ++n) h[n] = chunk ? (me.some ? fmaf(__builtin_amdgcn_exp2f(A2[n] * in.steps), first_h[n], in.h[n]) : 0.f) : first_h[n];
     __syncthreads();
+    if (chunk) load(chunk - 1);
+    float hs[L][NG], decay[KEEP ? L : 1][NG];
 #pragma unroll
     for (int i = 0; i < L; ++i) {
-      const Scalars low = low_of(chunk * L + i);
       const float di = lds.stage[0][i][lane], xi = lds.stage[1][i][lane];
+      const float* B = &lds.low[i][0][first_n];
 #pragma unroll
-      for (int n = 0; n < NG; ++n) h[n] = fmaf(__builtin_amdgcn_exp2f(di * A2[n]), h[n], xi * low[first_n + n]);
-    }
-  }
-  float dskip = 0.f, dbias = 0.f;
-  for (int chunk = chunks - 1; chunk >= 0; --chunk) {
-    if (chunk < chunks - 1)
-#pragma unroll
-      for (int n = 0; n < NG; ++n) h[n] = at_start(chunk, n);
-    __syncthreads();
-    stage(chunk, true);
-    __syncthreads();
-    float hs[L][NG];
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const Scalars low = low_of(chunk * L + i);
-      const float di = lds.stage[0][i][lane], xi = lds.stage[1][i][lane];
-#pragma unroll
-      for (int n = 0; n < NG; ++n) hs[i][n] = fmaf(__builtin_amdgcn_exp2f(di * A2[n]), i ? hs[i ? i - 1 : 0][n] : h[n], xi * low[first_n + n]);
+      for (int n = 0; n < NG; ++n) {
+        const float e = __builtin_amdgcn_exp2f(di * A2[n]);
+        if (KEEP) decay[KEEP ? i : 0][n] = e;
+        hs[i][n] = fmaf(e, i ? hs[i ? i - 1 : 0][n] : h[n], xi * B[n]);
+      }
     }
 #pragma unroll
     for (int half = L / PART_ROWS - 1; half >= 0; --half) {
@@ -406,18 +493,17 @@ __global__ __launch_bounds__(64 * LP) void scan_grad_kernel(const ScanArgs a) {
 #pragma unroll
         for (int e = 1; e >= 0; --e) {
           const int i = half * PART_ROWS + pair * 2 + e;
-          const Scalars low = low_of(chunk * L + i);
+          const float *B = &lds.low[i][0][first_n], *C = &lds.low[i][1][first_n];
           const float di = lds.stage[0][i][lane], xi = lds.stage[1][i][lane], dyi = lds.stage[2][i][lane];
           float sx = 0.f, sp = 0.f, sy = 0.f;
 #pragma unroll
           for (int n = 0; n < NG; ++n) {
-            const float B = low[first_n + n], C = low[NP + first_n + n];
-            const float q = fmaf(C, dyi, r[n]);
+            const float q = fmaf(C[n], dyi, r[n]);
             v[e * 2 * NG + n] = q * xi;
             v[e * 2 * NG + NG + n] = hs[i][n] * dyi;
-            if (GATE) sy = fmaf(C, hs[i][n], sy);
-            sx = fmaf(q, B, sx);
-            r[n] = q * __builtin_amdgcn_exp2f(di * A2[n]);
+            if (GATE) sy = fmaf(C[n], hs[i][n], sy);
+            sx = fmaf(q, B[n], sx);
+            r[n] = q * (KEEP ? decay[KEEP ? i : 0][n] : __builtin_amdgcn_exp2f(di * A2[n]));
             const float p = r[n] * (i ? hs[i ? i - 1 : 0][n] : h[n]);
             sp = fmaf(A2[n], p, sp);
             dA[n] = fmaf(di, p, dA[n]);
@@ -454,14 +540,11 @@ __global__ __launch_bounds__(64 * LP) void scan_grad_kernel(const ScanArgs a) {
         }
         if (!me.some || t >= s.rows) continue;
         const int64_t row = int64_t(s.first) + t;
-        const float ddt = fmaf(u[j], sx, sp * (1.f / LOG2E)) * slope[j];
-        static_cast<T*>(a.out)[row * a.ld_out + me.channel] = static_cast<T>(fmaf(d[j], sx, skip * dy[j]));
+        const float ddt = fmaf(u[j], sx, sp * (1.f / LOG2E)) * slope[j], d = lds.stage[0][i][lane], dy = lds.stage[2][i][lane];
+        static_cast<T*>(a.out)[row * a.ld_out + me.channel] = static_cast<T>(fmaf(d, sx, skip * dy));
         static_cast<T*>(a.ddt)[row * a.ld_ddt + me.channel] = static_cast<T>(ddt);
-        if constexpr (GATE) {
-          const float g = sigmoid_of<EXACT>(gate[j]);
-          static_cast<T*>(a.dgate)[row * a.ld_dgate + me.channel] = static_cast<T>(dout[j] * fmaf(skip, u[j], sy) * fmaf(gate[j] * g, 1.f - g, g));
-        }
-        dskip = fmaf(dy[j], u[j], dskip);
+        if constexpr (GATE) static_cast<T*>(a.dgate)[row * a.ld_dgate + me.channel] = static_cast<T>(through_gate[j] * fmaf(skip, u[j], sy));
+        dskip = fmaf(dy, u[j], dskip);
         dbias += ddt;
       }
       if (half) __syncthreads();  // (the parts have been read)
@@ -475,15 +558,11 @@ __global__ __launch_bounds__(64 * LP) void scan_grad_kernel(const ScanArgs a) {
   if (!me.some) return;
 #pragma unroll
   for (int n = 0; n < NG; ++n) parts[int64_t(first_n + n) * a.channels] = dA[n];
-  if (wave < 2) {
+  for (int k = wave; k < 2; k += LP) {
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < LP; ++w) sum += lds.part[w][0][wave][lane];
-    parts[int64_t(NP + wave) * a.channels] = sum;
-    if (LP == 1) {
-      sum = lds.part[0][0][1][lane];
-      parts[int64_t(NP + 1) * a.channels] = sum;
-    }
+    for (int w = 0; w < LP; ++w) sum += lds.part[w][0][k][lane];
+    parts[int64_t(NP + k) * a.channels] = sum;
   }
 }
 
@@ -691,10 +770,10 @@ extern "C" int spc_selective_scan_forward(const spc_scan_desc* d, const void* u,
     constexpr bool GATE = decltype(g)::value;
     if (d->n_rows) launch_low<T>(a, log_np, s);
     if (cut) {
-      hipLaunchKernelGGL((scan_kernel<T, NP, false, true, false>), dim3(a.ids * a.blocks), dim3(64), 0, s, a);
+      hipLaunchKernelGGL((scan_kernel<T, NP, false, true, false>), dim3((a.ids * a.blocks + 3) / 4), dim3(SCAN_THREADS), 0, s, a);
       launch_chain(a, np, false, s);
     }
-    hipLaunchKernelGGL((scan_kernel<T, NP, GATE, false, false>), dim3(a.ids * a.blocks), dim3(64), 0, s, a);
+    hipLaunchKernelGGL((scan_kernel<T, NP, GATE, false, false>), dim3((a.ids * a.blocks + 3) / 4), dim3(SCAN_THREADS), 0, s, a);
   });
   pool_free(ws, s);
   SPC_HIP_CHECK(hipGetLastError());
@@ -726,43 +805,44 @@ extern "C" int spc_selective_scan_backward(const spc_scan_desc* d, const void* d
   if (dstate_in && dstate_in == dstate_out) return set_error(SPC_ERR_ARG, "dstate_in is dstate_out");
   const StreamId s(static_cast<hipStream_t>(stream));
   const StreamWorkNote note{s};
-  const int log_np = log_padded(d->states), np = 1 << log_np, waves = np <= 16 ? np / 4 : np / 8;
+  const int log_np = log_padded(d->states), np = 1 << log_np, waves = np / grad_states(np);
   ScanArgs a{};
   scan_shape(a, d);
   a.u = u, a.ld_u = ld_u, a.dt = dt, a.ld_dt = ld_dt, a.gate = gate, a.ld_gate = ld_gate, a.dout = dout, a.ld_dout = ld_dout;
   a.out = du, a.ld_out = ld_du, a.ddt = ddt, a.ld_ddt = ld_ddt, a.dgate = dgate, a.ld_dgate = ld_dgate;
   if (d->n_rows) a.b = low_rows(B), a.c = low_rows(C), a.db = low_rows(dB), a.dc = low_rows(dC);
   a.A = A, a.skip = skip, a.bias = dt_bias, a.state_in = state_in, a.dstate_out = dstate_out, a.dstate_in = dstate_in;
-  a.scenes = {offsets, static_cast<int>(d->n_rows), d->n_scenes, segment_rows(d, a.blocks, 4096, 16, 128 >> std::max(0, log_np - 4))};
+  a.scenes = {offsets, static_cast<int>(d->n_rows), d->n_scenes, segment_rows(d, a.blocks, 4096, grad_rows(np), 4096)};
   a.ids = a.scenes.ids();
   SPC_RETURN_IF(check_grid(a, 64 * waves));
-  const bool cut = d->n_rows > a.scenes.seg_rows, shared = a.blocks > a.groups;
-  const size_t low = ((size_t(d->n_rows) + 1) * a.groups * 2) << log_np, states = cut ? size_t(a.ids) * np * a.channels : 0, steps = cut ? size_t(a.ids) * a.channels : 0;
+  const bool shared = a.blocks > a.groups;
+  const size_t low = ((size_t(d->n_rows) + 1) * a.groups * 2) << log_np, steps = size_t(a.ids) * a.channels, states = steps * np;
+  const size_t starts = size_t(a.ids) * (a.scenes.seg_rows / grad_rows(np)) * (np + 1) * a.channels;
   const size_t parts = size_t(a.ids) * (np + 2) * a.channels, low_parts = shared ? (size_t(a.blocks) * d->n_rows * 2) << log_np : 0;
-  float* ws = static_cast<float*>(pool_alloc(scratch_bytes((low + 2 * states + steps + parts + low_parts) * sizeof(float)), s));
+  float* ws = static_cast<float*>(pool_alloc(scratch_bytes((low + 2 * states + steps + starts + parts + low_parts) * sizeof(float)), s));
   if (!ws) return SPC_ERR_NOMEM;
-  a.low = ws, a.between = ws + low, a.behind = a.between + states, a.steps = a.behind + states, a.parts = a.steps + steps;
-  a.low_parts = shared ? a.parts + parts : nullptr;
+  a.low = ws, a.between = ws + low, a.behind = a.between + states, a.steps = a.behind + states, a.starts = a.steps + steps;
+  a.parts = a.starts + starts, a.low_parts = shared ? a.parts + parts : nullptr;
   int rc = SPC_OK;
   scan_variant(d, gate != nullptr, [&](auto t, auto n, auto g) {
     using T = decltype(t);
-    constexpr int NP = decltype(n)::value, NG = NP <= 16 ? 4 : 8, L = NP <= 16 ? 16 : 8, LP = NP / NG;
+    constexpr int NP = decltype(n)::value;
     constexpr bool GATE = decltype(g)::value;
-    const size_t lds = GradLds<NG, L, LP, GATE>::bytes(a.scenes.seg_rows / L);
-    constexpr auto kernel = scan_grad_kernel<T, NG, L, LP, GATE>;
-    if (lds > 64 * 1024) {
-      static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    constexpr size_t lds = sizeof(GradLds<NP, GATE>);
+    constexpr auto kernel = scan_grad_kernel<T, NP, GATE>;
+    if constexpr (lds > 64 * 1024) {
+      static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
       if (attr != hipSuccess) {
         rc = set_error(SPC_ERR_HIP, "hipFuncSetAttribute failed: %s", hipGetErrorString(attr));
         return;
       }
     }
-    if (d->n_rows) launch_low<T>(a, log_np, s);
-    if (cut) {
-      hipLaunchKernelGGL((scan_kernel<T, NP, GATE, true, true>), dim3(a.ids * a.blocks), dim3(64), 0, s, a);
+    if (d->n_rows) {
+      launch_low<T>(a, log_np, s);
+      hipLaunchKernelGGL((scan_kernel<T, NP, GATE, true, true>), dim3((a.ids * a.blocks + 3) / 4), dim3(SCAN_THREADS), 0, s, a);
       launch_chain(a, np, true, s);
     }
-    hipLaunchKernelGGL(kernel, dim3(a.ids * a.blocks), dim3(64 * LP), lds, s, a);
+    hipLaunchKernelGGL(kernel, dim3(a.ids * a.blocks), dim3(64 * waves), lds, s, a);
     if (shared && d->n_rows) {
       const int64_t m = d->n_rows * a.groups << (log_np + 1);
       hipLaunchKernelGGL(scan_low_grad_kernel<T>, dim3(std::min<int64_t>((m + 255) / 256, 8192)), dim3(256), 0, s, a, log_np);
