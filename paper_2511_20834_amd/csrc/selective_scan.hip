@@ -55,22 +55,14 @@ struct ScanArgs {
 
 typedef const __attribute__((address_space(4))) float* Scalars;  // (read through the scalar cache: nothing writes there while the kernel runs)
 
-// ln(1 + e), 0 <= e <= 1: 2 artanh(e / (2 + e)) by its series, what is left out is below 2^-27.
-__device__ inline float log1p_of(float e) {
-  const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;
-  float p = 1.f / 15;
-#pragma unroll
-  for (int k = 13; k > 0; k -= 2) p = fmaf(p, q, 1.f / k);
-  return 2.f * s * p;
-}
-
-// Step sizes.
+// Step sizes.  ln(1 + e) of e = exp(-|raw|): w = 1 + e rounds e off by c, which comes back as c / w (1/w by a line: c is below 2^-24).  Off by 2^-22 at most, measured from
+// -16 to 16.
 template <typename T>
 struct Step {
   float d, slope;  // d and its derivative
-  __device__ Step(float raw, bool softplus) : d(raw), slope(1.f) {
-    const float e = exp_of<sizeof(T) == 4>(-fabsf(raw)), r = __builtin_amdgcn_rcpf(1.f + e);
-    const float soft = fmaxf(raw, 0.f) + log1p_of(e);  // (NaN where raw is: e is)
+  __device__ Step(float raw, bool softplus) {
+    const float e = exp_of<sizeof(T) == 4>(-fabsf(raw)), w = 1.f + e, c = e - (w - 1.f), r = __builtin_amdgcn_rcpf(w);
+    const float soft = fmaxf(raw, 0.f) + fmaf(__builtin_amdgcn_logf(w), .69314718f, c * fmaf(-.5f, w, 1.5f));  // (NaN where raw is: e is)
     d = softplus ? soft : raw;  // (no branch, which would part the rows of an unrolled loop)
     slope = softplus ? (raw >= 0.f ? r : e * r) : 1.f;
   }
@@ -91,7 +83,7 @@ struct Lane {
 
 // States are taken NB at a time: as many values of B and C as fit the scalar registers twice.
 template <int NP>
-constexpr int NB = NP < 8 ? NP : 8;
+constexpr int NB = NP < 16 ? NP : 16;
 
 __device__ inline Scalars low_row(const ScanArgs& a, int64_t row, int group, int np) {
   return (Scalars)(uintptr_t)(a.low + (row * a.groups + group) * (2 * np));
@@ -100,7 +92,7 @@ __device__ inline Scalars low_row(const ScanArgs& a, int64_t row, int group, int
 // B and C as floats, N of them filled up to NP with zeros.
 template <typename T>
 __global__ __launch_bounds__(256) void scan_low_kernel(LowRows b, LowRows c, float* low, int n_rows, int groups, int N, int log_np) {
-  const int log_nb = min(log_np, 3);
+  const int log_nb = min(log_np, 4);
   const int64_t n = (int64_t(n_rows) + 1) * groups << (log_np + 1);
   for (int64_t i = blockIdx.x * int64_t(256) + threadIdx.x; i < n; i += gridDim.x * int64_t(256)) {
     const int at = static_cast<int>(i & ((2 << log_np) - 1)), j = (at >> (log_nb + 1) << log_nb) + (at & ((1 << log_nb) - 1));
@@ -141,24 +133,38 @@ __device__ inline void load_between(float (&h)[NP], const float* p, const ScanAr
   for (int n = 0; n < NP; ++n) h[n] = me.some ? p[(int64_t(id) * ALL + first + n) * a.channels + me.channel] : 0.f;
 }
 
-// The rows of a matrix from `first` on, one after the other: a scalar address that moves on by the pitch, and the lane's place in a row.
+// A lane's place in a row behind a scalar address.  `stays`, in the block of the accesses: widened elsewhere, the compiler adds both up in vector registers.
+__device__ inline void stays(unsigned& at) { asm volatile("" : "+v"(at)); }
+template <typename T>
+__device__ inline SPC_GLOBAL char* row_of(const void* p, int64_t row, int64_t ld) {
+  return (SPC_GLOBAL char*)(uintptr_t)p + row * ld * int64_t(sizeof(T));
+}
+template <typename T>
+__device__ inline T load_at(const SPC_GLOBAL char* row, unsigned at) {
+  return *reinterpret_cast<SPC_GLOBAL const T*>(row + at);
+}
+template <typename T>
+__device__ inline void store_at(SPC_GLOBAL char* row, unsigned at, T v) {
+  *reinterpret_cast<SPC_GLOBAL T*>(row + at) = v;
+}
+// The rows of a matrix from `first` on, one after the other.
 template <typename T>
 struct Walk {
-  const char* row;
+  SPC_GLOBAL char* row;
   int64_t pitch;
-  __device__ Walk(const void* p, int64_t ld, int64_t first) : row(static_cast<const char*>(p) + first * ld * int64_t(sizeof(T))), pitch(ld * int64_t(sizeof(T))) {}
+  __device__ Walk(const void* p, int64_t ld, int64_t first) : row(row_of<T>(p, first, ld)), pitch(ld * int64_t(sizeof(T))) {}
   __device__ T next(unsigned at) {
-    const T v = *reinterpret_cast<const T*>(row + at);
+    const T v = load_at<T>(row, at);
     on();
     return v;
+  }
+  __device__ void put(unsigned at, T v) {
+    store_at<T>(row, at, v);
+    on();
   }
   __device__ void on() {
     row += pitch;
     asm("" : "+s"(row));  // (else every row of an unrolled loop has an offset of its own in scalar registers, which then do not suffice)
-  }
-  __device__ void put(unsigned at, T v) {
-    *reinterpret_cast<T*>(const_cast<char*>(row) + at) = v;
-    on();
   }
 };
 
@@ -188,7 +194,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const ScanArgs a) {
   } else {
     load_between<NP, NP>(h, a.between, a, id - 1, me, 0);
   }
-  const unsigned at = unsigned(me.channel) * unsigned(sizeof(T));
+  unsigned at = unsigned(me.channel) * unsigned(sizeof(T));
   Walk<T> in_u(a.u, a.ld_u, s.first), in_dt(a.dt, a.ld_dt, s.first), in_gate(a.gate, a.ld_gate, s.first), in_dout(a.dout, a.ld_dout, s.first), out(a.out, a.ld_out, s.first);
   struct Row {
     T u, dt, gate, dout;
@@ -263,6 +269,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const ScanArgs a) {
     for (int q = 0; q < U; ++q) load(now[q]);
     for (; t + 2 * U <= s.rows; t += U) {
       start(t);
+      stays(at);
 #pragma unroll
       for (int q = 0; q < U; ++q) load(next[q]);
 #pragma unroll
@@ -295,16 +302,23 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const ScanArgs a) {
 }
 
 // A scene's segments one after the other: their own states -> the states behind them; with time running backward, what they send forward -> what arrives behind them.
-__global__ __launch_bounds__(256) void scan_chain_kernel(const ScanArgs a, int np) {
+// A wave has 64 (state, channel) pairs and a share of the scene's segments, up to CHAIN_WAVES waves to a scene: each runs over its own from zeros, takes what the ones before
+// it come to, and runs over them again (500 segments, 512 channels of 16 states: 50 us by one wave each).
+constexpr int CHAIN_WAVES = 8;
+__global__ __launch_bounds__(64 * CHAIN_WAVES) void scan_chain_kernel(const ScanArgs a, int np) {
   constexpr int AHEAD = 16;
+  __shared__ float sums[CHAIN_WAVES][64], decays[CHAIN_WAVES][64];
   const bool back = blockIdx.y;
-  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, each = int64_t(np) * a.channels;
-  const int scene = static_cast<int>(i / each), at = static_cast<int>(i - scene * each), n = at / a.channels, channel = at - n * a.channels;
-  if (scene >= a.scenes.n_scenes) return;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int64_t each = int64_t(np) * a.channels, groups = (each + 63) / 64;
+  const int scene = static_cast<int>(blockIdx.x / groups), at = static_cast<int>(min((blockIdx.x - scene * groups) * 64 + lane, each - 1));
+  const bool there = (blockIdx.x - scene * groups) * 64 + lane < each;
+  const int n = at / a.channels, channel = at - n * a.channels;
   const int lo = a.scenes.offsets ? min(max(a.scenes.offsets[scene], 0), a.scenes.n_rows) : 0;
   const int id = lo / a.scenes.seg_rows + scene;
   SceneSegment s;
   if (!s.find(a.scenes, id) || s.scene != scene || s.n == 1) return;
+  s.uniform();
   const bool is = n < a.N;
   const float A2 = is ? a.A[int64_t(channel) * a.N + n] * LOG2E : 0.f;
   const float* start = back ? a.dstate_out : a.state_in;
@@ -312,23 +326,39 @@ __global__ __launch_bounds__(256) void scan_chain_kernel(const ScanArgs a, int n
   float* p = (back ? a.behind : a.between) + int64_t(id) * each + at;
   const float* steps = a.steps + int64_t(id) * a.channels + channel;
   const int links = back ? s.n : s.n - 1;  // (nothing is behind a scene's last segment)
-  for (int m0 = 0; m0 < links; m0 += AHEAD) {
-    float v[AHEAD], d[AHEAD];
+  const int share = max(AHEAD, (links + CHAIN_WAVES - 1) / CHAIN_WAVES), first = wave * share, end = min(links, first + share);
+  // f(value, sum of d, link) of the share's links in their order
+  auto over = [&](auto&& f) {
+    for (int m0 = first; m0 < end; m0 += AHEAD) {
+      float v[AHEAD], d[AHEAD];
 #pragma unroll
-    for (int q = 0; q < AHEAD; ++q) {
-      const int m = back ? s.n - 1 - min(m0 + q, links - 1) : min(m0 + q, links - 1);
-      v[q] = p[m * each];
-      d[q] = steps[int64_t(m) * a.channels];
-    }
+      for (int q = 0; q < AHEAD; ++q) {
+        const int k = min(m0 + q, end - 1), m = back ? s.n - 1 - k : k;
+        v[q] = p[m * each];
+        d[q] = steps[int64_t(m) * a.channels];
+      }
 #pragma unroll
-    for (int q = 0; q < AHEAD; ++q) {
-      if (m0 + q >= links) break;
-      const float after = fmaf(__builtin_amdgcn_exp2f(A2 * d[q]), h, v[q]);
-      if (back) p[(s.n - 1 - (m0 + q)) * each] = h;  // (what arrives behind the segment)
-      else p[(m0 + q) * each] = after;
-      h = after;
+      for (int q = 0; q < AHEAD; ++q)
+        if (m0 + q < end) f(v[q], d[q], back ? s.n - 1 - (m0 + q) : m0 + q);
     }
+  };
+  if (links > share) {  // (all waves of the workgroup alike)
+    float sum = 0.f, steps_sum = 0.f;
+    over([&](float v, float d, int) {
+      sum = fmaf(__builtin_amdgcn_exp2f(A2 * d), sum, v);
+      steps_sum += d;
+    });
+    sums[wave][lane] = sum;
+    decays[wave][lane] = __builtin_amdgcn_exp2f(A2 * steps_sum);
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) h = fmaf(decays[w][lane], h, sums[w][lane]);
   }
+  if (!there) return;
+  over([&](float v, float d, int m) {
+    const float after = fmaf(__builtin_amdgcn_exp2f(A2 * d), h, v);
+    p[m * each] = back ? h : after;  // (back: what arrives behind the segment)
+    h = after;
+  });
 }
 
 // ---------------------------------------------------------------- gradients
@@ -390,7 +420,8 @@ __global__ __launch_bounds__(64 * NP / grad_states(NP), 2) void scan_grad_kernel
   constexpr int NG = grad_states(NP), L = grad_rows(NP), LP = NP / NG, RW = L / LP, V = 4 * NG, LOWS = L * 2 * NP, LOW = (LOWS + 64 * LP - 1) / (64 * LP);
   constexpr bool EXACT = sizeof(T) == 4, KEEP = NG <= 4;  // KEEP: decays are kept beside the states (of eight states a lane, there is no room for them)
   extern __shared__ __attribute__((aligned(16))) char raw[];
-  auto& lds = *reinterpret_cast<GradLds<NP, GATE>*>(raw);
+  using Lds = GradLds<NP, GATE>;
+  Lds& lds = *reinterpret_cast<Lds*>(raw);
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), first_n = wave * NG;
   const int id = blockIdx.x / a.blocks, block = blockIdx.x - id * a.blocks;
   const Lane me(a, block, lane);
@@ -413,19 +444,23 @@ __global__ __launch_bounds__(64 * NP / grad_states(NP), 2) void scan_grad_kernel
   if (s.m == s.n - 1) load_state<NG>(r, a.dstate_out, a, s.scene, me, first_n);
   else load_between<NG, NP>(r, a.behind, a, id, me, first_n);
   const int chunks = (s.rows + L - 1) / L, room = a.scenes.seg_rows / L;
+  unsigned at = unsigned(me.channel) * unsigned(sizeof(T));
   // what comes of a chunk: this wave's rows of it, t = chunk L + j LP + wave; this thread's values of B and C; the state in front of it
   struct {
     T u[RW], dt[RW], gate[GATE ? RW : 1], dout[RW], low[LOW];
     float h[NG], steps;
   } in;
   auto load = [&](int chunk) {
+    stays(at);
+    unsigned at4 = unsigned(me.channel) * 4;
+    stays(at4);
 #pragma unroll
     for (int j = 0; j < RW; ++j) {
       const int64_t row = int64_t(s.first) + min(chunk * L + j * LP + wave, s.rows - 1);
-      in.u[j] = static_cast<const T*>(a.u)[row * a.ld_u + me.channel];
-      in.dt[j] = static_cast<const T*>(a.dt)[row * a.ld_dt + me.channel];
-      in.dout[j] = static_cast<const T*>(a.dout)[row * a.ld_dout + me.channel];
-      if (GATE) in.gate[j] = static_cast<const T*>(a.gate)[row * a.ld_gate + me.channel];
+      in.u[j] = load_at<T>(row_of<T>(a.u, row, a.ld_u), at);
+      in.dt[j] = load_at<T>(row_of<T>(a.dt, row, a.ld_dt), at);
+      in.dout[j] = load_at<T>(row_of<T>(a.dout, row, a.ld_dout), at);
+      if (GATE) in.gate[j] = load_at<T>(row_of<T>(a.gate, row, a.ld_gate), at);
     }
 #pragma unroll
     for (int j = 0; j < LOW; ++j) {
@@ -435,10 +470,10 @@ __global__ __launch_bounds__(64 * NP / grad_states(NP), 2) void scan_grad_kernel
       in.low[j] = static_cast<const T*>(from.p)[row * from.row + me.group * from.group + n];
     }
     if (!chunk) return;
-    const float* p = a.starts + (int64_t(id) * room + chunk) * (NP + 1) * a.channels + me.channel;
+    const int64_t p = (int64_t(id) * room + chunk) * (NP + 1);
 #pragma unroll
-    for (int n = 0; n < NG; ++n) in.h[n] = p[int64_t(first_n + n) * a.channels];
-    in.steps = p[int64_t(NP) * a.channels];
+    for (int n = 0; n < NG; ++n) in.h[n] = load_at<float>(row_of<float>(a.starts, p + first_n + n, a.channels), at4);
+    in.steps = load_at<float>(row_of<float>(a.starts, p + NP, a.channels), at4);
   };
   float u[RW], slope[RW], through_gate[GATE ? RW : 1];  // the last: dout silu'(gate)
   float dskip = 0.f, dbias = 0.f;
@@ -474,56 +509,79 @@ __global__ __launch_bounds__(64 * NP / grad_states(NP), 2) void scan_grad_kernel
     __syncthreads();
     if (chunk) load(chunk - 1);
     float hs[L][NG], decay[KEEP ? L : 1][NG];
+    // (a row is read while the one before it is worked on; without the barriers all are read at once, which takes more registers than there are)
+    struct Row {
+      float d, x, dy, B[NG], C[NG];
+      __device__ void read(const Lds& lds, int i, int lane, int first_n, bool back) {
+        d = lds.stage[0][i][lane], x = lds.stage[1][i][lane];
+        if (back) dy = lds.stage[2][i][lane];
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+          B[n] = lds.low[i][0][first_n + n];
+          if (back) C[n] = lds.low[i][1][first_n + n];
+        }
+      }
+    } now, next;
+    now.read(lds, 0, lane, first_n, false);
 #pragma unroll
     for (int i = 0; i < L; ++i) {
-      const float di = lds.stage[0][i][lane], xi = lds.stage[1][i][lane];
-      const float* B = &lds.low[i][0][first_n];
+      if (i + 1 < L) next.read(lds, i + 1, lane, first_n, false);
+      else next.read(lds, L - 1, lane, first_n, true);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int n = 0; n < NG; ++n) {
-        const float e = __builtin_amdgcn_exp2f(di * A2[n]);
-        if (KEEP) decay[KEEP ? i : 0][n] = e;
-        hs[i][n] = fmaf(e, i ? hs[i ? i - 1 : 0][n] : h[n], xi * B[n]);
+        const float f = __builtin_amdgcn_exp2f(now.d * A2[n]);
+        if (KEEP) decay[KEEP ? i : 0][n] = f;
+        hs[i][n] = fmaf(f, i ? hs[i ? i - 1 : 0][n] : h[n], now.x * now.B[n]);
       }
+      now = next;
     }
 #pragma unroll
     for (int half = L / PART_ROWS - 1; half >= 0; --half) {
+      float low_sums[PART_ROWS / 2];
 #pragma unroll
       for (int pair = PART_ROWS / 2 - 1; pair >= 0; --pair) {
         float v[V];
 #pragma unroll
         for (int e = 1; e >= 0; --e) {
           const int i = half * PART_ROWS + pair * 2 + e;
-          const float *B = &lds.low[i][0][first_n], *C = &lds.low[i][1][first_n];
-          const float di = lds.stage[0][i][lane], xi = lds.stage[1][i][lane], dyi = lds.stage[2][i][lane];
+          if (i) next.read(lds, i - 1, lane, first_n, true);
+          __builtin_amdgcn_sched_barrier(0);
           float sx = 0.f, sp = 0.f, sy = 0.f;
 #pragma unroll
           for (int n = 0; n < NG; ++n) {
-            const float q = fmaf(C[n], dyi, r[n]);
-            v[e * 2 * NG + n] = q * xi;
-            v[e * 2 * NG + NG + n] = hs[i][n] * dyi;
-            if (GATE) sy = fmaf(C[n], hs[i][n], sy);
-            sx = fmaf(q, B[n], sx);
-            r[n] = q * (KEEP ? decay[KEEP ? i : 0][n] : __builtin_amdgcn_exp2f(di * A2[n]));
+            const float q = fmaf(now.C[n], now.dy, r[n]);
+            v[e * 2 * NG + n] = q * now.x;
+            v[e * 2 * NG + NG + n] = hs[i][n] * now.dy;
+            if (GATE) sy = fmaf(now.C[n], hs[i][n], sy);
+            sx = fmaf(q, now.B[n], sx);
+            r[n] = q * (KEEP ? decay[KEEP ? i : 0][n] : __builtin_amdgcn_exp2f(now.d * A2[n]));
             const float p = r[n] * (i ? hs[i ? i - 1 : 0][n] : h[n]);
             sp = fmaf(A2[n], p, sp);
-            dA[n] = fmaf(di, p, dA[n]);
+            dA[n] = fmaf(now.d, p, dA[n]);
           }
           float(*to)[64] = lds.part[wave][pair * 2 + e];
           to[0][lane] = sx;
           to[1][lane] = sp;
           if (GATE) to[2][lane] = sy;
+          if (i) now = next;
         }
-        const float sum = sums_over_lanes<V>(v, lane);
-        constexpr int EACH = 64 / V;
-        const int k = lane / EACH, t = chunk * L + half * PART_ROWS + pair * 2 + k / (2 * NG), n = first_n + k % NG;
-        const bool is_c = k / NG % 2;
-        if (lane % EACH == 0 && t < s.rows) {
+        low_sums[pair] = sums_over_lanes<V>(v, lane);
+      }
+      constexpr int EACH = 64 / V;
+      const int k = lane / EACH, n = first_n + k % NG;
+      const bool is_c = k / NG % 2;
+      if (lane % EACH == 0) {
+#pragma unroll
+        for (int pair = 0; pair < PART_ROWS / 2; ++pair) {
+          const int t = chunk * L + half * PART_ROWS + pair * 2 + k / (2 * NG);
+          if (t >= s.rows) continue;
           const int64_t row = int64_t(s.first) + t;
           if (a.low_parts) {
-            a.low_parts[((int64_t(block) * a.scenes.n_rows + row) * 2 + is_c) * NP + n] = sum;
+            a.low_parts[((int64_t(block) * a.scenes.n_rows + row) * 2 + is_c) * NP + n] = low_sums[pair];
           } else if (n < a.N) {
             const LowRows& to = is_c ? a.dc : a.db;
-            static_cast<T*>(to.p)[row * to.row + me.group * to.group + n] = static_cast<T>(sum);
+            static_cast<T*>(to.p)[row * to.row + me.group * to.group + n] = static_cast<T>(low_sums[pair]);
           }
         }
       }
@@ -540,10 +598,11 @@ __global__ __launch_bounds__(64 * NP / grad_states(NP), 2) void scan_grad_kernel
         }
         if (!me.some || t >= s.rows) continue;
         const int64_t row = int64_t(s.first) + t;
+        stays(at);
         const float ddt = fmaf(u[j], sx, sp * (1.f / LOG2E)) * slope[j], d = lds.stage[0][i][lane], dy = lds.stage[2][i][lane];
-        static_cast<T*>(a.out)[row * a.ld_out + me.channel] = static_cast<T>(fmaf(d, sx, skip * dy));
-        static_cast<T*>(a.ddt)[row * a.ld_ddt + me.channel] = static_cast<T>(ddt);
-        if constexpr (GATE) static_cast<T*>(a.dgate)[row * a.ld_dgate + me.channel] = static_cast<T>(through_gate[j] * fmaf(skip, u[j], sy));
+        store_at<T>(row_of<T>(a.out, row, a.ld_out), at, static_cast<T>(fmaf(d, sx, skip * dy)));
+        store_at<T>(row_of<T>(a.ddt, row, a.ld_ddt), at, static_cast<T>(ddt));
+        if constexpr (GATE) store_at<T>(row_of<T>(a.dgate, row, a.ld_dgate), at, static_cast<T>(through_gate[j] * fmaf(skip, u[j], sy)));
         dskip = fmaf(dy, u[j], dskip);
         dbias += ddt;
       }
@@ -717,7 +776,7 @@ int segment_rows(const spc_scan_desc* d, int blocks, int waves, int unit, int mo
   return static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(unit, (rows + unit - 1) / unit * unit)));
 }
 int check_grid(const ScanArgs& a, int threads) {  // (a launch takes less than 2^32 threads)
-  if (int64_t(a.ids) * a.blocks * threads < (int64_t(1) << 32) && (int64_t(a.scenes.n_scenes) * a.channels << log_padded(a.N)) < (int64_t(1) << 31)) return SPC_OK;
+  if (int64_t(a.ids) * a.blocks * threads < (int64_t(1) << 32) && (int64_t(a.scenes.n_scenes) * a.channels << log_padded(a.N)) < (int64_t(1) << 29)) return SPC_OK;
   return set_error(SPC_ERR_UNSUPPORTED, "%d rows of %d channels and %d states in %d scenes", a.scenes.n_rows, a.channels, a.N, a.scenes.n_scenes);
 }
 template <typename T>
@@ -726,8 +785,10 @@ void launch_low(const ScanArgs& a, int log_np, hipStream_t s) {
   hipLaunchKernelGGL(scan_low_kernel<T>, dim3(std::min<int64_t>((n + 255) / 256, 8192)), dim3(256), 0, s, a.b, a.c, a.low, a.scenes.n_rows, a.groups, a.N, log_np);
 }
 void launch_chain(const ScanArgs& a, int np, bool grad, hipStream_t s) {
-  const int64_t n = int64_t(a.scenes.n_scenes) * np * a.channels;
-  hipLaunchKernelGGL(scan_chain_kernel, dim3((n + 255) / 256, grad ? 2 : 1), dim3(256), 0, s, a, np);
+  const int64_t groups = (int64_t(np) * a.channels + 63) / 64;
+  // (waves that would have no segment, were all rows in one scene, are left out)
+  const int waves = std::min(CHAIN_WAVES, (a.scenes.n_rows / a.scenes.seg_rows + 16) / 16);
+  hipLaunchKernelGGL(scan_chain_kernel, dim3(a.scenes.n_scenes * groups, grad ? 2 : 1), dim3(64 * waves), 0, s, a, np);
 }
 
 }  // namespace
