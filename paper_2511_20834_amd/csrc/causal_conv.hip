@@ -32,15 +32,18 @@ struct ConvArgs {
 };
 
 // A piece of VEC channels: whole, the row's last ones (moved back to end with the row), or less than a piece.
-template <typename T, bool FEW>
+template <typename T, int VEC_, bool FEW>
 struct Channels {
-  static constexpr int VEC = 16 / sizeof(T);
+  static constexpr int VEC = VEC_;
   typedef T Values __attribute__((ext_vector_type(VEC)));
+  typedef int Words __attribute__((ext_vector_type(VEC * int(sizeof(T)) / 4)));
+  typedef int AnyWords __attribute__((ext_vector_type(VEC * int(sizeof(T)) / 4), aligned(2), may_alias));
+  typedef float Four __attribute__((ext_vector_type(4), aligned(4), may_alias));
   int at, c;  // first channel
   bool some;  // whether there is a channel
   int own;    // first of the piece's channels that no other piece has
   __device__ Channels(int piece, int channels) : at(FEW ? piece * VEC : min(piece * VEC, channels - VEC)), c(channels), some(piece * VEC < channels), own(piece * VEC - at) {}
-  __device__ void load(float (&f)[VEC], const void* p, int64_t row, int64_t ld) const {
+  __device__ Values fetch(const void* p, int64_t row, int64_t ld) const {
     const T* from = static_cast<const T*>(p) + row * ld + at;
     Values q{};
     if (FEW) {
@@ -48,11 +51,15 @@ struct Channels {
       for (int k = 0; k < VEC - 1; ++k)
         if (at + k < c) q[k] = from[k];
     } else {
-      q = __builtin_bit_cast(Values, static_cast<Words4>(*reinterpret_cast<const AnyWords4*>(from)));
+      q = __builtin_bit_cast(Values, static_cast<Words>(*reinterpret_cast<const AnyWords*>(from)));
     }
+    return q;
+  }
+  __device__ static void widen(float (&f)[VEC], Values q) {
 #pragma unroll
     for (int k = 0; k < VEC; ++k) f[k] = static_cast<float>(q[k]);
   }
+  __device__ void load(float (&f)[VEC], const void* p, int64_t row, int64_t ld) const { widen(f, fetch(p, row, ld)); }
   __device__ void store(const float (&f)[VEC], void* p, int64_t row, int64_t ld) const {
     T* to = static_cast<T*>(p) + row * ld + at;
     Values q;
@@ -63,14 +70,40 @@ struct Channels {
       for (int k = 0; k < VEC - 1; ++k)
         if (at + k < c) to[k] = q[k];
     } else {
-      *reinterpret_cast<AnyWords4*>(to) = __builtin_bit_cast(Words4, q);
+      *reinterpret_cast<AnyWords*>(to) = __builtin_bit_cast(Words, q);
     }
   }
-  __device__ void params(float (&f)[VEC], const float* p, int stride, int first) const {
+  // N floats of every channel: they lie one behind the other.
+  template <int N>
+  __device__ void params(float (&f)[N][VEC], const float* p) const {
+    float all[VEC * N];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) f[k] = p && (!FEW || at + k < c) ? p[int64_t(at + k) * stride + first] : 0.f;
+    for (int i = 0; i < VEC * N; ++i) all[i] = 0.f;
+    if (p) {
+      const float* from = p + int64_t(at) * N;
+      if (FEW) {
+#pragma unroll
+        for (int i = 0; i < VEC * N; ++i)
+          if (at + i / N < c) all[i] = from[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC * N; i += 4) {
+          const Four v = *reinterpret_cast<const Four*>(from + i);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) all[i + k] = v[k];
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) f[j][k] = all[k * N + j];
   }
 };
+// Channels of a piece: 16 bytes where a row's work is a few operations, four channels in the gradients, which hold some twenty values of each.
+template <typename T>
+constexpr int WIDE = 16 / int(sizeof(T));
+constexpr int NARROW = 4;
 
 // Row `pos` of the scene, which may lie in front of it.
 template <typename P, int W>
@@ -87,7 +120,7 @@ __device__ inline void row_or_past(const P& piece, float (&f)[P::VEC], const Con
 
 template <typename T, int W, bool FEW, bool SILU>
 __global__ __launch_bounds__(CONV_THREADS) void conv_forward_kernel(const ConvArgs a) {
-  using P = Channels<T, FEW>;
+  using P = Channels<T, WIDE<T>, FEW>;
   constexpr int VEC = P::VEC, AHEAD = 4;
   const int tp = 1 << a.log_tp, id = blockIdx.x / a.col_blocks, group = threadIdx.x >> a.log_tp;
   const P piece(blockIdx.x % a.col_blocks * tp + (threadIdx.x & (tp - 1)), a.c);
@@ -101,23 +134,29 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_forward_kernel(const ConvAr
     }
   const int t0 = group * a.per, t1 = min(t0 + a.per, s.rows);
   if (t0 >= t1) return;
-  float w[W][VEC], bias[VEC], x[W + AHEAD - 1][VEC];
+  typename P::Values next[AHEAD];  // (the next rows are on their way while those at hand are worked on)
+  auto fetch = [&](int t) {
 #pragma unroll
-  for (int j = 0; j < W; ++j) piece.params(w[j], a.weight, W, j);
-  piece.params(bias, a.bias, 1, 0);
+    for (int q = 0; q < AHEAD; ++q) next[q] = piece.fetch(a.x, int64_t(s.first) + min(t + q, t1 - 1), a.ld_x);
+  };
+  fetch(t0);
+  float w[W][VEC], bias[1][VEC], x[W + AHEAD - 1][VEC];
+  piece.params(w, a.weight);
+  piece.params(bias, a.bias);
   const int pos = s.first - s.lo + t0;
 #pragma unroll
   for (int j = 0; j < W - 1; ++j) row_or_past<P, W>(piece, x[j], a, s, pos - (W - 1) + j);
   for (int t = t0; t < t1; t += AHEAD) {
 #pragma unroll
-    for (int q = 0; q < AHEAD; ++q) piece.load(x[W - 1 + q], a.x, int64_t(s.first) + min(t + q, t1 - 1), a.ld_x);
+    for (int q = 0; q < AHEAD; ++q) P::widen(x[W - 1 + q], next[q]);
+    if (t + AHEAD < t1) fetch(t + AHEAD);
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) {
       if (t + q >= t1) break;
       float y[VEC];
 #pragma unroll
       for (int k = 0; k < VEC; ++k) {
-        float p = bias[k];
+        float p = bias[0][k];
 #pragma unroll
         for (int j = 0; j < W; ++j) p = fmaf(w[j][k], x[q + j][k], p);
         y[k] = SILU ? p * sigmoid_of<sizeof(T) == 4>(p) : p;
@@ -133,17 +172,16 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_forward_kernel(const ConvAr
 
 template <typename T, int W, bool FEW, bool SILU>
 __global__ __launch_bounds__(CONV_THREADS) void conv_backward_kernel(const ConvArgs a) {
-  using P = Channels<T, FEW>;
+  using P = Channels<T, NARROW, FEW>;
   constexpr int VEC = P::VEC, AHEAD = 4;
   extern __shared__ float sums[];  // [columns of a workgroup][W + 1] by piece
   const int tp = 1 << a.log_tp, group = threadIdx.x >> a.log_tp, lane_piece = threadIdx.x & (tp - 1);
   const int col_block = blockIdx.x % a.col_blocks, part = blockIdx.x / a.col_blocks, parts = gridDim.x / a.col_blocks;
   const P piece(col_block * tp + lane_piece, a.c);
-  float w[W][VEC], bias[VEC], dw[W][VEC] = {}, dbias[VEC] = {};
+  float w[W][VEC], bias[1][VEC], dw[W][VEC] = {}, dbias[VEC] = {};
   if (piece.some) {
-#pragma unroll
-    for (int j = 0; j < W; ++j) piece.params(w[j], a.weight, W, j);
-    piece.params(bias, a.bias, 1, 0);
+    piece.params(w, a.weight);
+    piece.params(bias, a.bias);
   }
   for (int id = part; id < a.ids; id += parts) {
     SceneSegment s;
@@ -162,13 +200,20 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_backward_kernel(const ConvA
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) row_or_past<P, W>(piece, x[j], a, s, t0 - (W - 1) + j);
     const int stop = t1 + W - 1;
-    for (int t = t0; t < stop; t += AHEAD) {
+    typename P::Values next_x[AHEAD], next_d[AHEAD];
+    auto fetch = [&](int t) {
 #pragma unroll
       for (int q = 0; q < AHEAD; ++q) {
-        const int row = min(min(t + q, stop - 1), len - 1);
-        piece.load(x[W - 1 + q], a.x, int64_t(s.lo) + row, a.ld_x);
-        piece.load(d[W - 1 + q], a.dy, int64_t(s.lo) + row, a.ld_dy);
+        const int64_t row = int64_t(s.lo) + min(min(t + q, stop - 1), len - 1);
+        next_x[q] = piece.fetch(a.x, row, a.ld_x);
+        next_d[q] = piece.fetch(a.dy, row, a.ld_dy);
       }
+    };
+    fetch(t0);
+    for (int t = t0; t < stop; t += AHEAD) {
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q) P::widen(x[W - 1 + q], next_x[q]), P::widen(d[W - 1 + q], next_d[q]);
+      if (t + AHEAD < stop) fetch(t + AHEAD);
 #pragma unroll
       for (int q = 0; q < AHEAD; ++q) {
         const int at = t + q;
@@ -178,7 +223,7 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_backward_kernel(const ConvA
         for (int k = 0; k < VEC; ++k) {
           float slope = 1.f;
           if (SILU) {
-            float p = bias[k];
+            float p = bias[0][k];
 #pragma unroll
             for (int j = 0; j < W; ++j) p = fmaf(w[j][k], x[q + j][k], p);
             const float g = sigmoid_of<sizeof(T) == 4>(p);
@@ -210,9 +255,16 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_backward_kernel(const ConvA
     }
   }
   if (!a.partial) return;
-  // the rows' groups one after the other: [channel][W] and [channel] as the parameters lie
-  for (int g = 0; g < CONV_THREADS >> a.log_tp; ++g) {
-    if (g == group && piece.some)
+  // a wave's groups of rows, then the waves one after the other: [channel][W] and [channel] as the parameters lie
+  for (int o = tp; o < 64; o <<= 1)
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) dw[j][k] += __shfl_xor(dw[j][k], o, 64);
+      dbias[k] += __shfl_xor(dbias[k], o, 64);
+    }
+  for (int g = 0; g < CONV_THREADS / 64; ++g) {
+    if (g == int(threadIdx.x) / 64 && threadIdx.x % 64 < tp && piece.some)
 #pragma unroll
       for (int k = 0; k < VEC; ++k) {
         if (k < piece.own || (FEW && piece.at + k >= a.c)) continue;
@@ -236,27 +288,25 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_backward_kernel(const ConvA
 // One row more of many streams: a thread has a piece of one stream's channels, its W - 1 rows move up by one.
 template <typename T, int W, bool FEW, bool SILU>
 __global__ __launch_bounds__(CONV_THREADS) void conv_step_kernel(const ConvArgs a, void* past, int64_t n, int pieces) {
-  using P = Channels<T, FEW>;
+  using P = Channels<T, WIDE<T>, FEW>;
   constexpr int VEC = P::VEC;
   const int64_t i = int64_t(blockIdx.x) * CONV_THREADS + threadIdx.x, row = i / pieces;
   if (row >= n) return;
   const P piece(static_cast<int>(i - row * pieces), a.c);
-  float x[W][VEC], p[VEC];
+  float x[W][VEC], p[1][VEC], w[W][VEC];
 #pragma unroll
   for (int j = 0; j < W - 1; ++j) piece.load(x[j], past, row * (W - 1) + j, a.c);
   piece.load(x[W - 1], a.x, row, a.ld_x);
-  piece.params(p, a.bias, 1, 0);
+  piece.params(p, a.bias);
+  piece.params(w, a.weight);
 #pragma unroll
-  for (int j = 0; j < W; ++j) {
-    float w[VEC];
-    piece.params(w, a.weight, W, j);
+  for (int j = 0; j < W; ++j)
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) p[k] = fmaf(w[k], x[j][k], p[k]);
-  }
+    for (int k = 0; k < VEC; ++k) p[0][k] = fmaf(w[j][k], x[j][k], p[0][k]);
   if (SILU)
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) p[k] *= sigmoid_of<sizeof(T) == 4>(p[k]);
-  piece.store(p, a.y, row, a.ld_y);
+    for (int k = 0; k < VEC; ++k) p[0][k] *= sigmoid_of<sizeof(T) == 4>(p[0][k]);
+  piece.store(p[0], a.y, row, a.ld_y);
 #pragma unroll
   for (int j = 0; j < W - 1; ++j) piece.store(x[j + 1], past, row * (W - 1) + j, a.c);
 }
@@ -278,10 +328,10 @@ int check_matrix(const char* what, const void* p, int64_t ld, int32_t c, int32_t
 
 // Calls f(type, W, FEW, SILU) for the kernels' variants.
 template <typename F>
-void conv_variant(int32_t dtype, int c, int width, bool silu, F&& f) {
+void conv_variant(int32_t dtype, int c, int width, bool silu, bool narrow, F&& f) {
   using std::integral_constant;
   by_dtype(dtype, [&](auto t) {
-    constexpr int VEC = 16 / sizeof(t);
+    const int VEC = narrow ? NARROW : WIDE<decltype(t)>;
     auto with = [&](auto w) {
       auto fit = [&](auto few) {
         if (silu) f(t, w, few, std::true_type{});
@@ -298,8 +348,8 @@ void conv_variant(int32_t dtype, int c, int width, bool silu, F&& f) {
 }
 
 // How a workgroup's threads are dealt to pieces and rows: up to 64 pieces side by side; rows of a thread so that there are some 2048 workgroups, 4 to 16.
-void conv_grid(ConvArgs& a, int es, int64_t n_rows) {
-  const int pieces = (a.c * es + 15) / 16;
+void conv_grid(ConvArgs& a, int vec, int64_t n_rows) {
+  const int pieces = (a.c + vec - 1) / vec;
   a.log_tp = 0;
   while (a.log_tp < 6 && (1 << a.log_tp) < pieces) ++a.log_tp;
   a.col_blocks = (pieces + (1 << a.log_tp) - 1) >> a.log_tp;
@@ -334,9 +384,9 @@ extern "C" int spc_causal_conv_forward(const void* x, int64_t ld_x, const float*
   ConvArgs a{};
   a.scenes = {offsets, static_cast<int>(n), n_scenes, 0};
   a.x = x, a.ld_x = ld_x, a.y = y, a.ld_y = ld_y, a.past = rows_in, a.past_out = rows_out, a.weight = weight, a.bias = bias, a.c = c;
-  conv_grid(a, es, n);
+  conv_grid(a, 16 / es, n);
   SPC_RETURN_IF(check_grid(a));
-  conv_variant(dtype, c, width, silu != 0, [&](auto t, auto w, auto few, auto act) {
+  conv_variant(dtype, c, width, silu != 0, false, [&](auto t, auto w, auto few, auto act) {
     hipLaunchKernelGGL((conv_forward_kernel<decltype(t), decltype(w)::value, decltype(few)::value, decltype(act)::value>), dim3(a.ids * a.col_blocks), dim3(CONV_THREADS), 0,
                        static_cast<hipStream_t>(stream), a);
   });
@@ -365,7 +415,7 @@ extern "C" int spc_causal_conv_backward(const void* dy, int64_t ld_dy, const voi
   a.scenes = {offsets, static_cast<int>(n), n_scenes, 0};
   a.x = x, a.ld_x = ld_x, a.dy = dy, a.ld_dy = ld_dy, a.y = dx, a.ld_y = ld_dx, a.past = rows_in, a.dpast = drows_out, a.past_out = drows_in;
   a.weight = weight, a.bias = bias, a.c = c;
-  conv_grid(a, es, n);
+  conv_grid(a, NARROW, n);
   SPC_RETURN_IF(check_grid(a));
   const bool params = dweight || dbias;
   const int parts = std::min(a.ids, std::max(1, 1024 / a.col_blocks));  // (what 256 CUs hold at once; each stores sums)
@@ -373,8 +423,8 @@ extern "C" int spc_causal_conv_backward(const void* dy, int64_t ld_dy, const voi
     a.partial = static_cast<float*>(pool_alloc(scratch_bytes(size_t(parts) * c * (width + 1) * sizeof(float)), s));
     if (!a.partial) return SPC_ERR_NOMEM;
   }
-  conv_variant(dtype, c, width, silu != 0, [&](auto t, auto w, auto few, auto act) {
-    const size_t lds = (size_t(16 / sizeof(t)) << a.log_tp) * (width + 1) * sizeof(float);
+  conv_variant(dtype, c, width, silu != 0, true, [&](auto t, auto w, auto few, auto act) {
+    const size_t lds = (size_t(NARROW) << a.log_tp) * (width + 1) * sizeof(float);
     hipLaunchKernelGGL((conv_backward_kernel<decltype(t), decltype(w)::value, decltype(few)::value, decltype(act)::value>), dim3(parts * a.col_blocks), dim3(CONV_THREADS),
                        lds, s, a);
   });
@@ -397,7 +447,7 @@ extern "C" int spc_causal_conv_step(const void* x, int64_t ld_x, const float* we
   if (n > (int64_t(1) << 31) / pieces) return set_error(SPC_ERR_UNSUPPORTED, "%lld streams of %d channels", static_cast<long long>(n), c);
   ConvArgs a{};
   a.x = x, a.ld_x = ld_x, a.y = y, a.ld_y = ld_y, a.weight = weight, a.bias = bias, a.c = c;
-  conv_variant(dtype, c, width, silu != 0, [&](auto t, auto w, auto few, auto act) {
+  conv_variant(dtype, c, width, silu != 0, false, [&](auto t, auto w, auto few, auto act) {
     hipLaunchKernelGGL((conv_step_kernel<decltype(t), decltype(w)::value, decltype(few)::value, decltype(act)::value>), dim3((n * pieces + CONV_THREADS - 1) / CONV_THREADS),
                        dim3(CONV_THREADS), 0, static_cast<hipStream_t>(stream), a, rows, n, pieces);
   });

@@ -6,7 +6,7 @@
 // rounding to the output's type.  (The matrix cores' products of 8-bit operands line up their terms in fewer bits: 2^-13.5 of the sum of magnitudes off at 128 places
 // of values from all binades, 2^-22.8 so.  They would be twice as fast, which bytes leave no use for: 120 k x 256 -> 1024 moves 277 MB for 63 GFLOP.)
 // A workgroup holds 128 rows in its waves' registers where their channels fit, so x is read once, and walks over the columns in tiles of 64, whose weights
-// all four waves read from LDS.  The weights are the product's left operand and a tile's lines are dealt to its four 16 x 16 products so that a lane ends up with 16
+// all four waves read from LDS, as bytes; the next tile is on its way meanwhile.  The weights are the product's left operand and a tile's lines are dealt to its four 16 x 16 products so that a lane ends up with 16
 // consecutive columns of one output row: whole lines are stored, 128 bytes a row and wave in 16 bits.
 #include <algorithm>
 #include <type_traits>
@@ -16,7 +16,7 @@
 namespace spc {
 namespace {
 
-constexpr int LIN_COLS = 64, LIN_K = 64;  // a tile of weights: columns, places of each
+constexpr int LIN_COLS = 64, LIN_K = 256, LIN_STEP = 64;  // a tile of weights: columns, bytes of each; places of two products
 constexpr int LIN_THREADS = 256, LIN_GROUPS = 2;  // groups of 16 rows a wave
 constexpr int LIN_MAX_C = 65536;
 
@@ -55,76 +55,84 @@ __device__ inline void to_halves(Words4 v, half8 (&f)[2]) {
   }
 }
 
-// KT: tiles of 64 places that a wave's rows are held in (0: they are read again for every tile of columns).  Lane l has row (column) l % 16 of every operand and 16 places of a
-// tile's 64 from 16 (l / 16) on, in two products of 32; of a result column l % 16 and rows 4 (l / 16) + r.
-template <typename T, int KT, bool WHOLE>
+// KS: steps of 64 places that a wave's rows are held for (0: they are read again for every tile of columns).  Lane l has row (column) l % 16 of every operand and 16 places of a
+// step's 64 from 16 (l / 16) on, in two products of 32; of a result column l % 16 and rows 4 (l / 16) + r.
+template <typename T, int KS, bool WHOLE>
 __global__ __launch_bounds__(LIN_THREADS) void linear8_kernel(const LinearArgs a) {
-  constexpr int RT = LIN_GROUPS;
-  __shared__ half8 tile[2][LIN_COLS * LIN_K / 8];
+  constexpr int RT = LIN_GROUPS, STEPS = KS ? KS : LIN_K / LIN_STEP, WIDTH = STEPS * LIN_STEP / 16;  // steps and pieces of 16 bytes of a tile's line
+  constexpr int MINE = LIN_COLS * WIDTH / LIN_THREADS;                                               // of which each thread fetches so many
+  __shared__ Words4 tile[2][LIN_COLS * WIDTH];
   const int t = threadIdx.x, lane = t % 64, wave = t / 64, i = lane % 16, g = lane / 16;
-  const int all = (a.cout + LIN_COLS - 1) / LIN_COLS, splits = (all + a.tiles - 1) / a.tiles, n_kt = (a.c + LIN_K - 1) / LIN_K;
+  const int all = (a.cout + LIN_COLS - 1) / LIN_COLS, splits = (all + a.tiles - 1) / a.tiles, parts = KS ? 1 : (a.c + LIN_K - 1) / LIN_K;
   const int64_t block = blockIdx.x / splits;
   const int first_tile = blockIdx.x % splits * a.tiles, last_tile = min(first_tile + a.tiles, all);
   const int64_t row0 = (block * 4 + wave) * (16 * RT) + i;  // of group 0; the lane's row of group q is 16 q further
-  // this thread's part of a tile of weights, 16 places of a line; line 16 q + m of the tile in LDS is column 16 (m / 4) + 4 q + m % 4, its pieces of 8 are turned by its number
-  const int line = t / 4, line_col = line % 16 / 4 * 16 + line / 16 * 4 + line % 4;
-  auto stage = [&](int ct, int kt) {
-    const int col = ct * LIN_COLS + line_col;
-    return col < a.cout ? piece16<WHOLE>(a.w + int64_t(col) * a.ld_w, kt * LIN_K + t % 4 * 16, a.c) : Words4{0, 0, 0, 0};
-  };
-  auto rows = [&](int kt, half8 (&f)[RT][2]) {
+  // line 16 q + m of a tile is column 16 (m / 4) + 4 q + m % 4; its pieces are turned by its number, so that 16 lines' same pieces lie in different banks
+  Words4 next[MINE];
+  auto fetch = [&](int ct, int part) {
 #pragma unroll
-    for (int q = 0; q < RT; ++q) {
-      Words4 v = {0, 0, 0, 0};
-      if (row0 + 16 * q < a.n) v = piece16<WHOLE>(a.x + (row0 + 16 * q) * a.ld_x, kt * LIN_K + 16 * g, a.c);
-      to_halves(v, f[q]);
+    for (int p = 0; p < MINE; ++p) {
+      const int line = (p * LIN_THREADS + t) / WIDTH, k = part * LIN_K + (p * LIN_THREADS + t) % WIDTH * 16;
+      const int col = ct * LIN_COLS + line % 16 / 4 * 16 + line / 16 * 4 + line % 4;
+      next[p] = Words4{0, 0, 0, 0};
+      if (col < a.cout) next[p] = piece16<WHOLE>(a.w + int64_t(col) * a.ld_w, k, a.c);
     }
   };
-  half8 held[KT ? KT : 1][RT][2];
-  if constexpr (KT > 0)
+  auto rows = [&](int k, Words4 (&v)[RT]) {
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) rows(kt, held[kt]);
+    for (int q = 0; q < RT; ++q) {
+      v[q] = Words4{0, 0, 0, 0};
+      if (row0 + 16 * q < a.n) v[q] = piece16<WHOLE>(a.x + (row0 + 16 * q) * a.ld_x, k + 16 * g, a.c);
+    }
+  };
+  Words4 held[KS ? KS : 1][RT];  // (as bytes: in halves they would leave room for two workgroups a CU, not three)
+  fetch(first_tile, 0);
+  if constexpr (KS > 0)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) rows(s * LIN_STEP, held[s]);
   float sx[RT];
 #pragma unroll
   for (int q = 0; q < RT; ++q) sx[q] = row0 + 16 * q < a.n ? a.sx[row0 + 16 * q] : 0.f;
-  Words4 next = stage(first_tile, 0);
   int buf = 0;
   for (int ct = first_tile; ct < last_tile; ++ct) {
+    if constexpr (KS > 0)
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int q = 0; q < RT; ++q) asm volatile("" : "+v"(held[s][q]));  // (else they are made halves once for all tiles)
     floatx4 acc[RT][4];
 #pragma unroll
     for (int q = 0; q < RT; ++q)
 #pragma unroll
       for (int m = 0; m < 4; ++m) acc[q][m] = floatx4{0.f, 0.f, 0.f, 0.f};
-    auto step = [&](int kt, const half8 (&f)[RT][2]) {
-      half8 w[2];
-      to_halves(next, w);
+    for (int part = 0; part < parts; ++part) {
 #pragma unroll
-      for (int p = 0; p < 2; ++p) tile[buf][line * 8 + ((t % 4 * 2 + p) ^ line % 8)] = w[p];
+      for (int p = 0; p < MINE; ++p) {
+        const int line = (p * LIN_THREADS + t) / WIDTH, at = (p * LIN_THREADS + t) % WIDTH;
+        tile[buf][line * WIDTH + (at ^ line % WIDTH)] = next[p];
+      }
       // (one barrier a tile: whoever stores to a buffer again has passed the barrier behind its last reads, since there are two)
       __syncthreads();
-      if (kt + 1 < n_kt) next = stage(ct, kt + 1);
-      else if (ct + 1 < last_tile) next = stage(ct + 1, 0);
+      if (part + 1 < parts) fetch(ct, part + 1);
+      else if (ct + 1 < last_tile) fetch(ct + 1, 0);
 #pragma unroll
-      for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const int from = 16 * m + i;
-          const half8 v = tile[buf][from * 8 + ((2 * g + p) ^ from % 8)];
-#pragma unroll
-          for (int q = 0; q < RT; ++q) acc[q][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, f[q][p], acc[q][m], 0, 0, 0);
-        }
-      buf ^= 1;
-    };
-    if constexpr (KT > 0) {
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-        if (kt < n_kt) step(kt, held[kt]);
-    } else {
-      for (int kt = 0; kt < n_kt; ++kt) {
+      for (int s = 0; s < STEPS; ++s) {
+        Words4 x[RT];
         half8 f[RT][2];
-        rows(kt, f);
-        step(kt, f);
+        if constexpr (KS == 0) rows(part * LIN_K + s * LIN_STEP, x);
+#pragma unroll
+        for (int q = 0; q < RT; ++q) to_halves(KS ? held[KS ? s : 0][q] : x[q], f[q]);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          half8 w[2];
+          to_halves(tile[buf][(16 * m + i) * WIDTH + ((4 * s + g) ^ (16 * m + i) % WIDTH)], w);
+#pragma unroll
+          for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int q = 0; q < RT; ++q) acc[q][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[p], f[q][p], acc[q][m], 0, 0, 0);
+        }
       }
+      buf ^= 1;
     }
     const int col = ct * LIN_COLS + 16 * g, left = a.cout - col;
     float sw[16];
