@@ -6,8 +6,9 @@
 // rounding to the output's type.  (The matrix cores' products of 8-bit operands line up their terms in fewer bits: 2^-13.5 of the sum of magnitudes off at 128 places
 // of values from all binades, 2^-22.8 so.  They would be twice as fast, which bytes leave no use for: 120 k x 256 -> 1024 moves 277 MB for 63 GFLOP.)
 // A workgroup holds 128 rows in its waves' registers where their channels fit, so x is read once, and walks over the columns in tiles of 64, whose weights
-// all four waves read from LDS, as bytes; the next tile is on its way meanwhile.  The weights are the product's left operand and a tile's lines are dealt to its four 16 x 16 products so that a lane ends up with 16
-// consecutive columns of one output row: whole lines are stored, 128 bytes a row and wave in 16 bits.
+// all four waves read from LDS, where they are halves already; the next tile's bytes are on their way meanwhile.  The weights are the product's left operand and a tile's lines
+// are dealt to its four 16 x 16 products so that a lane ends up with pieces of 16 bytes of one output row, next to its neighbours': every store of a wave fills 64
+// consecutive bytes of 16 rows.
 #include <algorithm>
 #include <type_traits>
 
@@ -16,8 +17,8 @@
 namespace spc {
 namespace {
 
-constexpr int LIN_COLS = 64, LIN_K = 256, LIN_STEP = 64;  // a tile of weights: columns, bytes of each; places of two products
-constexpr int LIN_THREADS = 256, LIN_GROUPS = 2;  // groups of 16 rows a wave
+constexpr int LIN_COLS = 32, LIN_K = 256, LIN_STEP = 64;  // a tile of weights: columns, bytes of each; places of two products
+constexpr int LIN_THREADS = 256, LIN_GROUPS = 4;  // groups of 16 rows a wave
 constexpr int LIN_MAX_C = 65536;
 
 typedef _Float16 half2 __attribute__((ext_vector_type(2)));
@@ -60,22 +61,44 @@ __device__ inline void to_halves(Words4 v, half8 (&f)[2]) {
 template <typename T, int KS, bool WHOLE>
 __global__ __launch_bounds__(LIN_THREADS) void linear8_kernel(const LinearArgs a) {
   constexpr int RT = LIN_GROUPS, STEPS = KS ? KS : LIN_K / LIN_STEP, WIDTH = STEPS * LIN_STEP / 16;  // steps and pieces of 16 bytes of a tile's line
-  constexpr int MINE = LIN_COLS * WIDTH / LIN_THREADS;                                               // of which each thread fetches so many
-  __shared__ Words4 tile[2][LIN_COLS * WIDTH];
+  constexpr int PIECES = LIN_COLS * WIDTH, MINE = (PIECES + LIN_THREADS - 1) / LIN_THREADS, MT = LIN_COLS / 16, TURNS = WIDTH >= 8 ? 16 : 8;  // of which each thread fetches so many
+  __shared__ half8 tiles[2][LIN_COLS * WIDTH * 2];
   const int t = threadIdx.x, lane = t % 64, wave = t / 64, i = lane % 16, g = lane / 16;
   const int all = (a.cout + LIN_COLS - 1) / LIN_COLS, splits = (all + a.tiles - 1) / a.tiles, parts = KS ? 1 : (a.c + LIN_K - 1) / LIN_K;
   const int64_t block = blockIdx.x / splits;
-  const int first_tile = blockIdx.x % splits * a.tiles, last_tile = min(first_tile + a.tiles, all);
+  const int first_tile = blockIdx.x % splits * a.tiles, count = min(a.tiles, all - first_tile);
+  // (a workgroup starts with a tile of its own: were all at the same columns at once, rows of a power of two would keep few memory channels busy)
+  const int turn = static_cast<int>(block % count);
+  auto tile_at = [&](int n) { return first_tile + (n + turn < count ? n + turn : n + turn - count); };
   const int64_t row0 = (block * 4 + wave) * (16 * RT) + i;  // of group 0; the lane's row of group q is 16 q further
-  // line 16 q + m of a tile is column 16 (m / 4) + 4 q + m % 4; its pieces are turned by its number, so that 16 lines' same pieces lie in different banks
+  // Line 16 m + 4 g + r of a tile is the column that a lane stores of result r of product m: piece 4 m / VEC of its row, lane by lane.  A line's pieces of 8 halves
+  // are turned by its number, so that 16 lines' reads of one place lie in different banks.
+  constexpr int VEC = 16 / sizeof(T);
+  auto column = [](int line) { return line / 16 * 4 / VEC * (4 * VEC) + line % 16 / 4 * VEC + line / 16 * 4 % VEC + line % 4; };
+  constexpr int STORES = LIN_COLS / (4 * VEC);
+  typedef float Some __attribute__((ext_vector_type(VEC), aligned(4), may_alias));
+  typedef T Values __attribute__((ext_vector_type(VEC)));
   Words4 next[MINE];
+  Some next_scale[STORES];  // (of the columns that this lane stores)
   auto fetch = [&](int ct, int part) {
 #pragma unroll
     for (int p = 0; p < MINE; ++p) {
-      const int line = (p * LIN_THREADS + t) / WIDTH, k = part * LIN_K + (p * LIN_THREADS + t) % WIDTH * 16;
-      const int col = ct * LIN_COLS + line % 16 / 4 * 16 + line / 16 * 4 + line % 4;
+      const int line = (p * LIN_THREADS + t) / WIDTH % LIN_COLS, k = part * LIN_K + (p * LIN_THREADS + t) % WIDTH * 16;
+      const int col = ct * LIN_COLS + column(line);
       next[p] = Words4{0, 0, 0, 0};
       if (col < a.cout) next[p] = piece16<WHOLE>(a.w + int64_t(col) * a.ld_w, k, a.c);
+    }
+  };
+  auto fetch_scale = [&](int ct) {
+#pragma unroll
+    for (int p = 0; p < STORES; ++p) {
+      const int col = ct * LIN_COLS + p * (4 * VEC) + g * VEC;
+      if ((ct + 1) * LIN_COLS <= a.cout) {
+        next_scale[p] = *reinterpret_cast<const Some*>(a.sw + col);
+      } else {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) next_scale[p][k] = col + k < a.cout ? a.sw[col + k] : 0.f;
+      }
     }
   };
   auto rows = [&](int k, Words4 (&v)[RT]) {
@@ -86,7 +109,8 @@ __global__ __launch_bounds__(LIN_THREADS) void linear8_kernel(const LinearArgs a
     }
   };
   Words4 held[KS ? KS : 1][RT];  // (as bytes: in halves they would leave room for two workgroups a CU, not three)
-  fetch(first_tile, 0);
+  fetch(tile_at(0), 0);
+  fetch_scale(tile_at(0));
   if constexpr (KS > 0)
 #pragma unroll
     for (int s = 0; s < KS; ++s) rows(s * LIN_STEP, held[s]);
@@ -94,27 +118,36 @@ __global__ __launch_bounds__(LIN_THREADS) void linear8_kernel(const LinearArgs a
 #pragma unroll
   for (int q = 0; q < RT; ++q) sx[q] = row0 + 16 * q < a.n ? a.sx[row0 + 16 * q] : 0.f;
   int buf = 0;
-  for (int ct = first_tile; ct < last_tile; ++ct) {
+  for (int n = 0; n < count; ++n) {
+    const int ct = tile_at(n);
+    Some scale[STORES];
+#pragma unroll
+    for (int p = 0; p < STORES; ++p) scale[p] = next_scale[p];
     if constexpr (KS > 0)
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int q = 0; q < RT; ++q) asm volatile("" : "+v"(held[s][q]));  // (else they are made halves once for all tiles)
-    floatx4 acc[RT][4];
+    floatx4 acc[RT][MT];
 #pragma unroll
     for (int q = 0; q < RT; ++q)
 #pragma unroll
-      for (int m = 0; m < 4; ++m) acc[q][m] = floatx4{0.f, 0.f, 0.f, 0.f};
-    for (int part = 0; part < parts; ++part) {
+      for (int m = 0; m < MT; ++m) acc[q][m] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int part = 0; part < parts; ++part, buf ^= 1) {
+      half8* tile = tiles[buf];
 #pragma unroll
       for (int p = 0; p < MINE; ++p) {
         const int line = (p * LIN_THREADS + t) / WIDTH, at = (p * LIN_THREADS + t) % WIDTH;
-        tile[buf][line * WIDTH + (at ^ line % WIDTH)] = next[p];
+        if (PIECES % LIN_THREADS && p * LIN_THREADS + t >= PIECES) continue;
+        half8 w[2];
+        to_halves(next[p], w);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) tile[line * (2 * WIDTH) + ((2 * at + h) ^ line % TURNS)] = w[h];
       }
       // (one barrier a tile: whoever stores to a buffer again has passed the barrier behind its last reads, since there are two)
       __syncthreads();
       if (part + 1 < parts) fetch(ct, part + 1);
-      else if (ct + 1 < last_tile) fetch(ct + 1, 0);
+      else if (n + 1 < count) fetch(tile_at(n + 1), 0), fetch_scale(tile_at(n + 1));
 #pragma unroll
       for (int s = 0; s < STEPS; ++s) {
         Words4 x[RT];
@@ -123,38 +156,33 @@ __global__ __launch_bounds__(LIN_THREADS) void linear8_kernel(const LinearArgs a
 #pragma unroll
         for (int q = 0; q < RT; ++q) to_halves(KS ? held[KS ? s : 0][q] : x[q], f[q]);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          half8 w[2];
-          to_halves(tile[buf][(16 * m + i) * WIDTH + ((4 * s + g) ^ (16 * m + i) % WIDTH)], w);
+        for (int m = 0; m < MT; ++m) {
 #pragma unroll
-          for (int p = 0; p < 2; ++p)
+          for (int p = 0; p < 2; ++p) {
+            const half8 w = tile[(16 * m + i) * (2 * WIDTH) + ((2 * (4 * s + g) + p) ^ i % TURNS)];
 #pragma unroll
-            for (int q = 0; q < RT; ++q) acc[q][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[p], f[q][p], acc[q][m], 0, 0, 0);
+            for (int q = 0; q < RT; ++q) acc[q][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w, f[q][p], acc[q][m], 0, 0, 0);
+          }
         }
       }
-      buf ^= 1;
     }
-    const int col = ct * LIN_COLS + 16 * g, left = a.cout - col;
-    float sw[16];
+    const bool full = (ct + 1) * LIN_COLS <= a.cout;
 #pragma unroll
-    for (int m = 0; m < 16; ++m) sw[m] = m < left ? a.sw[col + m] : 0.f;
+    for (int p = 0; p < STORES; ++p) {
+      const int col = ct * LIN_COLS + p * (4 * VEC) + g * VEC, left = a.cout - col;
 #pragma unroll
-    for (int q = 0; q < RT; ++q) {
-      if (row0 + 16 * q >= a.n) continue;
-      T* to = static_cast<T*>(a.out) + (row0 + 16 * q) * a.ld_out + col;
-      constexpr int VEC = 16 / sizeof(T);
-      typedef T Values __attribute__((ext_vector_type(VEC)));
-#pragma unroll
-      for (int p = 0; p < 16 / VEC; ++p) {
+      for (int q = 0; q < RT; ++q) {
+        if (row0 + 16 * q >= a.n) continue;
+        T* to = static_cast<T*>(a.out) + (row0 + 16 * q) * a.ld_out + col;
         Values v;
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) v[k] = static_cast<T>(acc[q][(p * VEC + k) / 4][k % 4] * sx[q] * sw[p * VEC + k]);
-        if ((p + 1) * VEC <= left) {
-          *reinterpret_cast<AnyWords4*>(to + p * VEC) = __builtin_bit_cast(Words4, v);
+        for (int k = 0; k < VEC; ++k) v[k] = static_cast<T>(acc[q][(p * VEC + k) / 4][k % 4] * sx[q] * scale[p][k]);
+        if (full || VEC <= left) {
+          *reinterpret_cast<AnyWords4*>(to) = __builtin_bit_cast(Words4, v);
         } else {
 #pragma unroll
           for (int k = 0; k < VEC; ++k)
-            if (p * VEC + k < left) to[p * VEC + k] = v[k];
+            if (k < left) to[k] = v[k];
         }
       }
     }
@@ -182,7 +210,7 @@ extern "C" int spc_linear_f8(const void* x, int64_t ld_x, const float* x_scale, 
   constexpr int ROWS = 64 * LIN_GROUPS;
   const int64_t blocks = (n + ROWS - 1) / ROWS;
   // columns are split between workgroups until there are some 1024 of them
-  const int splits = static_cast<int>(std::min<int64_t>(all, std::max<int64_t>(1, 1024 / blocks)));
+  const int splits = static_cast<int>(std::min<int64_t>(all, std::max<int64_t>(1, 512 / blocks)));
   a.tiles = (all + splits - 1) / splits;
   by_dtype(dtype, [&](auto type) {
     auto go = [&](auto kt, auto whole) {
