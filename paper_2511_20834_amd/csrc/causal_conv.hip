@@ -73,6 +73,14 @@ struct Channels {
       *reinterpret_cast<AnyWords*>(to) = __builtin_bit_cast(Words, q);
     }
   }
+  // Its own channels only: where another piece's thread reads what this one would store, too.
+  __device__ void store_own(const float (&f)[VEC], void* p, int64_t row, int64_t ld) const {
+    if (own == 0) return store(f, p, row, ld);
+    T* to = static_cast<T*>(p) + row * ld + at;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k)
+      if (k >= own) to[k] = static_cast<T>(f[k]);
+  }
   // N floats of every channel: they lie one behind the other.
   template <int N>
   __device__ void params(float (&f)[N][VEC], const float* p) const {
@@ -306,9 +314,10 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_step_kernel(const ConvArgs 
   if (SILU)
 #pragma unroll
     for (int k = 0; k < VEC; ++k) p[0][k] *= sigmoid_of<sizeof(T) == 4>(p[0][k]);
-  piece.store(p[0], a.y, row, a.ld_y);
+  // (the row's last piece shares channels with the one before it, whose thread may be another wave's and have moved them up already: it leaves them to that)
+  piece.store_own(p[0], a.y, row, a.ld_y);
 #pragma unroll
-  for (int j = 0; j < W - 1; ++j) piece.store(x[j + 1], past, row * (W - 1) + j, a.c);
+  for (int j = 0; j < W - 1; ++j) piece.store_own(x[j + 1], past, row * (W - 1) + j, a.c);
 }
 
 // ---------------------------------------------------------------- host

@@ -46,7 +46,9 @@ struct ScanArgs {
   float* between;  // [segment][NP][channels]: its state from zeros, then the state behind it
   float* behind;   // the same for the gradient: what reaches the rows in front of a segment, from zeros, then what arrives from behind it
   float* steps;    // [segment][channels]: sum of d
-  float* starts;   // [segment][chunk][NP][channels]: its state from zeros in front of every grad_rows rows but the first, and their sums of d as state NP
+  // [slot][NP + 1][channels]: a segment's state from zeros in front of every grad_rows rows but its first, and the sum of d up to there.  Its slots begin at
+  // first row / grad_rows + its number (as segments are numbered in their scenes, so do slots of segments stay apart).
+  float* starts;
   float* parts;    // [segment][NP + 2][channels]: dA, dD, dbias
   float* low_parts;  // [block of channels][row][B, C][NP], where several blocks share a group
   int channels, groups, share, N, blocks, ids;  // share: channels of a group; blocks: of 64 channels, of all groups
@@ -257,7 +259,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const ScanArgs a) {
   auto start = [&](int t) {  // in front of row t
     constexpr int L = grad_rows(NP);
     if (!(SUMS && GRAD) || t % L || !t) return;
-    float* to = a.starts + (int64_t(id) * (a.scenes.seg_rows / L) + t / L) * (NP + 1) * a.channels + me.channel;
+    float* to = a.starts + (int64_t(s.first) / L + id + t / L) * (NP + 1) * a.channels + me.channel;
 #pragma unroll
     for (int n = 0; n < NP; ++n) to[int64_t(n) * a.channels] = h[n];
     to[int64_t(NP) * a.channels] = steps;
@@ -443,7 +445,7 @@ __global__ __launch_bounds__(64 * NP / grad_states(NP), 2) void scan_grad_kernel
   else load_between<NG, NP>(first_h, a.between, a, id - 1, me, first_n);
   if (s.m == s.n - 1) load_state<NG>(r, a.dstate_out, a, s.scene, me, first_n);
   else load_between<NG, NP>(r, a.behind, a, id, me, first_n);
-  const int chunks = (s.rows + L - 1) / L, room = a.scenes.seg_rows / L;
+  const int chunks = (s.rows + L - 1) / L;
   unsigned at = unsigned(me.channel) * unsigned(sizeof(T));
   // what comes of a chunk: this wave's rows of it, t = chunk L + j LP + wave; this thread's values of B and C; the state in front of it
   struct {
@@ -470,7 +472,7 @@ __global__ __launch_bounds__(64 * NP / grad_states(NP), 2) void scan_grad_kernel
       in.low[j] = static_cast<const T*>(from.p)[row * from.row + me.group * from.group + n];
     }
     if (!chunk) return;
-    const int64_t p = (int64_t(id) * room + chunk) * (NP + 1);
+    const int64_t p = (int64_t(s.first) / L + id + chunk) * (NP + 1);
 #pragma unroll
     for (int n = 0; n < NG; ++n) in.h[n] = load_at<float>(row_of<float>(a.starts, p + first_n + n, a.channels), at4);
     in.steps = load_at<float>(row_of<float>(a.starts, p + NP, a.channels), at4);
@@ -672,18 +674,21 @@ __global__ __launch_bounds__(256) void scan_low_grad_kernel(const ScanArgs a, in
 // A lane has VEC states of a channel, 2^log_q neighbouring lanes have a channel's; states are read and written once, which bounds it.  The decay is taken as
 // 1 + (e^w - 1) where it is near 1: rounded to 24 bits every row, a stream's long memory would drift.
 template <typename T, int VEC, bool GATE>
-__global__ __launch_bounds__(256) void scan_step_kernel(const ScanArgs a, float* state, int64_t n, int log_q) {
+__global__ __launch_bounds__(256) void scan_step_kernel(const ScanArgs a, float* state, unsigned n, int log_q) {
   typedef float Values __attribute__((ext_vector_type(VEC), aligned(4), may_alias));
-  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) >> log_q, row = i / a.channels;
-  const int channel = static_cast<int>(i - row * a.channels), first = (threadIdx.x & ((1 << log_q) - 1)) * VEC;
-  const bool is = row < n && first < a.N;
+  // (fewer than 2^31 lanes have states)
+  const unsigned i = (blockIdx.x * 256u + threadIdx.x) >> log_q, first = (threadIdx.x & ((1u << log_q) - 1)) * VEC, channels = a.channels;
+  const bool is = i < n * channels && first < unsigned(a.N);
+  Values* S = reinterpret_cast<Values*>(state + int64_t(i) * a.N + first);
+  Values h;
+  if (is) h = *S;
+  const int64_t row = i / channels;
+  const int channel = static_cast<int>(i - unsigned(row) * channels);
   float y = 0.f, u = 0.f;
-  if (row < n) u = static_cast<float>(static_cast<const T*>(a.u)[row * a.ld_u + channel]);
   if (is) {
-    Values* S = reinterpret_cast<Values*>(state + i * a.N + first);
-    Values h = *S;
+    u = static_cast<float>(static_cast<const T*>(a.u)[row * a.ld_u + channel]);
     const float d = Step<T>(static_cast<float>(static_cast<const T*>(a.dt)[row * a.ld_dt + channel]) + (a.bias ? a.bias[channel] : 0.f), a.softplus).d;
-    const int group = channel / a.share;
+    const int group = a.groups > 1 ? channel / a.share : 0;
     const T* B = static_cast<const T*>(a.b.p) + row * a.b.row + group * a.b.group + first;
     const T* C = static_cast<const T*>(a.c.p) + row * a.c.row + group * a.c.group + first;
     const Values A = *reinterpret_cast<const Values*>(a.A + int64_t(channel) * a.N + first);
@@ -768,10 +773,11 @@ void scan_shape(ScanArgs& a, const spc_scan_desc* d) {
   a.blocks = (a.share + 63) / 64 * a.groups;
   a.softplus = d->softplus != 0;
 }
-// Rows of a segment, a multiple of `unit`: as few as give some `waves` waves, but not so few that the chain of a scene's segments takes longer than a segment.
+// Rows of a segment, a multiple of `unit`: as few as give some `waves` waves, but not so few that the chain of a scene's segments takes longer than a segment: a row of a wave that
+// has its SIMD for itself takes some 0.9 us in the two launches, a link of the chain 0.25 us, of which eight waves run at once.
 int segment_rows(const spc_scan_desc* d, int blocks, int waves, int unit, int most) {
   const int64_t fill = d->n_rows * blocks / waves;
-  const double chain = std::sqrt(double(d->n_rows) / d->n_scenes / 4);
+  const double chain = std::sqrt(double(d->n_rows) / d->n_scenes / CHAIN_WAVES * (0.25 / 0.9));
   const int64_t rows = std::max<int64_t>(fill, std::llround(chain));
   return static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(unit, (rows + unit - 1) / unit * unit)));
 }
@@ -817,7 +823,7 @@ extern "C" int spc_selective_scan_forward(const spc_scan_desc* d, const void* u,
   a.u = u, a.ld_u = ld_u, a.dt = dt, a.ld_dt = ld_dt, a.gate = gate, a.ld_gate = ld_gate, a.out = out, a.ld_out = ld_out;
   if (d->n_rows) a.b = low_rows(B), a.c = low_rows(C);
   a.A = A, a.skip = skip, a.bias = dt_bias, a.state_in = state_in, a.state_out = state_out;
-  a.scenes = {offsets, static_cast<int>(d->n_rows), d->n_scenes, segment_rows(d, a.blocks, 4096, 16, 4096)};
+  a.scenes = {offsets, static_cast<int>(d->n_rows), d->n_scenes, segment_rows(d, a.blocks, 4096, 8, 4096)};
   a.ids = a.scenes.ids();
   SPC_RETURN_IF(check_grid(a, 64));
   const bool cut = d->n_rows > a.scenes.seg_rows;
@@ -878,7 +884,7 @@ extern "C" int spc_selective_scan_backward(const spc_scan_desc* d, const void* d
   SPC_RETURN_IF(check_grid(a, 64 * waves));
   const bool shared = a.blocks > a.groups;
   const size_t low = ((size_t(d->n_rows) + 1) * a.groups * 2) << log_np, steps = size_t(a.ids) * a.channels, states = steps * np;
-  const size_t starts = size_t(a.ids) * (a.scenes.seg_rows / grad_rows(np)) * (np + 1) * a.channels;
+  const size_t starts = (size_t(a.ids) + d->n_rows / grad_rows(np)) * (np + 1) * a.channels;
   const size_t parts = size_t(a.ids) * (np + 2) * a.channels, low_parts = shared ? (size_t(a.blocks) * d->n_rows * 2) << log_np : 0;
   float* ws = static_cast<float*>(pool_alloc(scratch_bytes((low + 2 * states + steps + starts + parts + low_parts) * sizeof(float)), s));
   if (!ws) return SPC_ERR_NOMEM;
@@ -941,7 +947,7 @@ extern "C" int spc_selective_scan_step(const spc_scan_desc* d, const void* u, in
   by_dtype(d->dtype, [&](auto t) {
     using T = decltype(t);
     const int64_t threads = d->n_rows * d->channels << log_q;
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((threads + 255) / 256), dim3(256), 0, static_cast<hipStream_t>(stream), a, state, d->n_rows, log_q); };
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((threads + 255) / 256), dim3(256), 0, static_cast<hipStream_t>(stream), a, state, static_cast<unsigned>(d->n_rows), log_q); };
     if (vec == 4) gate ? go(scan_step_kernel<T, 4, true>) : go(scan_step_kernel<T, 4, false>);
     else gate ? go(scan_step_kernel<T, 1, true>) : go(scan_step_kernel<T, 1, false>);
   });

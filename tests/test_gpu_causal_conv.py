@@ -150,7 +150,7 @@ def test_long_scenes(lengths, c):
 
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 @pytest.mark.parametrize("width", [1, 2, 3, 4])
-@pytest.mark.parametrize("c", [5, 64, 90])
+@pytest.mark.parametrize("c", [5, 64, 90, 513, 519, 261])  # (the last piece of a row and the one before it in different waves, too)
 def test_rows_one_by_one(c, width, dtype):
     """The same bits as the scenes at once, and the same rows kept."""
     gen = torch.Generator().manual_seed(c + width)

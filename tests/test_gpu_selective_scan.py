@@ -205,6 +205,12 @@ def test_many_segments(N):
         close(getattr(g, name), ref[name], F32 if name in ("A", "skip", "dt_bias", "initial") else F32, name)
 
 
+@pytest.mark.parametrize("c,N", [(16, 4), (40, 33)])
+def test_many_short_scenes(c, N):
+    gen = torch.Generator().manual_seed(2)
+    check_all(*case(torch.randint(0, 5, (300,), generator=gen).tolist(), c, 1, N, F32))
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 @pytest.mark.parametrize("c,G,N", [(64, 1, 16), (1, 1, 1), (130, 2, 8), (65, 1, 3), (90, 3, 17), (20, 1, 64)])
 @pytest.mark.parametrize("gate,softplus", [(True, True), (False, False)])
