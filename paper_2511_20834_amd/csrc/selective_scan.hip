@@ -305,10 +305,11 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const ScanArgs a) {
 
 // A scene's segments one after the other: their own states -> the states behind them; with time running backward, what they send forward -> what arrives behind them.
 // A wave has 64 (state, channel) pairs and a share of the scene's segments, up to CHAIN_WAVES waves to a scene: each runs over its own from zeros, takes what the ones before
-// it come to, and runs over them again (500 segments, 512 channels of 16 states: 50 us by one wave each).
-constexpr int CHAIN_WAVES = 8;
+// it come to, and runs over them again.  Loads' latency bounds it, CHAIN_AHEAD of which are under way (500 segments, 512 channels of 16 states, us: one wave and 16 loads 50, eight
+// waves 19; with 120 k rows, 64 channels in 1750 segments the whole call 145, with 16 waves and 32 loads 138).
+constexpr int CHAIN_WAVES = 16, CHAIN_AHEAD = 32;
 __global__ __launch_bounds__(64 * CHAIN_WAVES) void scan_chain_kernel(const ScanArgs a, int np) {
-  constexpr int AHEAD = 16;
+  constexpr int AHEAD = CHAIN_AHEAD;
   __shared__ float sums[CHAIN_WAVES][64], decays[CHAIN_WAVES][64];
   const bool back = blockIdx.y;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -773,13 +774,13 @@ void scan_shape(ScanArgs& a, const spc_scan_desc* d) {
   a.blocks = (a.share + 63) / 64 * a.groups;
   a.softplus = d->softplus != 0;
 }
-// Rows of a segment, a multiple of `unit`: as few as give some `waves` waves, but not so few that the chain of a scene's segments takes longer than a segment: a row of a wave that
-// has its SIMD for itself takes some 0.9 us in the two launches, a link of the chain 0.25 us, of which eight waves run at once.
-int segment_rows(const spc_scan_desc* d, int blocks, int waves, int unit, int most) {
-  const int64_t fill = d->n_rows * blocks / waves;
-  const double chain = std::sqrt(double(d->n_rows) / d->n_scenes / CHAIN_WAVES * (0.25 / 0.9));
-  const int64_t rows = std::max<int64_t>(fill, std::llround(chain));
-  return static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(unit, (rows + unit - 1) / unit * unit)));
+// Rows of a segment, a multiple of `unit`: as few as give some `waves` waves, but not so few that the chain of a scene's segments takes longer than a segment, which balances at some
+// sqrt(rows) / 4, and, where there is work for every SIMD, about as many as make whole rounds of `round` waves.  us, at sqrt(rows) times 0.1 / 0.2 / 0.3: 30 k rows, 256 channels
+// 124 / 104 / 110, in rounds 101 / 98 (0.2, 0.3); 120 k rows, 64 channels 175 / 144 / 162, in rounds 138 / 134.  2118 rows, 64 channels: segments of 8 rows 28, 16 31, 32 39.
+int segment_rows(const spc_scan_desc* d, int blocks, int waves, int round, int unit) {
+  const double work = double(d->n_rows) * blocks, rows = std::max(work / waves, 0.25 * std::sqrt(double(d->n_rows) / d->n_scenes)), rounds = work / (rows * round);
+  const double units = rounds >= .5 ? std::ceil(work / (std::max(1., std::round(rounds)) * round) / unit) : std::round(rows / unit);
+  return static_cast<int>(std::min(4096., std::max(1., units) * unit));
 }
 int check_grid(const ScanArgs& a, int threads) {  // (a launch takes less than 2^32 threads)
   if (int64_t(a.ids) * a.blocks * threads < (int64_t(1) << 32) && (int64_t(a.scenes.n_scenes) * a.channels << log_padded(a.N)) < (int64_t(1) << 29)) return SPC_OK;
@@ -793,7 +794,7 @@ void launch_low(const ScanArgs& a, int log_np, hipStream_t s) {
 void launch_chain(const ScanArgs& a, int np, bool grad, hipStream_t s) {
   const int64_t groups = (int64_t(np) * a.channels + 63) / 64;
   // (waves that would have no segment, were all rows in one scene, are left out)
-  const int waves = std::min(CHAIN_WAVES, (a.scenes.n_rows / a.scenes.seg_rows + 16) / 16);
+  const int waves = std::min(CHAIN_WAVES, (a.scenes.n_rows / a.scenes.seg_rows + CHAIN_AHEAD) / CHAIN_AHEAD);
   hipLaunchKernelGGL(scan_chain_kernel, dim3(a.scenes.n_scenes * groups, grad ? 2 : 1), dim3(64 * waves), 0, s, a, np);
 }
 
@@ -823,7 +824,7 @@ extern "C" int spc_selective_scan_forward(const spc_scan_desc* d, const void* u,
   a.u = u, a.ld_u = ld_u, a.dt = dt, a.ld_dt = ld_dt, a.gate = gate, a.ld_gate = ld_gate, a.out = out, a.ld_out = ld_out;
   if (d->n_rows) a.b = low_rows(B), a.c = low_rows(C);
   a.A = A, a.skip = skip, a.bias = dt_bias, a.state_in = state_in, a.state_out = state_out;
-  a.scenes = {offsets, static_cast<int>(d->n_rows), d->n_scenes, segment_rows(d, a.blocks, 4096, 8, 4096)};
+  a.scenes = {offsets, static_cast<int>(d->n_rows), d->n_scenes, segment_rows(d, a.blocks, 8192, 1024, 8)};
   a.ids = a.scenes.ids();
   SPC_RETURN_IF(check_grid(a, 64));
   const bool cut = d->n_rows > a.scenes.seg_rows;
@@ -879,7 +880,7 @@ extern "C" int spc_selective_scan_backward(const spc_scan_desc* d, const void* d
   a.out = du, a.ld_out = ld_du, a.ddt = ddt, a.ld_ddt = ld_ddt, a.dgate = dgate, a.ld_dgate = ld_dgate;
   if (d->n_rows) a.b = low_rows(B), a.c = low_rows(C), a.db = low_rows(dB), a.dc = low_rows(dC);
   a.A = A, a.skip = skip, a.bias = dt_bias, a.state_in = state_in, a.dstate_out = dstate_out, a.dstate_in = dstate_in;
-  a.scenes = {offsets, static_cast<int>(d->n_rows), d->n_scenes, segment_rows(d, a.blocks, 4096, grad_rows(np), 4096)};
+  a.scenes = {offsets, static_cast<int>(d->n_rows), d->n_scenes, segment_rows(d, a.blocks, 4096, 512, grad_rows(np))};
   a.ids = a.scenes.ids();
   SPC_RETURN_IF(check_grid(a, 64 * waves));
   const bool shared = a.blocks > a.groups;
