@@ -18,7 +18,7 @@ namespace spc {
 namespace {
 
 constexpr int LIN_COLS = 32, LIN_K = 256, LIN_STEP = 64;  // a tile of weights: columns, bytes of each; places of two products
-constexpr int LIN_THREADS = 256, LIN_GROUPS = 4;  // groups of 16 rows a wave
+constexpr int LIN_THREADS = 256;
 constexpr int LIN_MAX_C = 65536;
 
 typedef _Float16 half2 __attribute__((ext_vector_type(2)));
@@ -56,11 +56,11 @@ __device__ inline void to_halves(Words4 v, half8 (&f)[2]) {
   }
 }
 
-// KS: steps of 64 places that a wave's rows are held for (0: they are read again for every tile of columns).  Lane l has row (column) l % 16 of every operand and 16 places of a
+// KS: steps of 64 places that a wave's rows are held for (0: they are read again for every tile of columns, 256 places at a time and those ahead).  RT: groups of 16 rows a wave.  Lane l has row (column) l % 16 of every operand and 16 places of a
 // step's 64 from 16 (l / 16) on, in two products of 32; of a result column l % 16 and rows 4 (l / 16) + r.
-template <typename T, int KS, bool WHOLE>
+template <typename T, int KS, int RT, bool WHOLE>
 __global__ __launch_bounds__(LIN_THREADS) void linear8_kernel(const LinearArgs a) {
-  constexpr int RT = LIN_GROUPS, STEPS = KS ? KS : LIN_K / LIN_STEP, WIDTH = STEPS * LIN_STEP / 16;  // steps and pieces of 16 bytes of a tile's line
+  constexpr int STEPS = KS ? KS : LIN_K / LIN_STEP, WIDTH = STEPS * LIN_STEP / 16;  // steps and pieces of 16 bytes of a tile's line
   constexpr int PIECES = LIN_COLS * WIDTH, MINE = (PIECES + LIN_THREADS - 1) / LIN_THREADS, MT = LIN_COLS / 16, TURNS = WIDTH >= 8 ? 16 : 8;  // of which each thread fetches so many
   __shared__ half8 tiles[2][LIN_COLS * WIDTH * 2];
   const int t = threadIdx.x, lane = t % 64, wave = t / 64, i = lane % 16, g = lane / 16;
@@ -108,12 +108,11 @@ __global__ __launch_bounds__(LIN_THREADS) void linear8_kernel(const LinearArgs a
       if (row0 + 16 * q < a.n) v[q] = piece16<WHOLE>(a.x + (row0 + 16 * q) * a.ld_x, k + 16 * g, a.c);
     }
   };
-  Words4 held[KS ? KS : 1][RT];  // (as bytes: in halves they would leave room for two workgroups a CU, not three)
+  Words4 held[STEPS][RT], ahead[KS ? 1 : STEPS][RT];  // (as bytes: halves would take twice the registers)
   fetch(tile_at(0), 0);
   fetch_scale(tile_at(0));
-  if constexpr (KS > 0)
 #pragma unroll
-    for (int s = 0; s < KS; ++s) rows(s * LIN_STEP, held[s]);
+  for (int s = 0; s < STEPS; ++s) rows(s * LIN_STEP, KS ? held[s] : ahead[KS ? 0 : s]);
   float sx[RT];
 #pragma unroll
   for (int q = 0; q < RT; ++q) sx[q] = row0 + 16 * q < a.n ? a.sx[row0 + 16 * q] : 0.f;
@@ -148,13 +147,20 @@ __global__ __launch_bounds__(LIN_THREADS) void linear8_kernel(const LinearArgs a
       __syncthreads();
       if (part + 1 < parts) fetch(ct, part + 1);
       else if (n + 1 < count) fetch(tile_at(n + 1), 0), fetch_scale(tile_at(n + 1));
+      if constexpr (KS == 0) {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+          for (int q = 0; q < RT; ++q) held[s][q] = ahead[s][q];
+        const int k = part + 1 < parts ? (part + 1) * LIN_K : 0;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) rows(k + s * LIN_STEP, ahead[s]);
+      }
 #pragma unroll
       for (int s = 0; s < STEPS; ++s) {
-        Words4 x[RT];
         half8 f[RT][2];
-        if constexpr (KS == 0) rows(part * LIN_K + s * LIN_STEP, x);
 #pragma unroll
-        for (int q = 0; q < RT; ++q) to_halves(KS ? held[KS ? s : 0][q] : x[q], f[q]);
+        for (int q = 0; q < RT; ++q) to_halves(held[s][q], f[q]);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
 #pragma unroll
@@ -207,25 +213,28 @@ extern "C" int spc_linear_f8(const void* x, int64_t ld_x, const float* x_scale, 
   if (reinterpret_cast<uintptr_t>(out) % (dtype == SPC_DTYPE_F32 ? 4 : 2)) return set_error(SPC_ERR_ARG, "out is not aligned to its type");
   LinearArgs a{static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(w), x_scale, w_scale, out, ld_x, ld_w, ld_out, n, c, cout, 1};
   const int all = (cout + LIN_COLS - 1) / LIN_COLS;
-  constexpr int ROWS = 64 * LIN_GROUPS;
-  const int64_t blocks = (n + ROWS - 1) / ROWS;
-  // columns are split between workgroups until there are some 1024 of them
-  const int splits = static_cast<int>(std::min<int64_t>(all, std::max<int64_t>(1, 512 / blocks)));
-  a.tiles = (all + splits - 1) / splits;
   by_dtype(dtype, [&](auto type) {
-    auto go = [&](auto kt, auto whole) {
-      hipLaunchKernelGGL((linear8_kernel<decltype(type), decltype(kt)::value, decltype(whole)::value>), dim3(blocks * ((all + a.tiles - 1) / a.tiles)), dim3(LIN_THREADS), 0,
+    auto go = [&](auto ks, auto rt, auto whole) {
+      constexpr int RT = decltype(rt)::value, ROWS = 64 * RT;
+      const int64_t blocks = (n + ROWS - 1) / ROWS;
+      // columns are split between workgroups until there are some 512 of them
+      const int splits = static_cast<int>(std::min<int64_t>(all, std::max<int64_t>(1, 512 / blocks)));
+      a.tiles = (all + splits - 1) / splits;
+      hipLaunchKernelGGL((linear8_kernel<decltype(type), decltype(ks)::value, RT, decltype(whole)::value>), dim3(blocks * ((all + a.tiles - 1) / a.tiles)), dim3(LIN_THREADS), 0,
                          static_cast<hipStream_t>(stream), a);
     };
-    auto with = [&](auto kt) {
-      if (c % 16 == 0) go(kt, std::true_type{});
-      else go(kt, std::false_type{});
+    auto with = [&](auto ks, auto rt) {
+      if (c % 16 == 0) go(ks, rt, std::true_type{});
+      else go(ks, rt, std::false_type{});
     };
     using std::integral_constant;
-    if (c <= 64) with(integral_constant<int, 1>{});
-    else if (c <= 128) with(integral_constant<int, 2>{});
-    else if (c <= 256) with(integral_constant<int, 4>{});
-    else with(integral_constant<int, 0>{});
+    const integral_constant<int, 2> two;
+    const integral_constant<int, 4> four;
+    if (c <= 64) with(integral_constant<int, 1>{}, four);
+    else if (c <= 128) with(integral_constant<int, 2>{}, four);
+    else if (c <= 256) with(integral_constant<int, 4>{}, four);
+    else if (c <= 512) with(integral_constant<int, 8>{}, two);
+    else with(integral_constant<int, 0>{}, two);
   });
   SPC_HIP_CHECK(hipGetLastError());
   return SPC_OK;
