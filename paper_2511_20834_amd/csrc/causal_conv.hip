@@ -9,6 +9,9 @@
 // A thread walks down `per` rows of a piece of 16 bytes of channels and keeps the last W - 1 rows (backward: of d as well) in registers, so everything is read once but
 // for the W - 1 rows in front (and behind) of its own, which the caches hold.  The bytes bound all of it.  Workgroups take segments of scenes; backward they
 // walk over several, keep the sums of dw and dbias and store them once; a second launch adds them up in a fixed order.
+//
+// us a pass (bytes at a copy's 4.76 TB/s): 120 k x 512 bf16, width 4, out of rows of 1024 53 (52); its gradients 121 (75); 70 k x 90 fp16, width 3, gradients 26 (8: a launch of 22, 72 % of the lanes have channels, rows twice, and one of 4); a row of 2048 streams of
+// 512 channels 6.0 in the kernel.
 #include <algorithm>
 #include <type_traits>
 
@@ -356,7 +359,8 @@ void conv_variant(int32_t dtype, int c, int width, bool silu, bool narrow, F&& f
   });
 }
 
-// How a workgroup's threads are dealt to pieces and rows: up to 64 pieces side by side; rows of a thread so that there are some 2048 workgroups, 4 to 16.
+// How a workgroup's threads are dealt to pieces and rows: up to 64 pieces side by side; rows of a thread so that there are some 2048 workgroups, 4 to 16 (120 k x 512, aiming at
+// 1024 / 2048 / 4096: 51 / 52 / 70 us, gradients 121 / 121 / 134; 70 k x 90 25.4 / 26.8 / 26.8).
 void conv_grid(ConvArgs& a, int vec, int64_t n_rows) {
   const int pieces = (a.c + vec - 1) / vec;
   a.log_tp = 0;

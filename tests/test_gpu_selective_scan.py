@@ -239,6 +239,21 @@ def test_long_streams_do_not_drift():
     assert abs(float(state) - ref) <= 10 * 64 * 2.0 ** -25
 
 
+def test_long_memories():
+    """20 000 rows of equal steps, decays l = exp(-1.3 x 2^-12), so 1 / (1 - l) = 3151 rows are remembered.  A row rounds its decay (an exp2 just below 1, a unit of
+    2^-24) and the state (2^-24): 2 x 2^-24, all one way at worst.  Segments of L rows (24 here) do that in their own sum and in their outputs, 2 L x 2^-24 each; between them the chain
+    does it once a segment, for 3151 / L remembered ones.  4 x 24 + 2 x 3151 / 24 = 359; row by row it could be 2 x 3151."""
+    n, d = 20_000, 1.3 * 2.0 ** -12
+    d = float(torch.tensor(d, dtype=torch.float32))
+    one = torch.ones(n, 1, 1, device="cuda")
+    y, state = B.spc_selective_scan_forward(torch.ones(n, 1, device="cuda"), torch.full((n, 1), d, device="cuda"), -torch.ones(1, 1, device="cuda"), one, one, softplus=False, want_state=True)
+    l = torch.exp(torch.tensor(-d, dtype=torch.float64))
+    t = torch.arange(1, n + 1, dtype=torch.float64)
+    ref = d * (1 - l ** t) / (1 - l)
+    assert ((y[:, 0].double().cpu() - ref).abs() / ref).max() <= 360 * 2.0 ** -24
+    assert abs(float(state) - float(ref[-1])) <= 360 * 2.0 ** -24 * float(ref[-1])
+
+
 def test_states_carry_on():
     k, dout, _ = case([400], 64, 1, 16, F32)
     y, state = B.spc_selective_scan_forward(**k, want_state=True)
