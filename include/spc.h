@@ -518,8 +518,8 @@ int spc_causal_conv_step(const void* x, int64_t ld_x, const float* weight, const
  *   y_t = sum over states of C_t h_t + skip u_t;   out_t = y_t gate_t / (1 + exp(-gate_t)) with a gate, y_t without.
  * channels / groups consecutive channels share a group's B and C.  States and sums are fp32 whatever the rows' type.  A decay near 1 is rounded to 24 bits a row: a
  * state is off by at most 2^-23 for every row that it remembers, of those since its segment's start (at most 4096 rows; a step has no such rounding).
- * At most 64 states, 65536 channels, 200000 scenes; scenes times channels times states (rounded up to a power of two) below 2^29, a step's streams times channels times
- * states below 2^31 (SPC_ERR_UNSUPPORTED above).
+ * At most 64 states, 65536 channels, 200000 scenes; with states rounded up to a power of two, scenes times channels times states below 2^29, a step's streams times channels
+ * times states below 2^31 (SPC_ERR_UNSUPPORTED above).
  */
 typedef struct spc_scan_desc {
   int32_t dtype;

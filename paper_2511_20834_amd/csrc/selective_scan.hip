@@ -948,7 +948,7 @@ extern "C" int spc_selective_scan_step(const spc_scan_desc* d, const void* u, in
   const int vec = d->states % 4 ? 1 : 4;
   int log_q = 0;
   while ((vec << log_q) < d->states) ++log_q;
-  if (d->n_rows >= (int64_t(1) << 31) / d->channels >> log_q) return set_error(SPC_ERR_UNSUPPORTED, "%lld streams of %d channels and %d states", static_cast<long long>(d->n_rows), d->channels, d->states);
+  if (d->n_rows > ((int64_t(1) << 31) - 1) / d->channels >> log_q) return set_error(SPC_ERR_UNSUPPORTED, "%lld streams of %d channels and %d states", static_cast<long long>(d->n_rows), d->channels, d->states);
   ScanArgs a{};
   scan_shape(a, d);
   a.u = u, a.ld_u = ld_u, a.dt = dt, a.ld_dt = ld_dt, a.gate = gate, a.ld_gate = ld_gate, a.out = out, a.ld_out = ld_out, a.b = low_rows(B), a.c = low_rows(C);

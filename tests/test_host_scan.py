@@ -147,6 +147,8 @@ def test_scan_has_limits():
         assert call(desc(scenes=0)) == call(desc(scenes=2)) == B.ERR_ARG
         assert call(desc(rows=BIG), at=P) == call(desc(scenes=200_001), at=P) == call(desc(scenes=200_000, channels=65_536), at=P, **wide) == B.ERR_UNSUPPORTED
     assert scan_step(desc(rows=1 << 24), ) == B.ERR_UNSUPPORTED
+    # (five states count as eight)
+    assert scan_step(desc(rows=1 << 28, channels=1, groups=1, states=5)) == scan_step(desc(rows=(1 << 28) // 3 + 1, channels=3, groups=1, states=5)) == B.ERR_UNSUPPORTED
     assert scan_step(desc(rows=0, scenes=-3), u=None, state=None) == scan(desc(rows=0), u=None, out=None) == B.OK
 
 
