@@ -55,7 +55,7 @@ __device__ inline float exp_of(float x) {
   const float h = x * L;
   if (!EXACT) return __builtin_amdgcn_exp2f(h);
   const float e = __builtin_amdgcn_exp2f(h), l = fmaf(x, REST, fmaf(x, L, -h));
-  return fabsf(h) < 200.f ? fmaf(e * l, .69314718f, e) : e;  // (2^l = 1 + l ln 2; infinite products keep out)
+  return fabsf(h) < 128.f ? fmaf(e * l, .69314718f, e) : e;  // (2^l = 1 + l ln 2; infinite powers keep out: times a rest below zero they would give NaN)
 }
 template <bool EXACT>
 __device__ inline float sigmoid_of(float x) {

@@ -231,3 +231,30 @@ def test_infinities_and_nan_reach_later_rows_of_their_channel_only():
     touched[38:40, 3] = True
     touched[70:74, 20] = True
     assert torch.equal(y2[~touched], y[~touched]) and not torch.isfinite(y2[38, 3])
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("width", [1, 4])
+@pytest.mark.parametrize("c", [16, 3])
+def test_activations_far_from_zero(c, width, dtype):
+    """Sums of -150 to 150 in steps of 1/64, where exp(-p) passes 2^128 at -88.7: the sigmoid, below 2^-126 from -87.3 on, may come out as zero there, which is |p| 2^-126 <= 2^-118
+    of y and twice that of its slope.  Everything else as above; the slope's error is relative to the sigmoid of the same sum: 2 es (1 + |p|) of it."""
+    gen = torch.Generator().manual_seed(c)
+    p = torch.arange(-150 * 64, 150 * 64 + 1, dtype=torch.float64) / 64
+    n = p.numel() // c
+    x = p[torch.randperm(p.numel(), generator=gen)[:n * c]].view(n, c).to(dtype).cuda()
+    dy, weight = matrix(n, c, dtype, gen), torch.zeros(c, width, device="cuda")
+    weight[:, -1] = 1
+    x64, dy64 = x.double(), dy.double()
+    sig = torch.sigmoid(x64)
+    y, slope, es = x64 * sig, sig * (1 + x64 * (1 - sig)), (x64.abs() + 8) * 2.0 ** -22
+    lost = dy64.abs() * (2 * es * (1 + x64.abs()) * sig + 2.0 ** -117)
+    got, _ = B.spc_causal_conv_forward(x, weight)
+    within(got, y, (es + U[dtype]) * y.abs() + 2.0 ** -118 + TINY[dtype], "y")
+    dx, dw, db, _ = B.spc_causal_conv_backward(dy, x, weight)
+    d = dy64 * slope
+    within(dx, d, lost + U[dtype] * d.abs() + TINY[dtype], "dx")
+    within(db, d.sum(0), (lost + 2.0 ** -15 * d.abs()).sum(0), "dbias")
+    within(dw[:, -1], (d * x64).sum(0), ((lost + 2.0 ** -15 * d.abs()) * x64.abs()).sum(0), "dweight")
+    rows = torch.zeros(n, width - 1, c, dtype=dtype, device="cuda")
+    assert torch.equal(B.spc_causal_conv_step(x, weight, rows), got)

@@ -374,3 +374,25 @@ def test_recorded_beside_eager_calls_on_other_streams():
         for out, _ in graphs:
             assert all(torch.equal(a, b) for a, b in zip(out, want))
         assert all(torch.equal(a, b) for a, b in zip(eager, want))
+
+
+def spread(n, c, dtype, gen):
+    """-150 to 150 in even steps, in any order."""
+    return torch.linspace(-150, 150, n * c, dtype=torch.float64)[torch.randperm(n * c, generator=gen)].view(n, c).to(dtype).cuda()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("which", ["gate", "dt"])
+def test_gates_and_steps_far_from_zero(which, dtype):
+    """exp(-gate) passes 2^128 at -88.7; steps of dt are exp(dt) below, dt above."""
+    gen = torch.Generator().manual_seed(8)
+    k, dout, dstate = case([200, 0, 100], 64, 1, 5, dtype)
+    k[which] = spread(300, 64, dtype, gen)
+    check_all(k, dout, dstate)
+    k, _, _ = case([1] * 300, 64, 1, 5, dtype)
+    k[which] = spread(300, 64, dtype, gen)
+    ref = wanted(k)
+    state = k["initial_state"]
+    y = B.spc_selective_scan_step(k["u"], k["dt"], k["A"], k["B"], k["C"], state, k["skip"], k["gate"], k["dt_bias"])
+    close(y, ref["y"], dtype, "y")
+    close(state, ref["state"], F32, "state")
