@@ -336,8 +336,8 @@ __global__ __launch_bounds__(64 * CHAIN_WAVES) void scan_chain_kernel(const Scan
   float h = start && is ? start[(int64_t(scene) * a.channels + channel) * a.N + n] : 0.f;
   float* p = (back ? a.behind : a.between) + int64_t(id) * each + at;
   const float* steps = a.steps + int64_t(id) * a.channels + channel;
-  const int links = back ? s.n : s.n - 1;  // (nothing is behind a scene's last segment)
-  const int share = max(AHEAD, (links + CHAIN_WAVES - 1) / CHAIN_WAVES), first = wave * share, end = min(links, first + share);
+  const int links = back ? s.n : s.n - 1, waves = blockDim.x / 64;  // (nothing is behind a scene's last segment)
+  const int share = max(AHEAD, (links + waves - 1) / waves), first = wave * share, end = min(links, first + share);
   // f(value, sum of d, link) of the share's links in their order
   auto over = [&](auto&& f) {
     for (int m0 = first; m0 < end; m0 += AHEAD) {
@@ -799,11 +799,13 @@ void launch_low(const ScanArgs& a, int log_np, hipStream_t s) {
   const int64_t n = (int64_t(a.scenes.n_rows) + 1) * a.groups << (log_np + 1);
   hipLaunchKernelGGL(scan_low_kernel<T>, dim3(std::min<int64_t>((n + 255) / 256, 8192)), dim3(256), 0, s, a.b, a.c, a.low, a.scenes.n_rows, a.groups, a.N, log_np);
 }
+// Waves that would have no segment, were all rows in one scene, are left out, and those that would take a launch to 2^32 threads.  (check_grid has fewer than 2^29 states and 200 000 scenes
+// pass, so that at most 2^23 + 200 000 workgroups have three waves left, both ways.)
 void launch_chain(const ScanArgs& a, int np, bool grad, hipStream_t s) {
-  const int64_t groups = (int64_t(np) * a.channels + 63) / 64;
-  // (waves that would have no segment, were all rows in one scene, are left out)
-  const int waves = std::min(CHAIN_WAVES, (a.scenes.n_rows / a.scenes.seg_rows + CHAIN_AHEAD) / CHAIN_AHEAD);
-  hipLaunchKernelGGL(scan_chain_kernel, dim3(a.scenes.n_scenes * groups, grad ? 2 : 1), dim3(64 * waves), 0, s, a, np);
+  const int64_t workgroups = (int64_t(np) * a.channels + 63) / 64 * a.scenes.n_scenes, ways = grad ? 2 : 1;
+  const int64_t some = (a.scenes.n_rows / a.scenes.seg_rows + CHAIN_AHEAD) / CHAIN_AHEAD, most = ((int64_t(1) << 32) - 1) / (64 * ways * workgroups);
+  const int waves = static_cast<int>(std::min<int64_t>({CHAIN_WAVES, some, most}));
+  hipLaunchKernelGGL(scan_chain_kernel, dim3(workgroups, ways), dim3(64 * waves), 0, s, a, np);
 }
 
 }  // namespace

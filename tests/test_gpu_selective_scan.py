@@ -396,3 +396,40 @@ def test_gates_and_steps_far_from_zero(which, dtype):
     y = B.spc_selective_scan_step(k["u"], k["dt"], k["A"], k["B"], k["C"], state, k["skip"], k["gate"], k["dt_bias"])
     close(y, ref["y"], dtype, "y")
     close(state, ref["state"], F32, "state")
+
+
+def many_scenes(n, scenes, c, N, gen):
+    """One long scene and many of a few rows; no decays, steps of one, whole numbers: every sum is exact."""
+    cuts = torch.randint(n - 4000, n + 1, (scenes - 1,), generator=gen).sort().values
+    at = torch.cat([torch.zeros(1, dtype=torch.long), cuts, torch.tensor([n])]).to(torch.int32).cuda()
+    one = torch.zeros(1, 1, N, device="cuda")
+    one[..., 3] = 1
+    u = torch.randint(-1, 2, (n, c), generator=torch.Generator("cuda").manual_seed(9), device="cuda").float()
+    k = {"u": u, "dt": torch.ones(n, c, device="cuda"), "A": torch.zeros(c, N, device="cuda"), "B": torch.ones(1, 1, N, device="cuda").expand(n, 1, N),
+         "C": one.expand(n, 1, N), "offsets": at}
+    scene = torch.searchsorted(at[1:].contiguous(), torch.arange(n, dtype=torch.int32, device="cuda"), right=True)
+    return k, at.long(), scene
+
+
+def test_chains_of_many_scenes():
+    """5000 scenes of 1024 channels of 64 states: sixteen waves for each 64 of their states would pass the 2^32 threads of a launch."""
+    k, at, scene = many_scenes(120_000, 5000, 1024, 64, torch.Generator().manual_seed(1))
+    y, _ = B.spc_selective_scan_forward(**k, softplus=False)
+    for c0 in range(0, 1024, 128):
+        total = torch.cat([torch.zeros(1, 128, dtype=torch.float64, device="cuda"), k["u"][:, c0:c0 + 128].double().cumsum(0)])
+        assert torch.equal(y[:, c0:c0 + 128].double(), total[1:] - total[at[scene]])
+
+
+def test_gradients_chains_of_many_scenes():
+    """34 900 scenes of 960 channels of 16 states: nine waves, both ways."""
+    k, at, scene = many_scenes(120_000, 34_900, 960, 16, torch.Generator().manual_seed(2))
+    dout = torch.randint(-1, 2, (120_000, 960), generator=torch.Generator("cuda").manual_seed(5), device="cuda").float()
+    g = B.spc_selective_scan_backward(dout, **k, softplus=False)
+    db = 0
+    for c0 in range(0, 960, 192):
+        total = torch.cat([torch.zeros(1, 192, dtype=torch.float64, device="cuda"), dout[:, c0:c0 + 192].double().cumsum(0)])
+        q = total[at[scene + 1]] - total[:-1]
+        u = k["u"][:, c0:c0 + 192].double()
+        assert torch.equal(g.u[:, c0:c0 + 192].double(), q) and torch.equal(g.dt[:, c0:c0 + 192].double(), q * u)
+        db = db + (q * u).sum(1)
+    assert torch.equal(g.B[:, 0, 3].double(), db)

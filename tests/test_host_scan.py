@@ -158,3 +158,10 @@ def test_scan_refuses_states_and_gradients():
     # (every row and group of an output has places of its own)
     for low in (B.AttnRows(P, 0, 16), B.AttnRows(P, 32, 0), B.AttnRows(P, 31, 16), B.AttnRows(P, 16, 600)):
         assert scan_back(db=low) == scan_back(dc=low) == B.ERR_ARG
+
+
+def test_scan_counts_states_of_all_scenes():
+    """2^29 of them, counted as powers of two, are too many (a chain of segments takes a lane for each)."""
+    for call in (scan, scan_back):
+        assert call(desc(scenes=1 << 16, channels=512, groups=1, states=16), at=P, ld_u=512, ld_dt=512, ld_out=512) == B.ERR_UNSUPPORTED
+        assert call(desc(scenes=1 << 16, channels=512, groups=1, states=9), at=P, ld_u=512, ld_dt=512, ld_out=512) == B.ERR_UNSUPPORTED
