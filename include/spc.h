@@ -530,7 +530,8 @@ typedef struct spc_scan_desc {
 } spc_scan_desc;
 /*
  *   u, dt, gate, out  [device] rows of `channels` elements, row pitches in elements; gate may be NULL; out overlaps no input.
- *   A           [device] channels x states floats, finite; usually below zero.
+ *   A           [device] channels x states floats, finite; usually below zero.  States may grow (d_t A above zero): a row's exp(d_t A) below 2^128, and states and gradients in 32 bits;
+ *               what is zero stays zero, however much the rows from one input to the next would have it grow.
  *   B, C        rows of `groups` heads of `states` elements (spc_attn_rows: row and group pitches, zero for a broadcast input).
  *   skip, dt_bias  [device] `channels` floats, NULL: zeros.
  *   offsets     as spc_linear_attention_forward's.  Rows in no scene are neither used nor written.

@@ -143,6 +143,16 @@ __device__ inline void load_between(float (&h)[NP], const float* p, const ScanAr
   for (int n = 0; n < NP; ++n) h[n] = me.some ? p[(int64_t(id) * ALL + first + n) * a.channels + me.channel] : 0.f;
 }
 
+// 2^w h + v.  GROWS: powers beyond 2^120 are taken by the state first, so that where a run of rows grows beyond 32 bits a state of zero stays zero, and one of little gets to where its rows
+// would bring it.  Elsewhere both are the same bits, and waves whose lanes are all there take the shorter one.
+constexpr float FAR = 120.f;
+template <bool GROWS>
+__device__ inline float carried(float w, float h, float v) {
+  if (!GROWS) return fmaf(__builtin_amdgcn_exp2f(w), h, v);
+  const int k = static_cast<int>(fmaxf(w - FAR, 0.f));
+  return fmaf(__builtin_amdgcn_exp2f(w - static_cast<float>(k)), ldexpf(h, k), v);
+}
+
 // A lane's place in a row behind a scalar address.  `stays`, in the block of the accesses: widened elsewhere, the compiler adds both up in vector registers.
 __device__ inline void stays(unsigned& at) { asm volatile("" : "+v"(at)); }
 template <typename T>
@@ -191,7 +201,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const ScanArgs a) {
   const Lane me(a, block, threadIdx.x % 64);
   if (!me.some) return;
   const float bias = a.bias ? a.bias[me.channel] : 0.f, skip = a.skip ? a.skip[me.channel] : 0.f;
-  float A2[NP], h[NP], sent[GRAD ? NP : 1] = {}, through[GRAD ? NP : 1], steps = 0.f;
+  float A2[NP], h[NP], sent[GRAD ? NP : 1] = {}, through[GRAD ? NP : 1], steps = 0.f, least = 0.f;
   rates<NP>(A2, a, me.channel, 0);
   if (SUMS) {
 #pragma unroll
@@ -234,6 +244,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const ScanArgs a) {
       }
     }
     if (SUMS) steps += d;
+    if (GRAD) least = fminf(least, d);
 #pragma unroll
     for (int k = 0; k < BLOCKS; ++k) {
       float ahead[2 * N1];
@@ -302,6 +313,35 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const ScanArgs a) {
     if (s.m == s.n - 1) store_state<NP>(h, a.state_out, a, s.scene, me, 0);
     return;
   }
+  if constexpr (GRAD) {
+    // Where decays may be above one, their products from the segment's first row on leave 32 bits (or come back from zero) though what they are multiplied by does not: such lanes take the
+    // recurrence from the last row on.
+    bool grows = least < 0.f;
+#pragma unroll
+    for (int n = 0; n < NP; ++n) grows |= A2[n] > 0.f;
+    if (__any(grows)) {
+      // (the arguments are read again: kept for this, they would push others out of the scalar registers in the loop above)
+      auto again = (const __attribute__((address_space(4))) ScanArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+      asm volatile("" : "+s"(again));
+      const auto& r = *again;
+      float back[NP] = {};
+      for (int t = s.rows - 1; t >= 0; --t) {
+        const int64_t row = int64_t(s.first) + t;
+        stays(at);
+        const float d = Step<T>(static_cast<float>(load_at<T>(row_of<T>(r.dt, row, r.ld_dt), at)) + bias, r.softplus).d;
+        float dy = static_cast<float>(load_at<T>(row_of<T>(r.dout, row, r.ld_dout), at));
+        if constexpr (GATED) {
+          const float z = static_cast<float>(load_at<T>(row_of<T>(r.gate, row, r.ld_gate), at));
+          dy *= z * sigmoid_of<EXACT>(z);
+        }
+        const Scalars from = (Scalars)(uintptr_t)(r.low + (row * r.groups + me.group) * (2 * NP));
+#pragma unroll
+        for (int n = 0; n < NP; ++n) back[n] = __builtin_amdgcn_exp2f(d * A2[n]) * fmaf(dy, from[n / N1 * (2 * N1) + N1 + n % N1], back[n]);
+      }
+#pragma unroll
+      for (int n = 0; n < NP; ++n) sent[n] = grows ? back[n] : sent[n];
+    }
+  }
   a.steps[int64_t(id) * a.channels + me.channel] = steps;
 #pragma unroll
   for (int n = 0; n < NP; ++n) {
@@ -318,7 +358,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const ScanArgs a) {
 constexpr int CHAIN_WAVES = 16, CHAIN_AHEAD = 32;
 __global__ __launch_bounds__(64 * CHAIN_WAVES) void scan_chain_kernel(const ScanArgs a, int np) {
   constexpr int AHEAD = CHAIN_AHEAD;
-  __shared__ float sums[CHAIN_WAVES][64], decays[CHAIN_WAVES][64];
+  __shared__ float sums[CHAIN_WAVES][64], powers[CHAIN_WAVES][64];
   const bool back = blockIdx.y;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int64_t each = int64_t(np) * a.channels, groups = (each + 63) / 64;
@@ -338,10 +378,10 @@ __global__ __launch_bounds__(64 * CHAIN_WAVES) void scan_chain_kernel(const Scan
   const float* steps = a.steps + int64_t(id) * a.channels + channel;
   const int links = back ? s.n : s.n - 1, waves = blockDim.x / 64;  // (nothing is behind a scene's last segment)
   const int share = max(AHEAD, (links + waves - 1) / waves), first = wave * share, end = min(links, first + share);
-  // f(value, sum of d, link) of the share's links in their order
+  // f(whether powers may leave 32 bits, value, sum of d, link) of the share's links in their order
   auto over = [&](auto&& f) {
     for (int m0 = first; m0 < end; m0 += AHEAD) {
-      float v[AHEAD], d[AHEAD];
+      float v[AHEAD], d[AHEAD], top = 0.f;
 #pragma unroll
       for (int q = 0; q < AHEAD; ++q) {
         const int k = min(m0 + q, end - 1), m = back ? s.n - 1 - k : k;
@@ -349,24 +389,30 @@ __global__ __launch_bounds__(64 * CHAIN_WAVES) void scan_chain_kernel(const Scan
         d[q] = steps[int64_t(m) * a.channels];
       }
 #pragma unroll
-      for (int q = 0; q < AHEAD; ++q)
-        if (m0 + q < end) f(v[q], d[q], back ? s.n - 1 - (m0 + q) : m0 + q);
+      for (int q = 0; q < AHEAD; ++q) top = fmaxf(top, A2 * d[q]);
+      auto with = [&](auto grows) {
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q)
+          if (m0 + q < end) f(grows, v[q], d[q], back ? s.n - 1 - (m0 + q) : m0 + q);
+      };
+      if (__any(top > FAR)) with(std::true_type{});
+      else with(std::false_type{});
     }
   };
   if (links > share) {  // (all waves of the workgroup alike)
     float sum = 0.f, steps_sum = 0.f;
-    over([&](float v, float d, int) {
-      sum = fmaf(__builtin_amdgcn_exp2f(A2 * d), sum, v);
+    over([&](auto grows, float v, float d, int) {
+      sum = carried<decltype(grows)::value>(A2 * d, sum, v);
       steps_sum += d;
     });
     sums[wave][lane] = sum;
-    decays[wave][lane] = __builtin_amdgcn_exp2f(A2 * steps_sum);
+    powers[wave][lane] = A2 * steps_sum;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) h = fmaf(decays[w][lane], h, sums[w][lane]);
+    for (int w = 0; w < wave; ++w) h = carried<true>(powers[w][lane], h, sums[w][lane]);
   }
   if (!there) return;
-  over([&](float v, float d, int m) {
-    const float after = fmaf(__builtin_amdgcn_exp2f(A2 * d), h, v);
+  over([&](auto grows, float v, float d, int m) {
+    const float after = carried<decltype(grows)::value>(A2 * d, h, v);
     p[m * each] = back ? h : after;  // (back: what arrives behind the segment)
     h = after;
   });
@@ -516,7 +562,14 @@ __global__ __launch_bounds__(64 * NP / grad_states(NP), 2) void scan_grad_kernel
     }
     float h[NG];
 #pragma unroll
-    for (int n = 0; n < NG; ++n) h[n] = chunk ? (me.some ? fmaf(__builtin_amdgcn_exp2f(A2[n] * in.steps), first_h[n], in.h[n]) : 0.f) : first_h[n];
+    for (int n = 0; n < NG; ++n) h[n] = chunk ? (me.some ? carried<false>(A2[n] * in.steps, first_h[n], in.h[n]) : 0.f) : first_h[n];
+    bool far = false;  // (made again where it has to be: a choice between the two takes registers that are not there, 1170 -> 1370 us a pass)
+#pragma unroll
+    for (int n = 0; n < NG; ++n) far |= A2[n] * in.steps > FAR;
+    if (chunk && __any(far)) {
+#pragma unroll
+      for (int n = 0; n < NG; ++n) h[n] = me.some ? carried<true>(A2[n] * in.steps, first_h[n], in.h[n]) : 0.f;
+    }
     __syncthreads();
     if (chunk) load(chunk - 1);
     float hs[L][NG], decay[KEEP ? L : 1][NG];

@@ -433,3 +433,44 @@ def test_gradients_chains_of_many_scenes():
         assert torch.equal(g.u[:, c0:c0 + 192].double(), q) and torch.equal(g.dt[:, c0:c0 + 192].double(), q * u)
         db = db + (q * u).sum(1)
     assert torch.equal(g.B[:, 0, 3].double(), db)
+
+
+def check_growing(k, dout, dstate):
+    k["dt_bias"] = None
+    check_all(k, dout, dstate, softplus=False)
+
+
+@pytest.mark.parametrize("lengths,c,N,rate,few", [([9000, 20], 5, 3, 1.2, 40), ([9000, 20], 3, 3, 8.0, 8), ([200, 3], 66, 2, 15.0, 5), ([300, 3], 3, 40, 15.0, 5)])
+def test_growing_states_stay_zero_until_an_input(lengths, c, N, rate, few):
+    """exp(d A) above one: what is zero stays zero, forward until the scene's last rows, backward behind its first ones, though the rows between would grow beyond 2^128."""
+    k, dout, dstate = case(lengths, c, 1, N, F32)
+    n = lengths[0]
+    k["A"] = torch.linspace(0.1, 1.0, c * N, device="cuda").view(c, N) * rate
+    k["A"][:, 1] *= -1
+    k["dt"] = torch.ones_like(k["dt"])
+    k["dt"][n:] = 0.1
+    k["u"][:n - few] = 0
+    dout[few:n] = 0
+    k["initial_state"][0], dstate[0] = 0, 0
+    check_growing(k, dout, dstate)
+
+
+def test_growing_states_of_little():
+    """States of 1e-36 that grow by exp(160), both ways: the powers pass 2^128, the states do not."""
+    k, dout, dstate = case([20], 70, 1, 5, F32)
+    k["A"], k["dt"] = torch.full_like(k["A"], 8.0), torch.ones_like(k["dt"])
+    k["u"].zero_()
+    k["initial_state"] *= 1e-36
+    dstate *= 1e-36
+    dout[:18], dout[18:] = 0, 1e-36 * dout[18:]
+    check_growing(k, dout, dstate)
+
+
+def test_steps_of_both_signs():
+    """Steps of 10 in rows 32 to 43, of -8 in rows 44 to 53: decays of exp(-120) that rows of exp(80) follow.  A gradient that comes from behind grows first and decays then."""
+    k, dout, dstate = case([9000], 3, 1, 2, F32, gate=False, states=False, skip=False)
+    k["A"], k["dt"] = torch.tensor([[-1.0, -0.9]] * 3, device="cuda"), torch.full_like(k["dt"], 0.01)
+    k["dt"][32:44], k["dt"][44:54] = 10, -8
+    k["u"][:44] = 0
+    dout[:54], dout[64:] = 0, 0
+    check_growing(k, dout, dstate)
