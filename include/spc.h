@@ -453,8 +453,8 @@ int spc_batch_offsets(const void* keys, int64_t n, const spc_pack_desc* d, int32
 
 /*
  * Root-mean-square norm of feature rows: z = x (+ residual), y = z / sqrt(mean(z^2) + eps) * gamma over the c channels of every row.  Arguments as
- * spc_layer_norm_forward's: sum receives z where there is a residual, rstd [device] n floats (may be NULL) what the backward pass needs.  A row whose squares
- * add up beyond 32 bits (values of 2^63 and more) comes out as zeros.
+ * spc_layer_norm_forward's: sum receives z where there is a residual, rstd [device] n floats (may be NULL) what the backward pass needs (with fewer
+ * bits, as 32 have below 2^-126, for rows of 2^126 and more).
  */
 int spc_rms_norm_forward(const void* x, int64_t ld_x, const void* residual, int64_t ld_r, const float* gamma, float eps,
                          void* y, int64_t ld_y, void* sum, int64_t ld_s, float* rstd, int64_t n, int32_t c, int32_t dtype,

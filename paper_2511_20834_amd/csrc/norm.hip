@@ -325,10 +325,21 @@ __global__ __launch_bounds__(NORM_THREADS) void rms_forward_kernel(const RmsArgs
       float s = 0.f;
 #pragma unroll
       for (int k = 0; k < R::E; ++k) s += FIT != MOVED || me.counts(k) ? z[k] * z[k] : 0.f;  // (places behind the last channel hold zeros)
-      const float rstd = 1.f / sqrtf(row_sum<G>(s, lds) / c + a.eps);
+      s = row_sum<G>(s, lds);
+      float unit = 1.f;
+      if (s == INFINITY) {  // values of 2^64 / sqrt(c) and more: the same in units of 2^80, where up to 8192 squares fit (all lanes of the row alike)
+        unit = 0x1p-80f, s = 0.f;
+#pragma unroll
+        for (int k = 0; k < R::E; ++k) {
+          z[k] *= unit;
+          s += FIT != MOVED || me.counts(k) ? z[k] * z[k] : 0.f;
+        }
+        s = row_sum<G>(s, lds);
+      }
+      const float rstd = 1.f / sqrtf(s / c + a.eps * (unit * unit));
 #pragma unroll
       for (int k = 0; k < R::E; ++k) z[k] = z[k] * rstd * gamma[k];
-      if (threadIdx.x % G == 0 && a.rstd) a.rstd[row] = rstd;
+      if (threadIdx.x % G == 0 && a.rstd) a.rstd[row] = rstd * unit;
     }
     if (FORM == SAME) {
       me.store(z, a.y, row, a.ld_y);

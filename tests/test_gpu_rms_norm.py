@@ -259,3 +259,31 @@ def test_norm_and_product_recorded():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("c", [1, 3, 64, 90, 257, 1024, 2051, 8192])
+@pytest.mark.parametrize("extra", [False, True])
+def test_rows_of_large_values(extra, c, dtype):
+    """Rows of 2^50 to 2^124, whose squares add up beyond 32 bits: tolerances as everywhere, with the type's spacing near zero where rstd and its products are as small."""
+    gen = torch.Generator().manual_seed(c)
+    size = 2.0 ** torch.arange(50, 125, dtype=torch.float64)[:, None]
+    big = lambda: (torch.randn(75, c, generator=gen).clamp(-4, 4) * size).to(dtype).cuda()  # noqa: E731
+    x, r, dy = big(), big() if extra else None, rows(75, c, dtype, gen)
+    gamma = (1 + torch.randn(c, generator=gen)).cuda()
+    y, s, rstd = B.spc_rms_norm_forward(x, gamma, eps=EPS, residual=r, want_stats=True)
+    z, rs, h, ref = reference(x, r, gamma)
+    near = {BF16: 2.0 ** -133, F32: 2.0 ** -149}[dtype]
+    within(rstd, rs, 2.0 ** -18 * rs + 2.0 ** -149, "rstd")
+    within(y, ref, (U[dtype] + 2.0 ** -17) * ref.abs(), "y")
+    q, scale, s8, rstd8 = B.spc_rms_norm_quantize(x, gamma, eps=EPS, residual=r, want_stats=True)
+    check_bytes(q, scale, ref, 2.0 ** -17, "q")
+    assert torch.equal(rstd8, rstd) and (s8 is None if r is None else torch.equal(s8, s))
+    x = x if s is None else s
+    dx, dgamma = B.spc_rms_norm_backward(dy, x, rstd, gamma)
+    k = rstd.double()[:, None]
+    h, w = x.double() * k, dy.double() * gamma.double()
+    ref = k * (w - h * (w * h).mean(1, keepdim=True))
+    lost = 2.0 ** -17 * k * (w.abs() + h.abs() * (w * h).abs().mean(1, keepdim=True))
+    within(dx, ref, (U[dtype] + 2.0 ** -23) * ref.abs() + near + lost, "dx")
+    within(dgamma, (dy.double() * h).sum(0), 2.0 ** -16 * (dy.double() * h).abs().sum(0), "dgamma")
