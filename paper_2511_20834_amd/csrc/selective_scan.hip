@@ -954,35 +954,26 @@ extern "C" int spc_selective_scan_backward(const spc_scan_desc* d, const void* d
   if (!ws) return SPC_ERR_NOMEM;
   a.low = ws, a.between = ws + low, a.behind = a.between + states, a.steps = a.behind + states, a.starts = a.steps + steps;
   a.parts = a.starts + starts, a.low_parts = shared ? a.parts + parts : nullptr;
-  int rc = SPC_OK;
   scan_variant(d, gate != nullptr, [&](auto t, auto n, auto g) {
     using T = decltype(t);
     constexpr int NP = decltype(n)::value;
     constexpr bool GATE = decltype(g)::value;
     constexpr size_t lds = sizeof(GradLds<NP, GATE>);
-    constexpr auto kernel = scan_grad_kernel<T, NP, GATE>;
-    if constexpr (lds > 64 * 1024) {
-      static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
-      if (attr != hipSuccess) {
-        rc = set_error(SPC_ERR_HIP, "hipFuncSetAttribute failed: %s", hipGetErrorString(attr));
-        return;
-      }
-    }
+    static_assert(lds <= 64 * 1024, "what a launch may ask for by itself");
     if (d->n_rows) {
       launch_low<T>(a, log_np, s);
       hipLaunchKernelGGL((scan_kernel<T, NP, GATE, true, true>), dim3((a.ids * a.blocks + 3) / 4), dim3(SCAN_THREADS), 0, s, a);
       launch_chain(a, np, true, s);
     }
-    hipLaunchKernelGGL(kernel, dim3(a.ids * a.blocks), dim3(64 * waves), lds, s, a);
+    hipLaunchKernelGGL((scan_grad_kernel<T, NP, GATE>), dim3(a.ids * a.blocks), dim3(64 * waves), lds, s, a);
     if (shared && d->n_rows) {
       const int64_t m = d->n_rows * a.groups << (log_np + 1);
       hipLaunchKernelGGL(scan_low_grad_kernel<T>, dim3(std::min<int64_t>((m + 255) / 256, 8192)), dim3(256), 0, s, a, log_np);
     }
   });
-  if (rc == SPC_OK && (dA || dskip || ddt_bias))
+  if (dA || dskip || ddt_bias)
     hipLaunchKernelGGL(scan_params_kernel, dim3(((np + 2) * a.channels + 31) / 32), dim3(1024), 0, s, a.parts, a.ids, np, a.channels, a.N, dA, dskip, ddt_bias);
   pool_free(ws, s);
-  SPC_RETURN_IF(rc);
   SPC_HIP_CHECK(hipGetLastError());
   return SPC_OK;
 }
