@@ -478,7 +478,7 @@ int spc_rms_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_t 
                           const void* dsum, int64_t ld_ds, void* dx, int64_t ld_dx, float* dgamma, int64_t n, int32_t c,
                           int32_t dtype, void* stream);
 /*
- * A 1x1x1 layer in 8 bits: out[r][j] = x_scale[r] * w_scale[j] * sum over k of x[r][k] w[j][k], e4m3 values added up in 32 bits.
+ * A 1x1x1 layer in 8 bits: out[r][j] = x_scale[r] * w_scale[j] * sum over k of x[r][k] w[j][k], e4m3 values added up in 32 bits (which the sum times x_scale[r] has to fit, too).
  *   x         [device] n rows of c bytes, pitch ld_x in bytes, any address; x_scale n floats (spc_rms_norm_quantize, spc_quantize_rows).
  *   w         [device] cout rows of c bytes, pitch ld_w: the layer's weights with output channels as rows; w_scale cout floats.
  *   out       [device] n rows of cout elements of dtype, pitch ld_out in elements; overlaps no input.
@@ -491,7 +491,8 @@ int spc_linear_f8(const void* x, int64_t ld_x, const float* x_scale, const void*
  * Short causal convolution of every channel along the rows of its scene: p_t = bias + sum over k < width of weight[width-1-k] x_{t-k}, y_t = p_t / (1 + exp(-p_t))
  * with silu, p_t without.  Sums are held in 32 bits.
  *   x, y        [device] n rows of c elements, pitches ld_x, ld_y; y overlaps no input.
- *   weight      [device] c x width floats, bias c floats (may be NULL), whatever the rows' type; width 1 to 4, c at most 65536 (SPC_ERR_UNSUPPORTED above).
+ *   weight      [device] c x width floats, bias c floats (may be NULL), whatever the rows' type; width 1 to 4, c at most 65536, n_scenes 200000 and
+ *               n_scenes times c 2^31 (SPC_ERR_UNSUPPORTED above).
  *   offsets     [device] n_scenes + 1 ascending row numbers (spc_batch_offsets); NULL: one scene of all rows.  Rows in no scene are neither
  *               used nor written.
  *   rows_in     [device] [n_scenes][width - 1][c] of the rows' type: the rows in front of each scene, oldest first; NULL: zeros.
@@ -508,7 +509,10 @@ int spc_causal_conv_backward(const void* dy, int64_t ld_dy, const void* x, int64
                              int32_t width, int32_t silu, const int32_t* offsets, int32_t n_scenes, const void* rows_in,
                              const void* drows_out, void* dx, int64_t ld_dx, float* dweight, float* dbias, void* drows_in,
                              int64_t n, int32_t c, int32_t dtype, void* stream);
-/* One more row of n independent streams: rows [device] [n][width - 1][c] (not read where width is 1) are the streams' last rows, updated in place. */
+/*
+ * One more row of n independent streams: rows [device] [n][width - 1][c] (not read where width is 1) are the streams' last rows, updated in place.  y overlaps no input.  n times the
+ * pieces of 16 bytes of a row is at most 2^31 (SPC_ERR_UNSUPPORTED above).
+ */
 int spc_causal_conv_step(const void* x, int64_t ld_x, const float* weight, const float* bias, int32_t width, int32_t silu,
                          void* rows, void* y, int64_t ld_y, int64_t n, int32_t c, int32_t dtype, void* stream);
 
@@ -518,8 +522,8 @@ int spc_causal_conv_step(const void* x, int64_t ld_x, const float* weight, const
  *   y_t = sum over states of C_t h_t + skip u_t;   out_t = y_t gate_t / (1 + exp(-gate_t)) with a gate, y_t without.
  * channels / groups consecutive channels share a group's B and C.  States and sums are fp32 whatever the rows' type.  A decay near 1 is rounded to 24 bits a row: a
  * state is off by at most 2^-23 for every row that it remembers, of those since its segment's start (at most 4096 rows; a step has no such rounding).
- * At most 64 states, 65536 channels, 200000 scenes; with states rounded up to a power of two, scenes times channels times states below 2^29, a step's streams times channels
- * times states below 2^31 (SPC_ERR_UNSUPPORTED above).
+ * At most 64 states, 65536 channels, 200000 scenes; with states rounded up to a power of two (four at least), scenes times channels times states below 2^29; with every group's
+ * channels rounded up to a multiple of 64, scenes times channels at most 2^28; a step's streams times channels times states (to a power of two) below 2^31 (SPC_ERR_UNSUPPORTED above).
  */
 typedef struct spc_scan_desc {
   int32_t dtype;

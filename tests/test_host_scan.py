@@ -165,3 +165,13 @@ def test_scan_counts_states_of_all_scenes():
     for call in (scan, scan_back):
         assert call(desc(scenes=1 << 16, channels=512, groups=1, states=16), at=P, ld_u=512, ld_dt=512, ld_out=512) == B.ERR_UNSUPPORTED
         assert call(desc(scenes=1 << 16, channels=512, groups=1, states=9), at=P, ld_u=512, ld_dt=512, ld_out=512) == B.ERR_UNSUPPORTED
+
+
+def test_limits_of_launches():
+    """Groups of one channel take a wave each; what a launch does not hold is refused before anything is enqueued."""
+    one = B.AttnRows(P, 512, 1)
+    many = dict(at=P, ld_u=512, ld_dt=512, ld_out=512, b=one, c=one)
+    assert scan_back(desc(scenes=60_000, channels=512, groups=512, states=1), **many, db=one, dc=one) == B.ERR_UNSUPPORTED  # (scenes x channels to 64 each: 2^30.9)
+    assert scan(desc(scenes=200_000, channels=512, groups=512, states=1), **many) == B.ERR_UNSUPPORTED
+    assert conv(c=65536, ld_x=65536, ld_y=65536, at=P, scenes=200_000, n=10, dtype=F32) == B.ERR_UNSUPPORTED
+    assert conv_step(n=(1 << 30) + 1, c=9, ld_x=9, ld_y=9) == conv_step(n=(1 << 29) + 1, c=13, ld_x=13, ld_y=13, dtype=F32) == B.ERR_UNSUPPORTED
