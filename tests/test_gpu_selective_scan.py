@@ -474,3 +474,9 @@ def test_steps_of_both_signs():
     k["u"][:44] = 0
     dout[:54], dout[64:] = 0, 0
     check_growing(k, dout, dstate)
+
+
+@pytest.mark.parametrize("c,N", [(20, 5), (3, 40)])
+def test_long_chains(c, N):
+    """More than 800 segments in a scene, both ways, so that every wave of a chain has more than one batch of 32; a short scene beside it."""
+    check_all(*case([40_000, 50], c, 1, N, F32))
