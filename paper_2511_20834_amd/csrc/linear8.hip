@@ -10,9 +10,10 @@
 // operand and a tile's lines are dealt to its 16 x 16 products so that a lane ends up with pieces of 16 bytes of one output row, next to its neighbours': every store of a
 // wave fills 64 consecutive bytes of 16 rows.
 //
-// 120 k x 256 -> 1024 to fp16: 92 us (0.69 PFLOP/s; torch's 8192^3 product reaches 1.15) for 58 of bytes; two waves a SIMD take turns at conversions and products (vector unit 53 % of the
-// CUs' cycles).  Tiles and rows a wave, us: 32 columns, 64 rows 91; 64, 32 105; 32, 32 102; 64, 64 120 (registers for one wave a SIMD).  All workgroups at the
-// same columns at once 128.  Rows' scales and columns' loaded where they are used 99.  60 k x 512 -> 512 45 (rows read again for every tile, 64 a wave: 90).  Small calls are the host's:
+// 120 k x 256 -> 1024 to fp16: 94 us (0.67 PFLOP/s; torch's 8192^3 product reaches 1.15) for 58 of bytes and 55 of products; two waves a SIMD take turns at conversions and products (vector
+// unit 53 % of the CUs' cycles; a wave's rows become halves again for each of 32 tiles).  Stores of halves to LDS use every other slot of 16 bytes: 1.9 M conflicts in 1.2 M instructions.  Tiles and rows a wave, us: 32 columns, 64 rows 91; 64, 32 105; 32, 32 102; 64, 64 120 (registers for one wave a SIMD).  All workgroups at the
+// same columns at once 128.  Rows' scales and columns' loaded where they are used 99.  60 k x 512 -> 512 47 (rows read again for every tile, 64 a wave: 90).  120 k x 128 -> 512 36 for 29 of bytes, 120 k x 64 -> 256 to fp32 28 for 27.  Rows of
+// more than 512 channels are read and made halves again for every 32 columns: 30 k x 1500 -> 512 175 for 40 of products.  Small calls are the host's:
 // 6011 x 128 -> 512 9.0 (kernel 6.2), one row 10.4.
 #include <algorithm>
 #include <type_traits>
@@ -113,7 +114,7 @@ __global__ __launch_bounds__(LIN_THREADS) void linear8_kernel(const LinearArgs a
       if (row0 + 16 * q < a.n) v[q] = piece16<WHOLE>(a.x + (row0 + 16 * q) * a.ld_x, k + 16 * g, a.c);
     }
   };
-  Words4 held[STEPS][RT], ahead[KS ? 1 : STEPS][RT];  // (as bytes: halves would take twice the registers)
+  Words4 held[STEPS][RT], ahead[KS ? 1 : STEPS][RT];  // (as bytes: halves of 256 channels would take 128 registers; those of up to 128 would fit, which was not measured)
   fetch(tile_at(0), 0);
   fetch_scale(tile_at(0));
 #pragma unroll

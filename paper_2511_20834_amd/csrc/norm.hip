@@ -286,7 +286,8 @@ __global__ __launch_bounds__(1024) void norm_params_kernel(const float* __restri
 
 // Root-mean-square norm: z = x + r, s = 1/sqrt(mean(z^2) + eps), y = z s gamma; or y in 8 bits: a = the row's largest |y|, q = e4m3(y 448 / a), scale = a / 448,
 // so that q scale is y.  BARE_BYTES: the rows themselves in 8 bits.  Layer norm's rows in registers and its shapes; the bytes bound these, too.  us a pass among others (bytes at a copy's
-// 4.76 TB/s): 120 k x 256 bf16 to 8 bits with a residual 42 (45; the kernel 35), gradients 240 k x 256 bf16 93 (103), 2118 x 64 fp32 9.0, which is the host's call (kernel 2.8).
+// 4.76 TB/s): 120 k x 256 bf16 to 8 bits with a residual 42 (45; the kernel 35), gradients 240 k x 256 bf16 93 (103), 2118 x 64 fp32 9.0, which is the host's call (kernel 2.8); 120 k x 256 bf16 rows to 8 bits as
+// they are 16 (19: caches hold them).
 enum Form { SAME, BYTES, BARE_BYTES };
 constexpr float F8_MOST = 448.f;              // e4m3's largest value
 constexpr float F8_LEAST = 0x1p-100f;         // rows below this are scaled as if it were their largest value: 448 / a stays finite, zeros stay zeros

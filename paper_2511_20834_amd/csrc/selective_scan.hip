@@ -13,11 +13,11 @@
 //
 // The vector unit bounds it: a state and row take an exponential (as long as three products) and three products or sums in the sums, four in the outputs, a row some thirty
 // instructions more for step size and gate.  120 k rows of 512 channels of 16 states, bf16, us (share of the CUs' cycles in which the vector unit issues, an instruction counted as four
-// cycles): 437, for 105 that the bytes take once at a copy's 4.76 TB/s and 141 for the exponentials and
-// products of one pass.  Gradients 1176, bytes 184.  Fastest dispatches under a profiler, which add up to a tenth more
-// than a pass without one: B and C 14, sums 192 (98 %), chain 29, outputs 247 (95 %); gradients: B and C 14, sums both ways 308 (91 %), chain 19, the way back 855 (87 %), dB and dC 27,
+// cycles): 439, for 105 that the bytes take once at a copy's 4.76 TB/s and 141 for the exponentials and
+// products of one pass.  Gradients 1172, bytes 184.  Fastest dispatches under a profiler, which add up to a tenth more
+// than a pass without one: B and C 14, sums 190 (98 %), chain 30, outputs 246 (95 %); gradients: B and C 14, sums both ways 309 (92 %), chain 21, the way back 860 (87 %), dB and dC 27,
 // parameters 8.
-// Small calls wait for launches and memory: 2118 rows of 64 channels, fp32, 28, in launches of some 2.5, 7, 10.5, 7.  First version, a row's loads where they are used: 653 and 2780.
+// Small calls wait for launches and memory: 2118 rows of 64 channels, fp32, 28, in launches of some 2.5, 7, 11.3, 7.  First version, a row's loads where they are used: 653 and 2780.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -354,7 +354,8 @@ __global__ __launch_bounds__(SCAN_THREADS) void scan_kernel(const ScanArgs a) {
 // A scene's segments one after the other: their own states -> the states behind them; with time running backward, what they send forward -> what arrives behind them.
 // A wave has 64 (state, channel) pairs and a share of the scene's segments, up to CHAIN_WAVES waves to a scene: each runs over its own from zeros, takes what the ones before
 // it come to, and runs over them again.  Loads' latency bounds it, CHAIN_AHEAD of which are under way (500 segments, 512 channels of 16 states, us: one wave and 16 loads 50, eight
-// waves 19; with 120 k rows, 64 channels in 1750 segments the whole call 145, with 16 waves and 32 loads 138).
+// waves 19; with 120 k rows, 64 channels in 1750 segments the whole call 145, with 16 waves and 32 loads 138, 135 now).
+// Growing links have code of their own, which costs calls that are launches a percent (6011 rows, gradients 74.0 -> 74.8; one code for all, longer, 74.4, and 120 k rows, 64 channels 134.8 -> 135.3).
 constexpr int CHAIN_WAVES = 16, CHAIN_AHEAD = 32;
 __global__ __launch_bounds__(64 * CHAIN_WAVES) void scan_chain_kernel(const ScanArgs a, int np) {
   constexpr int AHEAD = CHAIN_AHEAD;
@@ -733,8 +734,8 @@ __global__ __launch_bounds__(256) void scan_low_grad_kernel(const ScanArgs a, in
 }
 
 // ---------------------------------------------------------------- one row of many streams
-// A lane has VEC states of a channel, 2^log_q neighbouring lanes have a channel's; states are read and written once (2048 streams of 512 channels of 16 states, fp16: 36.5 us for
-// 142 MB, the vector unit issues in 86 % of the CUs' cycles).  The decay is taken as 1 + (e^w - 1) where it is near 1: rounded to 24 bits every row, a stream's long memory would
+// A lane has VEC states of a channel, 2^log_q neighbouring lanes have a channel's; states are read and written once (2048 streams of 512 channels of 16 states, fp16: 36.6 us for
+// 142 MB, the vector unit issues in 78 % of the CUs' cycles).  The decay is taken as 1 + (e^w - 1) where it is near 1: rounded to 24 bits every row, a stream's long memory would
 // drift (of shorter ones, up to 16 rows, it is off by some 16 x 2^-23).
 template <typename T, int VEC, bool GATE>
 __global__ __launch_bounds__(256) void scan_step_kernel(const ScanArgs a, float* state, unsigned n, int log_q) {

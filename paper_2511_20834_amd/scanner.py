@@ -61,7 +61,8 @@ class VoxelScan:
         """x (and residual): rows in sorted order; all_rows: every row lies in a scene.  Returns (result, s), and with `save` what backward needs."""
         inside = u = o = None
         if save and not all_rows and offsets is not None:
-            # backward adds up products over all rows, so both factors have to be finite in rows of no scene and one of them zero
+            # backward adds up products over all rows, so both factors have to be finite in rows of no scene and one of them zero (us without and with it: 120 k x 256, 512 channels
+            # of 16 states, fp16 965 and 1115, backward 7056 and 7198; 2118 x 64, 128 of 16, fp32 83 and 139, 260 and 307)
             row = torch.arange(x.shape[0], dtype=torch.int32, device=x.device)
             inside = ((row >= offsets[0]) & (row < offsets[-1]))[:, None]
             x, residual = torch.where(inside, x, 0), None if residual is None else torch.where(inside, residual, 0)
